@@ -1,5 +1,5 @@
-"""Thin Python binding of the C ABI in include/pam_lattice.h (and the benchmark's
-row-copy probe in include/pam_probe.h).
+"""Thin Python binding of the C ABI in include/pam_lattice.h and
+include/pam_attn.h (and the benchmark's row-copy probe in include/pam_probe.h).
 
 Argument marshalling only: every step of the filter runs in the HIP
 library ``libpam_lattice.so``.  PyTorch provides device memory and the
@@ -37,7 +37,18 @@ EXPORTS = (
     "pam_last_error", "pam_lattice_build_groups", "pam_lattice_export_groups", "pam_filter_fwd_asym",
     "pam_filter_bwd_asym", "pam_block_fwd", "pam_block_bwd_workspace", "pam_block_bwd", "pam_block_bwd_noalloc",
     "pam_probe_copy_rows",
+    "pam_diff_attn_fwd_workspace", "pam_diff_attn_bwd_workspace", "pam_diff_attn_fwd", "pam_diff_attn_bwd",
+    "pam_rotary_frequencies", "pam_rotary_table", "pam_rotary", "pam_dropout", "pam_norm_gate_fwd",
+    "pam_norm_gate_bwd_workspace", "pam_norm_gate_bwd",
 )
+
+# pam_dtype_t
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+PAM_ATTN_CAUSAL = 1
+PAM_ROTARY_INTERLEAVED = 1
+PAM_ROTARY_INVERSE = 2
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3}
+NORMS = {"rms": 0, "layer": 1}
 
 
 class BlockDesc(ctypes.Structure):
@@ -45,6 +56,31 @@ class BlockDesc(ctypes.Structure):
     _fields_ = [("c_in", ctypes.c_int32), ("d_tot", ctypes.c_int32), ("c_tot", ctypes.c_int32),
                 ("groups", ctypes.c_int32), ("dims", ctypes.c_int32 * 3), ("mesh_scale", ctypes.c_float),
                 ("slope", ctypes.c_float)]
+
+
+class DiffAttnDesc(ctypes.Structure):
+    """pam_diff_attn_desc_t of the C header."""
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("dim_v", ctypes.c_int32),
+                ("len_q", ctypes.c_int32), ("len_k", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("scale", ctypes.c_float), ("q_stride", ctypes.c_int64 * 4), ("k_stride", ctypes.c_int64 * 4),
+                ("v_stride", ctypes.c_int64 * 3)]
+
+
+class RotaryDesc(ctypes.Structure):
+    """pam_rotary_desc_t of the C header."""
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("length", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("pairs", ctypes.c_int32), ("flags", ctypes.c_uint32), ("start", ctypes.c_int64),
+                ("entries", ctypes.c_int64), ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3)]
+
+
+class NormDesc(ctypes.Structure):
+    """pam_norm_desc_t of the C header."""
+    _fields_ = [("dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("channels", ctypes.c_int32), ("eps", ctypes.c_float), ("gate_rows", ctypes.c_int64),
+                ("x_stride", ctypes.c_int64), ("z_stride", ctypes.c_int64), ("p", ctypes.c_double),
+                ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64)]
 
 _lib = None
 _vp = ctypes.c_void_p
@@ -105,6 +141,28 @@ def lib():
     L.pam_timing_read.argtypes = [_vp, _i32, ctypes.POINTER(_i64), ctypes.POINTER(ctypes.c_double)]
     L.pam_probe_copy_rows.restype = ctypes.c_int
     L.pam_probe_copy_rows.argtypes = [_vp, _vp, _vp, _i64, _i32, _i32, _vp]
+    L.pam_diff_attn_fwd_workspace.restype = ctypes.c_size_t
+    L.pam_diff_attn_fwd_workspace.argtypes = [ctypes.POINTER(DiffAttnDesc)]
+    L.pam_diff_attn_bwd_workspace.restype = ctypes.c_size_t
+    L.pam_diff_attn_bwd_workspace.argtypes = [ctypes.POINTER(DiffAttnDesc)]
+    L.pam_diff_attn_fwd.restype = ctypes.c_int
+    L.pam_diff_attn_fwd.argtypes = [ctypes.POINTER(DiffAttnDesc)] + [_vp] * 12
+    L.pam_diff_attn_bwd.restype = ctypes.c_int
+    L.pam_diff_attn_bwd.argtypes = [ctypes.POINTER(DiffAttnDesc)] + [_vp] * 10 + [ctypes.POINTER(_i64)] + [_vp] * 6
+    L.pam_rotary_frequencies.restype = ctypes.c_int
+    L.pam_rotary_frequencies.argtypes = [_i32, ctypes.c_double, _i32] + [ctypes.c_double] * 4 + [_vp, _vp]
+    L.pam_rotary_table.restype = ctypes.c_int
+    L.pam_rotary_table.argtypes = [_vp, _vp, _vp, _i64, _i32, _i32, ctypes.c_double, _vp, _vp]
+    L.pam_rotary.restype = ctypes.c_int
+    L.pam_rotary.argtypes = [ctypes.POINTER(RotaryDesc)] + [_vp] * 7
+    L.pam_dropout.restype = ctypes.c_int
+    L.pam_dropout.argtypes = [_vp, _i64, _i32, ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, _vp, _vp]
+    L.pam_norm_gate_fwd.restype = ctypes.c_int
+    L.pam_norm_gate_fwd.argtypes = [ctypes.POINTER(NormDesc)] + [_vp] * 11
+    L.pam_norm_gate_bwd_workspace.restype = ctypes.c_size_t
+    L.pam_norm_gate_bwd_workspace.argtypes = [ctypes.POINTER(NormDesc)]
+    L.pam_norm_gate_bwd.restype = ctypes.c_int
+    L.pam_norm_gate_bwd.argtypes = [ctypes.POINTER(NormDesc)] + [_vp] * 19
     L.pam_lattice_destroy.restype = None
     L.pam_lattice_destroy.argtypes = [_vp]
     L.pam_status_string.restype = ctypes.c_char_p
@@ -386,3 +444,284 @@ def pam_probe_copy_rows(src: torch.Tensor, dst: torch.Tensor, perm: torch.Tensor
 
 def pam_lattice_destroy(lat: Lattice):
     lat.destroy()
+
+
+# ---------------------------------------------------------------------------
+# the operators around an attention layer (include/pam_attn.h)
+# ---------------------------------------------------------------------------
+
+def _dtype_of(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16")
+    return _DTYPES[t.dtype]
+
+
+def _rows_ptr(t: torch.Tensor, like: torch.Tensor, name: str) -> int:
+    """Pointer of a strided tensor whose last axis is contiguous, of ``like``'s type and device."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} must be {like.dtype} on {like.device}")
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+    return t.data_ptr()
+
+
+def _shaped_ptr(t: torch.Tensor | None, shape, dtype, like: torch.Tensor, name: str) -> int | None:
+    """Pointer of a contiguous tensor of the given shape and type on ``like``'s device (None: NULL)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != like.device:
+        raise ValueError(f"{name} must be on {like.device}")
+    return _dev_ptr(t, dtype, name)
+
+
+class _on_stream:
+    """New tensors belong to the stream that writes them: with a stream given,
+    memory freed after the call is not handed out while the stream uses it."""
+
+    def __init__(self, stream, like: torch.Tensor):
+        if like.is_cuda and like.device.index != torch.cuda.current_device():
+            raise ValueError("the tensors must be on the current device")
+        self.ctx = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask):
+    """Descriptor of a call and the pointers that both directions take."""
+    if q.dim() != 5 or q.shape[3] != 2 or k.dim() != 5 or k.shape[3] != 2 or v.dim() != 4:
+        raise ValueError("q must be B x Lq x H x 2 x d, k B x Lk x Hk x 2 x d, v B x Lk x Hk x dv")
+    B, lq, H, _, d = q.shape
+    lk, hk, dv = k.shape[1], k.shape[2], v.shape[3]
+    if k.shape[0] != B or k.shape[4] != d or tuple(v.shape[:3]) != (B, lk, hk):
+        raise ValueError("q, k and v do not agree in sequences, lengths, key heads or head size")
+    dtype = _dtype_of(q, "q")
+    ptrs = [_rows_ptr(q, q, "q"), _rows_ptr(k, q, "k"), _rows_ptr(v, q, "v"),
+            _shaped_ptr(lam, (H,), q.dtype, q, "lam"), _shaped_ptr(q_len, (B,), torch.int32, q, "q_len"),
+            _shaped_ptr(k_len, (B,), torch.int32, q, "k_len"), None]
+    if key_mask is not None:
+        if key_mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError("key_mask must be bool or uint8")
+        ptrs[6] = _shaped_ptr(key_mask, (B, lk), key_mask.dtype, q, "key_mask")
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    desc = DiffAttnDesc(dtype, B, H, hk, d, dv, lq, lk, PAM_ATTN_CAUSAL if causal else 0,
+                        d ** -0.5 if scale is None else scale, qs[:4], ks[:4], vs[:3])
+    return desc, ptrs
+
+
+def pam_diff_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor, *,
+                      scale: float | None = None, causal: bool = False, q_len: torch.Tensor | None = None,
+                      k_len: torch.Tensor | None = None, key_mask: torch.Tensor | None = None, save: bool = False,
+                      stream=None):
+    """Differential attention, out = (P1 - lam P2) v per head.
+
+    ``q`` is B x Lq x H x 2 x d, ``k`` B x Lk x Hk x 2 x d, ``v`` B x Lk x Hk x dv (any strides, last axis
+    contiguous), ``lam`` H values of q's type; ``scale`` 1 / sqrt(d) if not given; ``q_len``, ``k_len`` B int32
+    and ``key_mask`` B x Lk (bool or uint8) on the device.  Returns ``out`` (B x Lq x H x dv); with ``save``
+    (out, saved), saved being what pam_diff_attn_bwd takes."""
+    desc, ptrs = _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask)
+    L = lib()
+    B, lq, H, dv = desc.batch, desc.len_q, desc.heads, desc.dim_v
+    ws_bytes = L.pam_diff_attn_fwd_workspace(ctypes.byref(desc))
+    if ws_bytes == ctypes.c_size_t(-1).value:
+        raise PamError(PAM_ERR_INVALID_ARGUMENT, "pam_diff_attn_fwd", last_error())
+    with _on_stream(stream, q):
+        out = torch.empty((B, lq, H, dv), dtype=q.dtype, device=q.device)
+        so = lse = ws = None
+        if save:
+            so = torch.empty((2, B, lq, H, dv), dtype=q.dtype, device=q.device)
+            lse = torch.empty((2, B, H, lq), dtype=torch.float32, device=q.device)
+        if ws_bytes:
+            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+    _check(L.pam_diff_attn_fwd(ctypes.byref(desc), *ptrs, out.data_ptr(), so.data_ptr() if save else None,
+                               lse.data_ptr() if save else None, ws.data_ptr() if ws_bytes else None,
+                               _stream_ptr(stream)), "pam_diff_attn_fwd")
+    return (out, (so, lse)) if save else out
+
+
+def pam_diff_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor, saved,
+                      grad_out: torch.Tensor, *, scale: float | None = None, causal: bool = False,
+                      q_len: torch.Tensor | None = None, k_len: torch.Tensor | None = None,
+                      key_mask: torch.Tensor | None = None, stream=None):
+    """Gradients (q, k, v, lam) of pam_diff_attn_fwd with the same arguments,
+    from its ``saved`` and ``grad_out`` (B x Lq x H x dv, any strides)."""
+    desc, ptrs = _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask)
+    L = lib()
+    B, lq, H, dv = desc.batch, desc.len_q, desc.heads, desc.dim_v
+    so, lse = saved
+    pso = _shaped_ptr(so, (2, B, lq, H, dv), q.dtype, q, "saved o")
+    plse = _shaped_ptr(lse, (2, B, H, lq), torch.float32, q, "saved lse")
+    if tuple(grad_out.shape) != (B, lq, H, dv):
+        raise ValueError(f"grad_out has shape {tuple(grad_out.shape)}, expected {(B, lq, H, dv)}")
+    pdo = _rows_ptr(grad_out, q, "grad_out")
+    ws_bytes = L.pam_diff_attn_bwd_workspace(ctypes.byref(desc))
+    if ws_bytes == ctypes.c_size_t(-1).value:
+        raise PamError(PAM_ERR_INVALID_ARGUMENT, "pam_diff_attn_bwd", last_error())
+    with _on_stream(stream, q):
+        gq, gk, gv, gl = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v, lam))
+        ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=q.device)
+    _check(L.pam_diff_attn_bwd(ctypes.byref(desc), *ptrs, pso, plse, pdo, (_i64 * 3)(*grad_out.stride()[:3]),
+                               gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), gl.data_ptr(), ws.data_ptr(),
+                               _stream_ptr(stream)), "pam_diff_attn_bwd")
+    return gq, gk, gv, gl
+
+
+def pam_rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                           original_len: float = 0.0, beta_slow: float = 1.0, beta_fast: float = 32.0):
+    """Angles per unit of position of the rot / 2 pairs (CPU float64) and the factor of cosines and sines;
+    ``scaling`` "plain", "linear", "ntk" or "yarn" for contexts longer than the trained one."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+    freq = torch.empty(max(rot // 2, 1), dtype=torch.float64)
+    mag = ctypes.c_double(0.0)
+    _check(lib().pam_rotary_frequencies(rot, base, ROPE_SCALINGS[scaling], factor, original_len, beta_slow, beta_fast,
+                                        freq.data_ptr(), ctypes.byref(mag)), "pam_rotary_frequencies")
+    return freq, mag.value
+
+
+def pam_rotary_table(freq: torch.Tensor, entries: int | None = None, coord: torch.Tensor | None = None,
+                     axis: torch.Tensor | None = None, magnitude: float = 1.0, stream=None) -> torch.Tensor:
+    """Table (entries x pairs x 2 fp32) of the cosines and sines of freq[i] times the entry's number, or times
+    coord[t, axis[i]] (``coord`` entries x axes fp32, ``axis`` pairs int32)."""
+    if freq.dim() != 1:
+        raise ValueError("freq must have one axis")
+    pairs, axes = freq.shape[0], 1
+    if coord is not None:
+        if coord.dim() != 2:
+            raise ValueError("coord must be entries x axes")
+        if entries is not None and entries != coord.shape[0]:
+            raise ValueError("entries is not the number of coordinates")
+        entries, axes = coord.shape
+    elif entries is None:
+        raise ValueError("give entries or coord")
+    pf = _dev_ptr(freq, torch.float64, "freq")
+    pc = _shaped_ptr(coord, (entries, axes), torch.float32, freq, "coord")
+    pa = _shaped_ptr(axis, (pairs,), torch.int32, freq, "axis")
+    with _on_stream(stream, freq):
+        table = torch.empty((max(entries, 0), pairs, 2), dtype=torch.float32, device=freq.device)
+    _check(lib().pam_rotary_table(pf, pc, pa, entries, pairs, axes, magnitude, table.data_ptr(),
+                                  _stream_ptr(stream)), "pam_rotary_table")
+    return table
+
+
+def pam_rotary(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, *, pos: torch.Tensor | None = None,
+               start: int = 0, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
+    """Rotates the first 2 pairs channels of the heads of ``q`` (B x L x H x d) and ``k`` (B x L x Hk x d, or
+    None) by ``table`` (entries x pairs x 2); token l takes entry pos[b, l] (B x L int32) or start + l.
+    ``inverse`` rotates back (gradients).  ``out`` = (q_out, k_out), contiguous; contiguous inputs may be their
+    own outputs.  Returns (q', k')."""
+    if q.dim() != 4 or (k is not None and (k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3])):
+        raise ValueError("q must be B x L x H x d and k B x L x Hk x d")
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("table must be entries x pairs x 2")
+    B, n, H, d = q.shape
+    hk = 0 if k is None else k.shape[2]
+    flags = (PAM_ROTARY_INTERLEAVED if interleaved else 0) | (PAM_ROTARY_INVERSE if inverse else 0)
+    desc = RotaryDesc(_dtype_of(q, "q"), B, n, H, hk, d, table.shape[1], flags, start, table.shape[0],
+                      q.stride()[:3], (0, 0, 0) if k is None else k.stride()[:3])
+    pq, pk = _rows_ptr(q, q, "q"), None if k is None else _rows_ptr(k, q, "k")
+    pt = _shaped_ptr(table, table.shape, torch.float32, q, "table")
+    pp = _shaped_ptr(pos, (B, n), torch.int32, q, "pos")
+    with _on_stream(stream, q):
+        if out is None:
+            out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
+                   None if k is None else torch.empty(k.shape, dtype=q.dtype, device=q.device))
+    qo, ko = out
+    pqo = _shaped_ptr(qo, q.shape, q.dtype, q, "q_out")
+    pko = None if k is None else _shaped_ptr(ko, k.shape, q.dtype, q, "k_out")
+    _check(lib().pam_rotary(ctypes.byref(desc), pq, pk, pt, pp, pqo, pko, _stream_ptr(stream)), "pam_rotary")
+    return qo, ko
+
+
+def pam_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, out: torch.Tensor | None = None,
+                stream=None) -> torch.Tensor:
+    """x times 1 / (1 - p) where the numbers that Philox4x32-10 makes of (seed, offset, element) keep it, else 0.
+    The gradient is the same call on the upstream gradient.  ``out`` may be ``x``."""
+    dtype = _dtype_of(x, "x")
+    px = _dev_ptr(x, x.dtype, "x")
+    with _on_stream(stream, x):
+        if out is None:
+            out = torch.empty_like(x)
+    po = _shaped_ptr(out, x.shape, x.dtype, x, "out")
+    _check(lib().pam_dropout(px, x.numel(), dtype, p, seed, offset, po, _stream_ptr(stream)), "pam_dropout")
+    return out
+
+
+def _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, seed, offset):
+    if x.dim() != 2 or (z is not None and z.shape != x.shape):
+        raise ValueError("x and z must be rows x channels")
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {sorted(NORMS)}")
+    n, c = x.shape
+    gate_rows = 0
+    if gate is not None:
+        if gate.dim() != 2 or gate.shape[1] != c or (gate.shape[0] == 0) != (n == 0) or \
+                (gate.shape[0] and n % gate.shape[0]):
+            raise ValueError("gate must be rows x channels, its rows dividing x's")
+        gate_rows = n // gate.shape[0] if gate.shape[0] else 1
+    desc = NormDesc(_dtype_of(x, "x"), NORMS[norm], n, c, eps, gate_rows, x.stride(0),
+                    x.stride(0) if z is None else z.stride(0), p, seed, offset)
+    f32 = torch.float32
+    ptrs = {"x": _rows_ptr(x, x, "x"), "z": None if z is None else _rows_ptr(z, x, "z"),
+            "w_post": _shaped_ptr(w_post, (c,), f32, x, "w_post"),
+            "b_post": _shaped_ptr(b_post, (c,), f32, x, "b_post"),
+            "gate": None if gate is None else _shaped_ptr(gate, gate.shape, x.dtype, x, "gate"),
+            "scale": _shaped_ptr(scale, (c,), f32, x, "scale"), "w_pre": _shaped_ptr(w_pre, (c,), f32, x, "w_pre"),
+            "b_pre": _shaped_ptr(b_pre, (c,), f32, x, "b_pre")}
+    return desc, ptrs
+
+
+def pam_norm_gate_fwd(x: torch.Tensor, *, z: torch.Tensor | None = None, w_post: torch.Tensor | None = None,
+                      b_post: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                      scale: torch.Tensor | None = None, w_pre: torch.Tensor | None = None,
+                      b_pre: torch.Tensor | None = None, norm: str = "rms", eps: float = 1e-6, p: float = 0.0,
+                      seed: int = 0, offset: int = 0, next_norm: bool = True, stream=None):
+    """r = x + drop(scale gate (N(z) w_post + b_post)) and h = N(r) w_pre + b_pre, in one pass over the rows.
+
+    ``x``, ``z`` rows x channels (``z`` None: r is x), ``gate`` G x channels (each row for rows / G consecutive
+    rows), vectors fp32.  Returns (r, h); r is None without z, h without ``next_norm``."""
+    desc, ptr = _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, seed, offset)
+    with _on_stream(stream, x):
+        r = None if z is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if next_norm else None
+    _check(lib().pam_norm_gate_fwd(ctypes.byref(desc), *ptr.values(), None if r is None else r.data_ptr(),
+                                   None if h is None else h.data_ptr(), _stream_ptr(stream)), "pam_norm_gate_fwd")
+    return r, h
+
+
+def pam_norm_gate_bwd(x: torch.Tensor, *, grad_r: torch.Tensor | None, grad_h: torch.Tensor | None,
+                      z: torch.Tensor | None = None, w_post: torch.Tensor | None = None,
+                      b_post: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                      scale: torch.Tensor | None = None, w_pre: torch.Tensor | None = None,
+                      b_pre: torch.Tensor | None = None, norm: str = "rms", eps: float = 1e-6, p: float = 0.0,
+                      seed: int = 0, offset: int = 0, stream=None) -> dict:
+    """Gradients of pam_norm_gate_fwd with the same arguments, by the arguments' names (None for those not
+    given), from ``grad_r`` (None: 0) and ``grad_h`` (None: the forward call had no next norm)."""
+    desc, ptr = _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, seed, offset)
+    L = lib()
+    pr = _shaped_ptr(grad_r, x.shape, x.dtype, x, "grad_r")
+    ph = _shaped_ptr(grad_h, x.shape, x.dtype, x, "grad_h")
+    ws_bytes = L.pam_norm_gate_bwd_workspace(ctypes.byref(desc))
+    if ws_bytes == ctypes.c_size_t(-1).value:
+        raise PamError(PAM_ERR_INVALID_ARGUMENT, "pam_norm_gate_bwd", last_error())
+    given = {"x": x, "z": z, "w_post": w_post, "b_post": b_post, "gate": gate, "scale": scale, "w_pre": w_pre,
+             "b_pre": b_pre}
+    with _on_stream(stream, x):
+        grads = {name: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+                 for name, t in given.items()}
+        ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=x.device)
+    out = {name: None if t is None else t.data_ptr() for name, t in grads.items()}
+    _check(L.pam_norm_gate_bwd(ctypes.byref(desc), *(ptr[a] for a in ("x", "z", "w_post", "b_post", "gate", "scale",
+                                                                      "w_pre")), pr, ph,
+                               *(out[a] for a in ("x", "z", "w_post", "b_post", "gate", "scale", "w_pre", "b_pre")),
+                               ws.data_ptr(), _stream_ptr(stream)), "pam_norm_gate_bwd")
+    return grads

@@ -514,6 +514,33 @@ pam_status_t build_pass(pam_lattice_s *h, bool allow_fixed)
 
 }  // namespace
 
+namespace pam {
+
+// the text is lost, and the status kept, if there is no memory for it
+pam_status_t abi_fail(pam_status_t s, const char *msg) noexcept
+{
+    try {
+        return fail(s, msg);
+    } catch (...) {
+        return s;
+    }
+}
+pam_status_t abi_hip_fail(hipError_t e, const char *what) noexcept
+{
+    try {
+        return hip_fail(e, what);
+    } catch (...) {
+        return e == hipErrorOutOfMemory ? PAM_ERR_OUT_OF_MEMORY : PAM_ERR_DEVICE;
+    }
+}
+pam_status_t abi_sticky_error() noexcept
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PAM_OK : abi_hip_fail(e, "earlier asynchronous work");
+}
+
+}  // namespace pam
+
 extern "C" {
 
 const char *pam_status_string(pam_status_t s)

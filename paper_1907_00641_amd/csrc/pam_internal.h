@@ -9,6 +9,7 @@
 #include <string>
 #include <vector>
 
+#include "../../include/pam_attn.h"
 #include "../../include/pam_lattice.h"
 #include "../../include/pam_probe.h"
 
@@ -244,5 +245,40 @@ hipError_t launch_block_bwd(const pam_block_desc_t &ds, const float *x, const fl
 constexpr size_t kBlockScratchFloats = (size_t)1 << 20;
 // its address on the current device (taken once per device)
 hipError_t block_scratch(float **out);
+
+// ---- the operators around an attention layer (pam_attn.h)
+// Status and text of a failure, for ABI calls outside pam_abi.cpp.
+pam_status_t abi_fail(pam_status_t s, const char *msg) noexcept;
+pam_status_t abi_hip_fail(hipError_t e, const char *what) noexcept;
+// an error of earlier asynchronous work, PAM_OK if there is none
+pam_status_t abi_sticky_error() noexcept;
+
+// differential attention (pam_attn.hip); device workspaces in bytes
+size_t attn_fwd_workspace(const pam_diff_attn_desc_t &d);
+size_t attn_bwd_workspace(const pam_diff_attn_desc_t &d);
+hipError_t launch_attn_fwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
+                           const void *lam, const int32_t *q_len, const int32_t *k_len, const uint8_t *key_mask,
+                           void *out, void *so, float *lse, void *workspace, hipStream_t s);
+hipError_t launch_attn_bwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
+                           const void *lam, const int32_t *q_len, const int32_t *k_len, const uint8_t *key_mask,
+                           const void *so, const float *lse, const void *dout, const int64_t *dos, void *gq, void *gk,
+                           void *gv, void *glam, void *workspace, hipStream_t s);
+// rotary positions (pam_rotary.hip)
+hipError_t launch_rotary_table(const double *freq, const float *coord, const int32_t *axis, int64_t entries,
+                               int32_t pairs, int32_t axes, double magnitude, float *table, hipStream_t s);
+hipError_t launch_rotary(const pam_rotary_desc_t &d, const void *q, const void *k, const float *table,
+                         const int32_t *pos, void *q_out, void *k_out, hipStream_t s);
+// norms, gate, residual scale, dropout (pam_norm.hip)
+hipError_t launch_dropout(const void *x, int64_t n, int32_t dtype, double p, uint64_t seed, uint64_t offset, void *y,
+                          hipStream_t s);
+hipError_t launch_norm_fwd(const pam_norm_desc_t &d, const void *x, const void *z, const float *w_post,
+                           const float *b_post, const void *gate, const float *scale, const float *w_pre,
+                           const float *b_pre, void *r, void *h, hipStream_t s);
+size_t norm_bwd_workspace(const pam_norm_desc_t &d);
+hipError_t launch_norm_bwd(const pam_norm_desc_t &d, const void *x, const void *z, const float *w_post,
+                           const float *b_post, const void *gate, const float *scale, const float *w_pre,
+                           const void *grad_r, const void *grad_h, void *grad_x, void *grad_z, float *gw_post,
+                           float *gb_post, void *grad_gate, float *gscale, float *gw_pre, float *gb_pre,
+                           void *workspace, hipStream_t s);
 
 }  // namespace pam
