@@ -63,8 +63,9 @@ typedef enum { PAM_F32 = 0, PAM_F16 = 1, PAM_BF16 = 2 } pam_dtype_t;
  *         of len_q, len_k.
  *   key_mask : batch x len_k bytes on the device, NULL: every key is seen.
  * Limits: 1 <= dim <= PAM_ATTN_MAX_DIM, 1 <= dim_v <= 2 PAM_ATTN_MAX_DIM,
- * kv_heads divides heads; batch, len_q and len_k may be 0;
- * batch heads len_q < 2^31; scale positive.
+ * kv_heads divides heads; batch, len_q and len_k may be 0 and are less than
+ * 2^30; batch heads len_q and batch kv_heads len_k less than 2^31; scale
+ * positive.
  */
 typedef struct {
     int32_t dtype; /* pam_dtype_t */

@@ -14,7 +14,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpam_lattice.so")
 SOURCES = ["pam_build.hip", "pam_filter.hip", "pam_block.hip", "pam_probe.hip", "pam_abi.cpp",
-           "pam_attn.hip", "pam_rotary.hip", "pam_norm.hip", "pam_attn_abi.cpp"]
+           "pam_attn_f32.hip", "pam_attn_f16.hip", "pam_attn_bf16.hip", "pam_attn.cpp",
+           "pam_rotary.hip", "pam_norm.hip", "pam_attn_abi.cpp"]
 ARCH = "gfx950"
 
 

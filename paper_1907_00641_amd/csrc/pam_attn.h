@@ -23,7 +23,17 @@ struct AttnArgs {
     void *gq, *gk, *gv, *glam;
     float *dsum;      // D^m, laid out as lse
     float *dlam;      // per row sum_j p^1 dp: batch x heads x len_q
+    float *parts;     // grad_k and, parts_v floats on, grad_v per head, or null: no heads to add up
+    int64_t parts_v;
 };
+
+// per element type (pam_attn_f32.hip, pam_attn_f16.hip, pam_attn_bf16.hip)
+hipError_t attn_fwd_f32(const AttnArgs &a, bool wide, hipStream_t s);
+hipError_t attn_fwd_f16(const AttnArgs &a, bool wide, hipStream_t s);
+hipError_t attn_fwd_bf16(const AttnArgs &a, bool wide, hipStream_t s);
+hipError_t attn_bwd_f32(const AttnArgs &a, bool wide, hipStream_t s);
+hipError_t attn_bwd_f16(const AttnArgs &a, bool wide, hipStream_t s);
+hipError_t attn_bwd_bf16(const AttnArgs &a, bool wide, hipStream_t s);
 
 // lengths of sequence b, clamped to the arrays
 __device__ __forceinline__ int q_len_of(const AttnArgs &a, int b)

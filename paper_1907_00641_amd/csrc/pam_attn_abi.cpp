@@ -68,8 +68,8 @@ pam_status_t check_attn(const pam_diff_attn_desc_t *d)
     const int64_t most = ((int64_t)1 << 31) - 1;
     REQUIRE((__int128)d->batch * d->heads * d->len_q <= most, "batch heads len_q must be less than 2^31");
     REQUIRE((__int128)d->batch * d->kv_heads * d->len_k <= most, "batch kv_heads len_k must be less than 2^31");
-    // (token, dim) offsets of a sequence are formed in 64 bits, lengths in 32 with room for a tile
-    REQUIRE(d->len_q <= most - 4096 && d->len_k <= most - 4096, "len_q and len_k must be less than 2^31 - 4096");
+    // sums of two lengths and a tile are formed in 32 bits
+    REQUIRE(d->len_q < 1 << 30 && d->len_k < 1 << 30, "len_q and len_k must be less than 2^30");
     return PAM_OK;
 }
 
