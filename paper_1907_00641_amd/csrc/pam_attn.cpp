@@ -75,8 +75,8 @@ bool split_heads(const pam_diff_attn_desc_t &d)
 }
 
 int64_t rows_of(const pam_diff_attn_desc_t &d) { return (int64_t)d.batch * d.heads * d.len_q; }
-// D of both maps and the rows of grad_lambda, whole groups of four floats
-int64_t row_floats(const pam_diff_attn_desc_t &d) { return (3 * rows_of(d) + 3) / 4 * 4; }
+// the rows' statistics and their parts of grad_lambda, whole groups of four floats
+int64_t row_floats(const pam_diff_attn_desc_t &d) { return (5 * rows_of(d) + 3) / 4 * 4; }
 
 }  // namespace
 
@@ -121,10 +121,10 @@ hipError_t launch_attn_bwd(const pam_diff_attn_desc_t &d, const void *q, const v
     a.gk = gk;
     a.gv = gv;
     a.glam = glam;
-    a.dsum = (float *)workspace;
-    a.dlam = a.dsum + 2 * a.lse_map;
+    a.stats = (float *)workspace;
+    a.dlam = a.stats + 4 * a.lse_map;
     if (split_heads(d)) {
-        a.parts = a.dsum + row_floats(d);
+        a.parts = a.stats + row_floats(d);
         a.parts_v = (int64_t)d.batch * d.len_k * d.heads * 2 * d.dim;
     }
     Wide w = wide_of(d, q, k, v);

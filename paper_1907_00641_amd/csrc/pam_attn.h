@@ -21,7 +21,7 @@ struct AttnArgs {
     const void *dout;
     int64_t dos[3];
     void *gq, *gk, *gv, *glam;
-    float *dsum;      // D^m, laid out as lse
+    float *stats;     // lse^0 and lse^1 (base 2; infinity where a row sees nothing), D^0, D^1, each laid out as lse
     float *dlam;      // per row sum_j p^1 dp: batch x heads x len_q
     float *parts;     // grad_k and, parts_v floats on, grad_v per head, or null: no heads to add up
     int64_t parts_v;

@@ -39,8 +39,12 @@ struct Sizes {
     // for the scores
     static constexpr bool kSmall = (sizeof(T) == 2 && DP <= 64) || (sizeof(T) == 4 && DP <= 32);
     static constexpr int kWavesPerSimd = kSmall ? 2 : 1;
-    static constexpr int kKeyTile = kKeys * (RK::kBytes + RV::kBytes);
-    static constexpr int kQueryTile = kQueries * (RK::kBytes + RV::kBytes) + 4 * kQueries * 4;
+    // LDS: a tile of keys and values; of queries and dout with 4 statistics
+    // each; the block's values of the keys' pass
+    static constexpr int kKeyTile = RK::size(kKeys) + RV::size(kKeys);
+    static constexpr int kQueryTile = RK::size(kQueries) + RV::size(kQueries) + 4 * kQueries * 4;
+    static constexpr bool kKeepValues = 2 * kQueryTile + RV::size(kBlockRows) <= (160 << 10);
+    static constexpr int kValues = kKeepValues ? RV::size(kBlockRows) : 0;
 };
 
 // fp16 has 2^-14 as its smallest full-precision value.  Probabilities are at
@@ -84,11 +88,31 @@ struct Range {
 // Work item n of `total` for the block that the dispatcher hands out as number
 // n: consecutive items, which share keys and values, go to one of the eight
 // dies (blocks go round them), so that its L2 serves them.
-__device__ __forceinline__ int64_t die_order(int64_t n, int64_t total)
+__device__ __forceinline__ uint32_t die_order(uint32_t n, uint32_t total)
 {
-    const int64_t per = total / 8, rest = total - per * 8, die = n % 8;
+    const uint32_t per = total / 8, rest = total - per * 8, die = n % 8;
     return die * per + min(die, rest) + n / 8;
 }
+
+// A value that is the same in every lane, in a scalar register: divisions are
+// vector code, and what is computed from their results would stay there.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uniform_float(float x)
+{
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+
+// Item n: its tile of 128 rows, sequence and head.
+struct Item {
+    int tile, b, h;
+    __device__ __forceinline__ Item(uint32_t n, uint32_t total, uint32_t tiles, uint32_t heads)
+    {
+        const uint32_t x = die_order(n, total), bh = x / tiles;
+        tile = uniform(x - bh * tiles);
+        b = uniform(bh / heads);
+        h = uniform(bh - bh / heads * heads);
+    }
+};
 
 // Bits of the tile's keys that are part of the sequence and not hidden.
 __device__ __forceinline__ bool key_seen(const AttnArgs &a, int b, int nk, int j)
@@ -130,18 +154,17 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
     constexpr int KT = S::kKeys;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int l = lane_id(), w = wave_id();
-    const int tiles = (a.len_q + kBlockRows - 1) / kBlockRows;
-    const int64_t total = (int64_t)tiles * a.heads * a.batch;
+    const uint32_t tiles = (a.len_q + kBlockRows - 1) / kBlockRows, total = tiles * a.heads * a.batch;
     const float c = a.scale * kLog2e;
     if (a.dim < DP || a.dim_v < DVP) {  // the channels that no load writes
         for (int e = threadIdx.x; e < 2 * S::kKeyTile / 16; e += kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
-    for (int64_t n = blockIdx.x; n < total; n += gridDim.x) {
-        const int64_t item = die_order(n, total);
-        const int bh = (int)(item / tiles), q0 = (tiles - 1 - (int)(item % tiles)) * kBlockRows;
-        const int b = bh / a.heads, h = bh - b * a.heads, hk = h / a.group;
+    for (uint32_t n = blockIdx.x; n < total; n += gridDim.x) {
+        const Item item(n, total, tiles, a.heads);
+        const int q0 = ((int)tiles - 1 - item.tile) * kBlockRows;  // causal: the longest first
+        const int b = item.b, h = item.h, hk = uniform(h / a.group);
         const int nq = q_len_of(a, b), nk = k_len_of(a, b);
         const int i = q0 + 32 * w + (l & 31);  // this lane's query
         const bool in = i < nq;
@@ -152,7 +175,8 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         const int end = q0 < nq ? (a.causal ? min(nk, last + nk - nq + 1) : nk) : 0;
         const int wend = q0 + 32 * w < nq ? (a.causal ? min(nk, wlast + nk - nq + 1) : nk) : 0;
         const int wall = q0 + 32 * w + 31 < nq ? (a.causal ? min(nk, q0 + 32 * w + nk - nq + 1) : nk) : 0;
-        const T *kp = (const T *)a.k + b * a.ks[0] + hk * a.ks[2], *vp = (const T *)a.v + b * a.vs[0] + hk * a.vs[2];
+        const T *kp = uniform_ptr((const T *)a.k + b * a.ks[0] + hk * a.ks[2]);
+        const T *vp = uniform_ptr((const T *)a.v + b * a.vs[0] + hk * a.vs[2]);
 
         uint4v q[2][S::CK];
         {
@@ -166,11 +190,12 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         f32x16 o[2][S::TV] = {};
         float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
 
-        auto issue = [&](int k0, int buf) {
+        auto issue = [&](int k0, int buf) {  // tiles in order
             char *at = lds + buf * S::kKeyTile;
-            load_rows<T, 2 * DP, 2, KT, kAttnWaves, WIDE>(at, kp + k0 * a.ks[1], a.ks[1], a.ks[3], nk - 1 - k0, a.dim);
-            load_rows<T, DVP, 1, KT, kAttnWaves, WIDE>(at + KT * RK::kBytes, vp + k0 * a.vs[1], a.vs[1], 0,
-                                                       nk - 1 - k0, a.dim_v);
+            load_rows<T, 2 * DP, 2, KT, kAttnWaves, WIDE>(at, kp, a.ks[1], a.ks[3], nk - 1 - k0, a.dim);
+            load_rows<T, DVP, 1, KT, kAttnWaves, WIDE>(at + RK::size(KT), vp, a.vs[1], 0, nk - 1 - k0, a.dim_v);
+            kp = uniform_ptr(kp + KT * a.ks[1]);
+            vp = uniform_ptr(vp + KT * a.vs[1]);
         };
         const int trips = (end + KT - 1) / KT;
         // the mask's byte of this lane's key of the next tile, compared only when
@@ -184,7 +209,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         }
         for (int t = 0; t < trips; ++t) {
             const int k0 = t * KT, buf = t & 1;
-            char *kb = lds + buf * S::kKeyTile, *vb = kb + KT * RK::kBytes;
+            char *kb = lds + buf * S::kKeyTile, *vb = kb + RK::size(KT);
             wait_loads();
             __syncthreads();  // tile t is there for every wave, and tile t - 1 done with
             const uint64_t seen = __ballot(next != 0 && l < KT && k0 + l < nk);
@@ -198,6 +223,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 clear_rows<T, DVP, KT, kAttnWaves>(vb, seen);
                 __syncthreads();
             }
+            const uint32_t kr = lds_address(kb) + RK::row_lane(), vc = lds_address(vb) + RV::col_lane();
 #pragma unroll
             for (int kt = 0; kt < KT / 32; ++kt) {
                 const int j0 = k0 + 32 * kt;
@@ -208,7 +234,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int x = 0; x < S::CK; ++x)
-                        mma<T>(s[m], RK::row_chunk(kb, 32 * kt, m * S::CK + x), q[m][x]);
+                        mma<T>(s[m], RK::row_chunk(kr, 32 * kt, m * S::CK + x), q[m][x]);
                 if (some_hidden || j0 + 32 > wall) {
                     hide(s[0], j0, limit, (uint32_t)(seen >> (32 * kt)));
                     hide(s[1], j0, limit, (uint32_t)(seen >> (32 * kt)));
@@ -244,7 +270,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 for (int x = 0; x < S::CP; ++x)
 #pragma unroll
                     for (int v = 0; v < S::TV; ++v) {
-                        const uint4v vf = RV::col_chunk(vb, 32 * kt, x, 32 * v);
+                        const uint4v vf = RV::col_chunk(vc, 32 * kt, x, 32 * v);
                         mma<T>(o[0][v], vf, p[0][x]);
                         mma<T>(o[1][v], vf, p[1][x]);
                     }
@@ -281,7 +307,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 }
             }
         if (a.lse && l < 32) {
-            const int64_t at = (int64_t)bh * a.len_q + i;
+            const int64_t at = ((int64_t)b * a.heads + h) * a.len_q + i;
 #pragma unroll
             for (int m = 0; m < 2; ++m)
                 a.lse[m * a.lse_map + at] =
@@ -306,18 +332,17 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
     constexpr int KT = S::kKeys;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int l = lane_id(), w = wave_id();
-    const int tiles = (a.len_q + kBlockRows - 1) / kBlockRows;
-    const int64_t total = (int64_t)tiles * a.heads * a.batch;
+    const uint32_t tiles = (a.len_q + kBlockRows - 1) / kBlockRows, total = tiles * a.heads * a.batch;
     const float c = a.scale * kLog2e;
     if (a.dim < DP || a.dim_v < DVP) {
         for (int e = threadIdx.x; e < 2 * S::kKeyTile / 16; e += kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
-    for (int64_t n = blockIdx.x; n < total; n += gridDim.x) {
-        const int64_t item = die_order(n, total);
-        const int bh = (int)(item / tiles), q0 = (tiles - 1 - (int)(item % tiles)) * kBlockRows;
-        const int b = bh / a.heads, h = bh - b * a.heads, hk = h / a.group;
+    for (uint32_t n = blockIdx.x; n < total; n += gridDim.x) {
+        const Item item(n, total, tiles, a.heads);
+        const int q0 = ((int)tiles - 1 - item.tile) * kBlockRows;  // causal: the longest first
+        const int b = item.b, h = item.h, hk = uniform(h / a.group);
         const int nq = q_len_of(a, b), nk = k_len_of(a, b);
         const int i = q0 + 32 * w + (l & 31);
         const bool in = i < nq;
@@ -326,14 +351,17 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         const int end = q0 < nq ? (a.causal ? min(nk, last + nk - nq + 1) : nk) : 0;
         const int wend = q0 + 32 * w < nq ? (a.causal ? min(nk, wlast + nk - nq + 1) : nk) : 0;
         const int wall = q0 + 32 * w + 31 < nq ? (a.causal ? min(nk, q0 + 32 * w + nk - nq + 1) : nk) : 0;
-        const T *kp = (const T *)a.k + b * a.ks[0] + hk * a.ks[2], *vp = (const T *)a.v + b * a.vs[0] + hk * a.vs[2];
-        const int64_t row = ((int64_t)b * a.len_q + i) * a.heads + h, at = (int64_t)bh * a.len_q + i;
+        const T *kp = uniform_ptr((const T *)a.k + b * a.ks[0] + hk * a.ks[2]);
+        const T *vp = uniform_ptr((const T *)a.v + b * a.vs[0] + hk * a.vs[2]);
+        const int64_t row = ((int64_t)b * a.len_q + i) * a.heads + h,
+                      at = ((int64_t)b * a.heads + h) * a.len_q + i;
 
-        auto issue = [&](int k0, int buf) {
+        auto issue = [&](int k0, int buf) {  // tiles in order
             char *to = lds + buf * S::kKeyTile;
-            load_rows<T, 2 * DP, 2, KT, kAttnWaves, WIDE>(to, kp + k0 * a.ks[1], a.ks[1], a.ks[3], nk - 1 - k0, a.dim);
-            load_rows<T, DVP, 1, KT, kAttnWaves, WIDE>(to + KT * RK::kBytes, vp + k0 * a.vs[1], a.vs[1], 0,
-                                                       nk - 1 - k0, a.dim_v);
+            load_rows<T, 2 * DP, 2, KT, kAttnWaves, WIDE>(to, kp, a.ks[1], a.ks[3], nk - 1 - k0, a.dim);
+            load_rows<T, DVP, 1, KT, kAttnWaves, WIDE>(to + RK::size(KT), vp, a.vs[1], 0, nk - 1 - k0, a.dim_v);
+            kp = uniform_ptr(kp + KT * a.ks[1]);
+            vp = uniform_ptr(vp + KT * a.vs[1]);
         };
         const int trips = (end + KT - 1) / KT;
         // the mask's byte of this lane's key of the next tile, compared only when
@@ -369,15 +397,17 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 const float x = a.lse[m * a.lse_map + at];
                 lse[m] = x == -INFINITY ? INFINITY : x * kLog2e;
             }
-            if (l < 32 && i < a.len_q)
-                a.dsum[m * a.lse_map + at] = D[m];
+            if (l < 32 && i < a.len_q) {
+                a.stats[m * a.lse_map + at] = lse[m];
+                a.stats[(2 + m) * a.lse_map + at] = D[m];
+            }
         }
         f32x16 acc[2][S::TK] = {};
         float dlam = 0.0f;
         Range range;
         for (int t = 0; t < trips; ++t) {
             const int k0 = t * KT, buf = t & 1;
-            char *kb = lds + buf * S::kKeyTile, *vb = kb + KT * RK::kBytes;
+            char *kb = lds + buf * S::kKeyTile, *vb = kb + RK::size(KT);
             wait_loads();
             __syncthreads();
             const uint64_t seen = __ballot(next != 0 && l < KT && k0 + l < nk);
@@ -391,6 +421,8 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 clear_rows<T, DVP, KT, kAttnWaves>(vb, seen);
                 __syncthreads();
             }
+            const uint32_t kr = lds_address(kb) + RK::row_lane(), kc = lds_address(kb) + RK::col_lane();
+            const uint32_t vr = lds_address(vb) + RV::row_lane();
 #pragma unroll
             for (int kt = 0; kt < KT / 32; ++kt) {
                 const int j0 = k0 + 32 * kt;
@@ -401,10 +433,10 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int x = 0; x < S::CK; ++x)
-                        mma<T>(s[m], RK::row_chunk(kb, 32 * kt, m * S::CK + x), q[m][x]);
+                        mma<T>(s[m], RK::row_chunk(kr, 32 * kt, m * S::CK + x), q[m][x]);
 #pragma unroll
                 for (int x = 0; x < S::CV; ++x)
-                    mma<T>(dp, RV::row_chunk(vb, 32 * kt, x), g[x]);
+                    mma<T>(dp, RV::row_chunk(vr, 32 * kt, x), g[x]);
                 if (some_hidden || j0 + 32 > wall) {
                     hide(s[0], j0, limit, (uint32_t)(seen >> (32 * kt)));
                     hide(s[1], j0, limit, (uint32_t)(seen >> (32 * kt)));
@@ -438,7 +470,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                     for (int x = 0; x < S::CP; ++x)
 #pragma unroll
                         for (int v = 0; v < S::TK; ++v)
-                            mma<T>(acc[m][v], RK::col_chunk(kb, 32 * kt, x, m * DP + 32 * v), ds[m][x]);
+                            mma<T>(acc[m][v], RK::col_chunk(kc, 32 * kt, x, m * DP + 32 * v), ds[m][x]);
             }
         }
         __syncthreads();
@@ -480,19 +512,18 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
     constexpr int QT = S::kQueries;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int l = lane_id(), w = wave_id();
-    const int tiles = (a.len_k + kBlockRows - 1) / kBlockRows;
     const int heads = a.parts ? a.heads : a.kv_heads;
-    const int64_t total = (int64_t)tiles * heads * a.batch;
+    const uint32_t tiles = (a.len_k + kBlockRows - 1) / kBlockRows, total = tiles * heads * a.batch;
     const float c = a.scale * kLog2e;
     if (a.dim < DP || a.dim_v < DVP) {
-        for (int e = threadIdx.x; e < 2 * S::kQueryTile / 16; e += kAttnThreads)
+        for (int e = threadIdx.x; e < (2 * S::kQueryTile + S::kValues) / 16; e += kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
-    for (int64_t n = blockIdx.x; n < total; n += gridDim.x) {
-        const int64_t item = die_order(n, total);
-        const int bh = (int)(item / tiles), k0 = (int)(item % tiles) * kBlockRows;  // causal: the longest first
-        const int b = bh / heads, hx = bh - b * heads, hk = a.parts ? hx / a.group : hx;
+    for (uint32_t n = blockIdx.x; n < total; n += gridDim.x) {
+        const Item item(n, total, tiles, heads);
+        const int k0 = item.tile * kBlockRows;  // causal: the longest first
+        const int b = item.b, hx = item.h, hk = a.parts ? uniform(hx / a.group) : hx;
         const int h0 = a.parts ? hx : hx * a.group, h1 = a.parts ? hx + 1 : h0 + a.group;
         const int nq = q_len_of(a, b), nk = k_len_of(a, b);
         const int j = k0 + 32 * w + (l & 31);  // this lane's key
@@ -504,19 +535,23 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         const bool all = __all(seen);
         const bool wany = __any(seen);
 
-        uint4v kf[2][S::CK], vf[S::CV];
+        uint4v kf[2][S::CK];
         {
             const T *krow = (const T *)a.k + b * a.ks[0] + j * a.ks[1] + hk * a.ks[2];
-            const T *vrow = (const T *)a.v + b * a.vs[0] + j * a.vs[1] + hk * a.vs[2];
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int s = 0; s < S::CK; ++s)
                     kf[m][s] = memory_chunk<T, WIDE>(krow + m * a.ks[3], s, a.dim, seen);
-#pragma unroll
-            for (int s = 0; s < S::CV; ++s)
-                vf[s] = memory_chunk<T, WIDE>(vrow, s, a.dim_v, seen);
         }
+        // The wave's 32 rows of values stay in LDS: with them in registers too, two
+        // maps of 64 bf16 channels did not fit 256.  (The largest class has no LDS
+        // for them and reads them again and again, through the caches.)
+        char *vrows = lds + 2 * S::kQueryTile + RV::size(32) * w;
+        const T *vrow = (const T *)a.v + b * a.vs[0] + j * a.vs[1] + hk * a.vs[2];
+        if constexpr (S::kKeepValues)
+            for (int s = 0; s < S::CV; ++s)
+                store16(vrows + RV::at(l & 31, 2 * s + (l >> 5)), memory_chunk<T, WIDE>(vrow, s, a.dim_v, seen));
         f32x16 gk[2][S::TK] = {}, gv[S::TV] = {};
         Range range;
         // fp16: probabilities, at most 1 + |lambda| together, go into the product
@@ -528,81 +563,89 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 most = __builtin_fmaxf(most, __builtin_fabsf((float)((const T *)a.lam)[h]));
             lift = (float)(14 - __builtin_amdgcn_frexp_expf(1.0f + most));
         }
+        const float lifted = lift / c;  // what the scores' sums start from
 
-        // tiles of all heads in one run: trip t is tile t % per of head h0 + t / per
+        // tiles of all heads in one run, loads a tile ahead
         const int per = nk > k0 && nq > first ? (nq - first + QT - 1) / QT : 0;
         const int trips = per * (h1 - h0);
-        float stat = 0.0f;
         int nh = h0, ni = first;  // head and first query of the next tile to load
+        const T *qp, *gp;
+        const float *sp;
+        auto head = [&](int h) {
+            qp = uniform_ptr((const T *)a.q + b * a.qs[0] + first * a.qs[1] + h * a.qs[2]);
+            gp = uniform_ptr((const T *)a.dout + b * a.dos[0] + first * a.dos[1] + h * a.dos[2]);
+            sp = uniform_ptr(a.stats + ((int64_t)b * a.heads + h) * a.len_q + first);
+        };
         auto issue = [&](int buf) {
             char *to = lds + buf * S::kQueryTile;
-            const T *qp = (const T *)a.q + b * a.qs[0] + ni * a.qs[1] + nh * a.qs[2];
-            const T *gp = (const T *)a.dout + b * a.dos[0] + ni * a.dos[1] + nh * a.dos[2];
             load_rows<T, 2 * DP, 2, QT, kAttnWaves, WIDE>(to, qp, a.qs[1], a.qs[3], nq - 1 - ni, a.dim);
-            load_rows<T, DVP, 1, QT, kAttnWaves, WIDE>(to + QT * RK::kBytes, gp, a.dos[1], 0, nq - 1 - ni, a.dim_v);
-            if (threadIdx.x < 4 * QT) {  // statistics of both maps, then D of both
-                const int what = threadIdx.x / QT, i = ni + threadIdx.x % QT;
-                stat = what < 2 ? INFINITY : 0.0f;
-                if (i < nq) {
-                    const int64_t at = ((int64_t)b * a.heads + nh) * a.len_q + i;
-                    if (what < 2) {
-                        const float x = a.lse[what * a.lse_map + at];
-                        stat = x == -INFINITY ? INFINITY : x * kLog2e - lift;
-                    } else {
-                        stat = a.dsum[(what - 2) * a.lse_map + at];
-                    }
-                }
+            load_rows<T, DVP, 1, QT, kAttnWaves, WIDE>(to + RK::size(QT), gp, a.dos[1], 0, nq - 1 - ni, a.dim_v);
+            if (w < 2) {  // 4 statistics of 32 queries: a wave takes two of them
+                const int y = again(l);
+                const float *p = sp + (2 * w + (y >> 5)) * a.lse_map + min(y & 31, nq - 1 - ni);
+                __builtin_amdgcn_global_load_lds((const PAM_GLOBAL void *)p,
+                                                 (PAM_LDS void *)(to + RK::size(QT) + RV::size(QT) + w * 256), 4, 0, 0);
             }
             ni += QT;
-            if (ni >= nq) {
+            qp = uniform_ptr(qp + QT * a.qs[1]);
+            gp = uniform_ptr(gp + QT * a.dos[1]);
+            sp += QT;
+            if (ni >= nq && ++nh < h1) {
                 ni = first;
-                ++nh;
+                head(nh);
             }
         };
-        auto stats_of = [&](int buf) {
-            return reinterpret_cast<float *>(lds + buf * S::kQueryTile + QT * (RK::kBytes + RV::kBytes));
-        };
         if (trips > 0) {
+            head(h0);
             issue(0);
-            if (threadIdx.x < 4 * QT)
-                stats_of(0)[threadIdx.x] = stat;
         }
-        int ci = first, ch = h0;  // of the tile at hand
+        int i0 = first - QT, ch = h0;  // of the tile at hand
+        float lam = -uniform_float((float)((const T *)a.lam)[h0]);
         for (int t = 0; t < trips; ++t) {
             const int buf = t & 1;
-            char *qb = lds + buf * S::kQueryTile, *gb = qb + QT * RK::kBytes;
-            const float *st = stats_of(buf);
+            char *qb = lds + buf * S::kQueryTile, *gb = qb + RK::size(QT);
+            const float *st = reinterpret_cast<const float *>(gb + RV::size(QT));
+            i0 += QT;
+            if (i0 >= nq) {
+                i0 = first;
+                lam = -uniform_float((float)((const T *)a.lam)[++ch]);
+            }
             wait_loads();
             __syncthreads();
             if (t + 1 < trips)
                 issue(buf ^ 1);
-            const int i0 = ci;
-            const float lam = -(float)((const T *)a.lam)[ch];
-            ci += QT;
-            if (ci >= nq) {
-                ci = first;
-                ++ch;
-            }
-            if (i0 + QT > nq) {  // rows past the sequence
+            const bool tail = i0 + QT > nq;
+            if (tail) {  // rows past the sequence
                 clear_rows<T, 2 * DP, QT, kAttnWaves>(qb, (1ull << (nq - i0)) - 1);
                 clear_rows<T, DVP, QT, kAttnWaves>(gb, (1ull << (nq - i0)) - 1);
                 __syncthreads();
             }
             if (wany && i0 + QT > wfirst) {
+                const uint32_t qr = lds_address(qb) + RK::row_lane(), qc = lds_address(qb) + RK::col_lane();
+                const uint32_t gr = lds_address(gb) + RV::row_lane(), gc = lds_address(gb) + RV::col_lane();
+                const uint32_t vr = lds_address(vrows) + RV::row_lane();
                 f32x16 s[2] = {}, dp = {};
+                if constexpr (std::is_same<T, f16>::value) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[0][r] = s[1][r] = lifted;
+                }
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int x = 0; x < S::CK; ++x)
-                        mma<T>(s[m], RK::row_chunk(qb, 0, m * S::CK + x), kf[m][x]);
+                        mma<T>(s[m], RK::row_chunk(qr, 0, m * S::CK + x), kf[m][x]);
 #pragma unroll
                 for (int x = 0; x < S::CV; ++x)
-                    mma<T>(dp, RV::row_chunk(gb, 0, x), vf[x]);
-                if (!all || i0 < wfirst + 31) {
-                    const int lim = from - i0 - 4 * (l >> 5);
+                    if constexpr (S::kKeepValues)
+                        mma<T>(dp, RV::row_chunk(gr, 0, x), RV::row_chunk(vr, 0, x));
+                    else
+                        mma<T>(dp, RV::row_chunk(gr, 0, x), memory_chunk<T, WIDE>(vrow, x, a.dim_v, seen));
+                if (!all || i0 < wfirst + 31 || tail) {
+                    const int lim = from - i0 - 4 * (l >> 5), rows = nq - i0 - 4 * (l >> 5);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const bool see = 8 * (r >> 2) + (r & 3) >= lim;
+                        const bool see = 8 * (r >> 2) + (r & 3) >= lim && 8 * (r >> 2) + (r & 3) < rows;
                         s[0][r] = see ? s[0][r] : -INFINITY;
                         s[1][r] = see ? s[1][r] : -INFINITY;
                     }
@@ -610,23 +653,31 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 uint4v wf[S::CP], ds[2][S::CP];
                 f32x16 wt;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int at = 8 * g + 4 * (l >> 5);
-                    const float4v l0 = *reinterpret_cast<const float4v *>(st + at);
-                    const float4v l1 = *reinterpret_cast<const float4v *>(st + QT + at);
-                    const float4v d0 = *reinterpret_cast<const float4v *>(st + 2 * QT + at);
-                    const float4v d1 = *reinterpret_cast<const float4v *>(st + 3 * QT + at);
+                for (int x = 0; x < S::CP; ++x) {
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int r = 4 * g + y;
-                        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, -l0[y]));
-                        const float p1 = lam * __builtin_amdgcn_exp2f(__builtin_fmaf(s[1][r], c, -l1[y]));
-                        wt[r] = p0 + p1;
-                        s[0][r] = p0 * (dp[r] - d0[y]);
-                        s[1][r] = p1 * (dp[r] - d1[y]);
+                    for (int g = x * 4 / S::CP; g < (x + 1) * 4 / S::CP; ++g) {
+                        const int at = 8 * g + 4 * (l >> 5);
+                        const float4v l0 = *reinterpret_cast<const float4v *>(st + at);
+                        const float4v l1 = *reinterpret_cast<const float4v *>(st + QT + at);
+                        const float4v d0 = *reinterpret_cast<const float4v *>(st + 2 * QT + at);
+                        const float4v d1 = *reinterpret_cast<const float4v *>(st + 3 * QT + at);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const int r = 4 * g + y;
+                            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, -l0[y]));
+                            const float p1 = lam * __builtin_amdgcn_exp2f(__builtin_fmaf(s[1][r], c, -l1[y]));
+                            wt[r] = p0 + p1;
+                            s[0][r] = p0 * (dp[r] - d0[y]);
+                            s[1][r] = p1 * (dp[r] - d1[y]);
+                        }
+                    }
+                    wf[x] = operand<T>(wt, x);
+                    if constexpr (!std::is_same<T, f16>::value) {
+                        ds[0][x] = operand<T>(s[0], x);
+                        ds[1][x] = operand<T>(s[1], x);
                     }
                 }
-                if constexpr (std::is_same<T, f16>::value)
+                if constexpr (std::is_same<T, f16>::value) {
                     range.fit(s, [&](float f) {
 #pragma unroll
                         for (int m = 0; m < 2; ++m)
@@ -635,25 +686,23 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                                 gk[m][v] *= f;
                     });
 #pragma unroll
-                for (int x = 0; x < S::CP; ++x) {
-                    wf[x] = operand<T>(wt, x);
-                    ds[0][x] = operand<T>(s[0], x);
-                    ds[1][x] = operand<T>(s[1], x);
+                    for (int x = 0; x < S::CP; ++x) {
+                        ds[0][x] = operand<T>(s[0], x);
+                        ds[1][x] = operand<T>(s[1], x);
+                    }
                 }
 #pragma unroll
                 for (int x = 0; x < S::CP; ++x) {
 #pragma unroll
                     for (int v = 0; v < S::TV; ++v)
-                        mma<T>(gv[v], RV::col_chunk(gb, 0, x, 32 * v), wf[x]);
+                        mma<T>(gv[v], RV::col_chunk(gc, 0, x, 32 * v), wf[x]);
 #pragma unroll
                     for (int m = 0; m < 2; ++m)
 #pragma unroll
                         for (int v = 0; v < S::TK; ++v)
-                            mma<T>(gk[m][v], RK::col_chunk(qb, 0, x, m * DP + 32 * v), ds[m][x]);
+                            mma<T>(gk[m][v], RK::col_chunk(qc, 0, x, m * DP + 32 * v), ds[m][x]);
                 }
             }
-            if (t + 1 < trips && threadIdx.x < 4 * QT)
-                stats_of(buf ^ 1)[threadIdx.x] = stat;
         }
         __syncthreads();
         if (j >= a.len_k)
@@ -764,7 +813,7 @@ hipError_t bwd_class(const AttnArgs &a, hipStream_t s)
         e = launch_lds(k_attn_dq<T, DP, DVP, WIDE>, item_blocks(rows), 2 * S::kKeyTile, a, s);
     const int64_t keys = (int64_t)((a.len_k + kBlockRows - 1) / kBlockRows) * (a.parts ? a.heads : a.kv_heads) * a.batch;
     if (e == hipSuccess && keys)
-        e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE>, item_blocks(keys), 2 * S::kQueryTile, a, s);
+        e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE>, item_blocks(keys), 2 * S::kQueryTile + S::kValues, a, s);
     return e;
 }
 

@@ -28,9 +28,25 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 #define PAM_GLOBAL __attribute__((address_space(1)))
 
 __device__ __forceinline__ int lane_id() { return threadIdx.x & 63; }
+// address of LDS memory
+__device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)(uintptr_t)(const PAM_LDS char *)p; }
+template <class X>
+__device__ __forceinline__ PAM_LDS X *lds_at(uint32_t address)
+{
+    return (PAM_LDS X *)(uintptr_t)address;
+}
 // the wave's number within its block, in a scalar register
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 __device__ __forceinline__ int result_row(int r) { return 8 * (r >> 2) + 4 * (lane_id() >> 5) + (r & 3); }
+
+// x, of which the compiler cannot tell that it is the same in every turn of a
+// loop: what is derived from it is computed again there instead of being kept in
+// registers, or spilled, across the loop.
+__device__ __forceinline__ int again(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
 
 // channels (or rows) of a chunk
 template <class T>
@@ -75,53 +91,71 @@ __device__ __forceinline__ uint4v operand(const f32x16 &p, int s)
     }
 }
 
-// Rows of NC channels in LDS, without padding, since the loads that write LDS
-// directly fill it in order.  The 16-byte pieces of a row are permuted by an
-// exclusive or with an even number that depends on the row, so that eight
-// lanes that read one piece of eight rows, and sixteen that read two pieces of
-// four rows, meet every bank once.
+// Rows of NC channels in LDS.  The loads that write LDS directly fill 1024
+// bytes in order, so rows cannot be padded one by one: the 16-byte pieces of a
+// row are permuted by an exclusive or with 0, 2, 4 or 6, which depends on the
+// row, and 128 bytes are left free after every four rows of 256 bytes or more.
+// Eight lanes that read one piece of eight rows, and sixteen that read two
+// pieces of four rows, then meet every bank once; and the addresses of a
+// lane's pieces differ by constants in all but two bits, which keeps them in few
+// registers.
 template <class T, int NC>
 struct Rows {
     static constexpr int kBytes = NC * sizeof(T);  // per row
     static constexpr int kPieces = kBytes / 16;
-    static_assert(kPieces >= 8, "rows of 128 bytes at least");
+    static constexpr int kGap = kPieces == 8 ? 0 : 128;
+    static_assert(kPieces >= (sizeof(T) == 4 ? 16 : 8), "rows of 128 bytes (fp32: 256) at least");
+    static constexpr int size(int rows) { return rows * kBytes + rows / 4 * kGap; }
     __device__ __forceinline__ static int turn(int row)
     {
-        return kPieces == 8 ? (row & 6) : ((row & 7) << 1);
+        return kPieces == 8 ? (row & 6) : ((row & 3) << 1);
     }
+    __device__ __forceinline__ static int at(int row) { return row * kBytes + (row >> 2) * kGap; }
+    __device__ __forceinline__ static int at(int row, int piece) { return at(row) + ((piece ^ turn(row)) << 4); }
+    // A lane's place in a tile, to be added to the tile's address once, and the
+    // chunks that follow from the sum (tiles start at multiples of 128 bytes):
     // chunk s of channels of row (row0 + lane % 32)
-    __device__ __forceinline__ static uint4v row_chunk(const char *lds, int row0, int s)
+    __device__ __forceinline__ static uint32_t row_lane() { return at(lane_id() & 31, lane_id() >> 5); }
+    __device__ __forceinline__ static uint4v row_chunk(uint32_t tile_lane, int row0, int s)
     {
-        const int l = lane_id(), row = l & 31;
-        return load16(lds + (row0 + row) * kBytes + (((2 * s + (l >> 5)) ^ turn(row)) << 4));
+        return *lds_at<uint4v>((tile_lane ^ ((2 * s & 7) << 4)) + at(row0) + ((2 * s >> 3) << 7));
     }
     // chunk s of the rows from row0 on, column c0 + lane % 32 (c0 a multiple of 32)
-    __device__ __forceinline__ static uint4v col_chunk(const char *lds, int row0, int s, int c0)
+    __device__ __forceinline__ static uint32_t col_lane()
     {
         const int l = lane_id(), h = l >> 5;
+        if constexpr (sizeof(T) == 4)
+            return at(4 * h, (l & 31) >> 2) + ((l & 3) << 2);
+        else  // the transposing read: of sixteen lanes, lane 4 r + c gives the address of four columns of row r,
+              // and lane i gets column i of the four rows
+            return at(4 * h + ((l & 15) >> 2), 2 * ((l >> 4) & 1) + ((l & 3) >> 1)) + ((l & 1) << 3);
+    }
+    __device__ __forceinline__ static uint4v col_chunk(uint32_t tile_lane, int row0, int s, int c0)
+    {
         if constexpr (sizeof(T) == 4) {
             uint4v r;
-            const int piece = (c0 >> 2) + ((l & 31) >> 2);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = 4 * h + j;
-                r[j] = *reinterpret_cast<const uint32_t *>(lds + (row0 + 8 * s + row) * kBytes +
-                                                           ((piece ^ turn(row)) << 4) + ((l & 3) << 2));
-            }
+            for (int j = 0; j < 4; ++j)
+                r[j] = *lds_at<uint32_t>((tile_lane ^ (j << 5)) + j * kBytes + at(row0 + 8 * s) + (c0 << 2));
             return r;
         } else {
-            // the transposing read: of sixteen lanes, lane 4 r + c gives the
-            // address of four columns of row r, lane i gets column i of the four rows
-            const int row = 4 * h + ((l & 15) >> 2);
-            const int piece = ((2 * ((l >> 4) & 1) + ((l & 3) >> 1)) ^ turn(row)) ^ (c0 >> 3);
-            const char *p = lds + (row0 + 16 * s + row) * kBytes + (piece << 4) + ((l & 1) << 3);
-            const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PAM_LDS short4v *)p);
-            const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PAM_LDS short4v *)(p + 8 * kBytes));
+            const uint32_t p = (tile_lane ^ ((c0 & 32) << 1)) + at(row0 + 16 * s) + ((c0 >> 6) << 7);
+            const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<short4v>(p));
+            const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<short4v>(p + at(8)));
             const uint2v x = __builtin_bit_cast(uint2v, a), y = __builtin_bit_cast(uint2v, b);
             return uint4v{x[0], x[1], y[0], y[1]};
         }
     }
 };
+
+// A pointer that is the same in every lane, in scalar registers.
+template <class P>
+__device__ __forceinline__ P *uniform_ptr(P *p)
+{
+    const uint64_t x = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (P *)((uint64_t)hi << 32 | lo);
+}
 
 // Brings ROWS rows of PARTS parts (maps) of up to NC / PARTS channels from
 // memory to LDS.  Rows past `last` repeat row `last` (they are cleared, or
@@ -140,25 +174,25 @@ __device__ __forceinline__ void load_rows(char *lds, const T *from, int64_t row_
     if constexpr (WIDE) {
         constexpr int kLoads = ROWS * R::kBytes / 1024, kStep = WAVES * 64 / R::kPieces;  // rows between a wave's loads
         static_assert(kLoads % WAVES == 0, "whole loads per wave");
-        const int w = wave_id(), at = w * 64 + lane_id();
+        const int w = wave_id();
+        const uint32_t at = w * 64 + again(lane_id());
         const int row0 = at / R::kPieces;
 #pragma unroll
         for (int n = 0; n < kLoads / WAVES; ++n) {
             const int row = row0 + n * kStep;
-            const int piece = (at % R::kPieces) ^ R::turn(kStep % 8 == 0 ? row0 : row);
+            const uint32_t piece = (at % R::kPieces) ^ R::turn(kStep % 4 == 0 ? row0 : row);
             const int part = piece / kPart, ch = (piece % kPart) * per;
             const uint32_t off = (uint32_t)(min(row, last) * (int)row_stride + part * (int)part_stride + ch);
             if (ch < dim)
                 __builtin_amdgcn_global_load_lds(
                     (const PAM_GLOBAL void *)((const char *)from + (uint32_t)(off * sizeof(T))),
-                    (PAM_LDS void *)(lds + (n * WAVES + w) * 1024), 16, 0, 0);
+                    (PAM_LDS void *)(lds + R::at((n * WAVES + w) * 64 / R::kPieces)), 16, 0, 0);
         }
     } else {
-        for (int e = threadIdx.x; e < ROWS * PARTS * dim; e += 64 * WAVES) {
+        for (int e = again(threadIdx.x); e < ROWS * PARTS * dim; e += 64 * WAVES) {
             const int c = e % dim, part = e / dim % PARTS, row = e / dim / PARTS;
             const int ch = part * (NC / PARTS) + c;
-            const int piece = (ch / per) ^ R::turn(row);
-            *reinterpret_cast<T *>(lds + row * R::kBytes + piece * 16 + (ch % per) * sizeof(T)) =
+            *reinterpret_cast<T *>(lds + R::at(row, ch / per) + (ch % per) * sizeof(T)) =
                 from[min(row, last) * row_stride + part * part_stride + c];
         }
     }
@@ -169,9 +203,9 @@ template <class T, int NC, int ROWS, int WAVES>
 __device__ __forceinline__ void clear_rows(char *lds, uint64_t seen)
 {
     using R = Rows<T, NC>;
-    for (int e = threadIdx.x; e < ROWS * R::kPieces; e += 64 * WAVES)
+    for (int e = again(threadIdx.x); e < ROWS * R::kPieces; e += 64 * WAVES)
         if (!(seen >> (e / R::kPieces) & 1))
-            store16(lds + e * 16, uint4v{0, 0, 0, 0});
+            store16(lds + R::at(e / R::kPieces) + e % R::kPieces * 16, uint4v{0, 0, 0, 0});
 }
 
 // A row as an operand, straight from memory: chunk s of channels of `row` for
