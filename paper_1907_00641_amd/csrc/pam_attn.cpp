@@ -65,29 +65,106 @@ Wide wide_of(const pam_diff_attn_desc_t &d, const void *q, const void *k, const 
     return w;
 }
 
-// Whether the keys' gradients are formed per head and then added up: heads
-// that share keys, and too few blocks of 128 keys for the card without (two per
-// CU: 256 blocks of unequal length leave half the card idle at the end).
-bool split_heads(const pam_diff_attn_desc_t &d)
+// Blocks that the card holds at once: 256 CUs with two (one, where a lane's
+// registers or a block's LDS are for one) of four waves.
+constexpr int64_t kCUs = 256;
+
+int64_t at_once(const pam_diff_attn_desc_t &d)
 {
-    const int64_t blocks = (int64_t)((d.len_k + 127) / 128) * d.kv_heads * d.batch;
-    return d.heads > d.kv_heads && blocks < 1024 && d.len_q > 0;
+    const int cls = attn_class(d.dim, d.dim_v);
+    return kCUs * (cls == 0 || (cls == 1 && d.dtype != PAM_F32) ? 2 : 1);
 }
 
-int64_t rows_of(const pam_diff_attn_desc_t &d) { return (int64_t)d.batch * d.heads * d.len_q; }
-// the rows' statistics and their parts of grad_lambda, whole groups of four floats
-int64_t row_floats(const pam_diff_attn_desc_t &d) { return (5 * rows_of(d) + 3) / 4 * 4; }
+// Units beyond whole rounds of `room` blocks are cut into parts that fill one
+// more round, of at least `least` of the unit's `trips` each.  Causal units are of
+// unequal lengths and fill the rounds by themselves, longest first, where there
+// are enough.
+Plan plan_of(int64_t tiles, int64_t heads, int64_t batch, int64_t room, int64_t trips, int64_t least, bool causal)
+{
+    Plan p{};
+    p.tiles = (uint32_t)tiles;
+    p.heads = (uint32_t)heads;
+    p.rows_of_heads = causal ? (uint32_t)(heads * batch) : 0;
+    const int64_t units = tiles * heads * batch;
+    p.units = p.full = (uint32_t)units;
+    p.parts = 1;
+    const int64_t most = trips / least;
+    if (units == 0 || most < 2 || (causal && units >= room))
+        return p;
+    const int64_t full = units / room * room, rest = units - full;
+    if (rest == 0)
+        return p;
+    const int64_t parts = std::min(most, (causal ? 2 * room : room) / rest);
+    if (parts < 2)
+        return p;
+    p.full = (uint32_t)full;
+    p.parts = (uint32_t)parts;
+    return p;
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct FwdPlan {
+    Plan plan;
+    bool few;
+    int value_parts, rows, dvp;
+    int64_t floats() const { return plan.parts > 1 ? (int64_t)plan.slots() * rows * (2 * dvp + 4) : 0; }
+};
+
+FwdPlan fwd_plan(const pam_diff_attn_desc_t &d)
+{
+    FwdPlan f;
+    const int cls = attn_class(d.dim, d.dim_v);
+    f.dvp = cls == 0 ? 64 : 128;
+    f.value_parts = (int)ceil_div(d.dim_v, f.dvp);
+    // a block of 128 rows of one head would be half empty
+    f.few = d.len_q <= 64;
+    const bool causal = d.flags & PAM_ATTN_CAUSAL;
+    if (f.few) {
+        f.rows = 32;
+        const int64_t tiles = ceil_div((int64_t)(d.heads / d.kv_heads) * d.len_q, 32);
+        // a block's four waves take a part each already
+        f.plan = plan_of(tiles, (int64_t)d.kv_heads * f.value_parts, d.batch, kCUs, ceil_div(d.len_k, 128), 2, false);
+    } else {
+        f.rows = 128;
+        f.plan = plan_of(ceil_div(d.len_q, 128), (int64_t)d.heads * f.value_parts, d.batch, at_once(d),
+                         ceil_div(d.len_k, 64), 4, causal);
+    }
+    return f;
+}
+
+struct BwdPlan {
+    Plan rows, keys;
+    int64_t stats, dlam, row_part, key_part;  // floats
+};
+
+BwdPlan bwd_plan(const pam_diff_attn_desc_t &d)
+{
+    BwdPlan p;
+    const bool causal = d.flags & PAM_ATTN_CAUSAL;
+    const int cls = attn_class(d.dim, d.dim_v), dp = cls == 0 ? 32 : (cls == 1 ? 64 : 128);
+    p.rows = plan_of(ceil_div(d.len_q, 128), d.heads, d.batch, at_once(d), ceil_div(d.len_k, 64), 4,
+                     causal);
+    p.keys = plan_of(ceil_div(d.len_k, 128), d.kv_heads, d.batch, at_once(d),
+                     ceil_div(d.len_q, 32) * (d.heads / d.kv_heads), 8, causal);
+    p.stats = 4 * (int64_t)d.batch * d.heads * d.len_q;
+    p.dlam = (int64_t)p.rows.items() * 4;
+    p.row_part = (int64_t)p.rows.slots() * 128 * 2 * dp;
+    p.key_part = (int64_t)p.keys.slots() * 128 * 4 * dp;
+    return p;
+}
 
 }  // namespace
 
-size_t attn_fwd_workspace(const pam_diff_attn_desc_t &) { return 0; }
+size_t attn_fwd_workspace(const pam_diff_attn_desc_t &d)
+{
+    return d.batch && d.len_q ? (size_t)fwd_plan(d).floats() * sizeof(float) : 0;
+}
 
 size_t attn_bwd_workspace(const pam_diff_attn_desc_t &d)
 {
-    int64_t n = row_floats(d);
-    if (split_heads(d))
-        n += (int64_t)d.batch * d.len_k * d.heads * (2 * d.dim + d.dim_v);
-    return (size_t)n * sizeof(float);
+    const BwdPlan p = bwd_plan(d);
+    return (size_t)(p.row_part + p.key_part + p.stats + p.dlam) * sizeof(float);
 }
 
 hipError_t launch_attn_fwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
@@ -98,12 +175,17 @@ hipError_t launch_attn_fwd(const pam_diff_attn_desc_t &d, const void *q, const v
     a.out = out;
     a.so = so;
     a.lse = lse;
+    const FwdPlan f = fwd_plan(d);
+    a.plan = f.plan;
+    a.value_parts = f.value_parts;
+    a.part = (float *)workspace;
     Wide w = wide_of(d, q, k, v);
     w.at(out);
     w.at(so);
+    a.wide = w.ok;
     if (d.dtype == PAM_F32)
-        return attn_fwd_f32(a, w.ok, s);
-    return d.dtype == PAM_F16 ? attn_fwd_f16(a, w.ok, s) : attn_fwd_bf16(a, w.ok, s);
+        return attn_fwd_f32(a, w.ok, f.few, s);
+    return d.dtype == PAM_F16 ? attn_fwd_f16(a, w.ok, f.few, s) : attn_fwd_bf16(a, w.ok, f.few, s);
 }
 
 hipError_t launch_attn_bwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
@@ -121,18 +203,22 @@ hipError_t launch_attn_bwd(const pam_diff_attn_desc_t &d, const void *q, const v
     a.gk = gk;
     a.gv = gv;
     a.glam = glam;
-    a.stats = (float *)workspace;
-    a.dlam = a.stats + 4 * a.lse_map;
-    if (split_heads(d)) {
-        a.parts = a.stats + row_floats(d);
-        a.parts_v = (int64_t)d.batch * d.len_k * d.heads * 2 * d.dim;
-    }
+    // whole groups of four floats first
+    const BwdPlan p = bwd_plan(d);
+    a.plan = p.rows;
+    a.key_plan = p.keys;
+    a.part = (float *)workspace;
+    a.key_part = a.part + p.row_part;
+    a.stats = a.key_part + p.key_part;
+    a.dlam = a.stats + p.stats;
+    a.value_parts = 1;
     Wide w = wide_of(d, q, k, v);
     w.rows(dout, dos, 3, d.dim_v);
     w.at(so);
     w.at(gq);
     w.at(gk);
     w.at(gv);
+    a.wide = w.ok;
     if (d.dtype == PAM_F32)
         return attn_bwd_f32(a, w.ok, s);
     return d.dtype == PAM_F16 ? attn_bwd_f16(a, w.ok, s) : attn_bwd_bf16(a, w.ok, s);

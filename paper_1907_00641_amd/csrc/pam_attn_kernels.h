@@ -42,14 +42,17 @@ struct Sizes {
     // LDS: a tile of keys and values; of queries and dout with 4 statistics
     // each; the block's values of the keys' pass
     static constexpr int kKeyTile = RK::size(kKeys) + RV::size(kKeys);
+    // a wave's own tile of 32 keys in the kernel for few queries, and the waves
+    // of a block that have LDS for two of them, and for their sums
+    static constexpr int kFewTile = RK::size(32) + RV::size(32);
+    static constexpr int kFewWaves = (2 * kFewTile + 512) * 4 <= (160 << 10) ? 4 : ((2 * kFewTile + 512) * 2 <= (160 << 10) ? 2 : 1);
     static constexpr int kQueryTile = RK::size(kQueries) + RV::size(kQueries) + 4 * kQueries * 4;
     static constexpr bool kKeepValues = 2 * kQueryTile + RV::size(kBlockRows) <= (160 << 10);
     static constexpr int kValues = kKeepValues ? RV::size(kBlockRows) : 0;
 };
 
-// fp16 has 2^-14 as its smallest full-precision value.  Probabilities are at
-// most 2^8 of the running maximum's: 2^7 more keeps them under 2^15 and gives
-// small ones 7 bits of room.
+// fp16 has 2^-14 as its smallest full-precision value: its probabilities are
+// taken 2^7 larger, which gives small ones 7 bits of room, and are at most 2^15.
 template <class T>
 constexpr float kLift = std::is_same<T, f16>::value ? 7.0f : 0.0f;
 
@@ -85,13 +88,14 @@ struct Range {
     __device__ __forceinline__ float down() const { return up == 0.0f ? 1.0f : 1.0f / up; }
 };
 
-// Work item n of `total` for the block that the dispatcher hands out as number
-// n: consecutive items, which share keys and values, go to one of the eight
-// dies (blocks go round them), so that its L2 serves them.
-__device__ __forceinline__ uint32_t die_order(uint32_t n, uint32_t total)
+// Orders a wave's own LDS accesses: its lanes exchange data through LDS.  They are
+// waited for, since the loads that write LDS directly keep no order with them.
+__device__ __forceinline__ void wave_fence()
 {
-    const uint32_t per = total / 8, rest = total - per * 8, die = n % 8;
-    return die * per + min(die, rest) + n / 8;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt 0, others not waited for
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // A value that is the same in every lane, in a scalar register: divisions are
@@ -102,15 +106,45 @@ __device__ __forceinline__ float uniform_float(float x)
     return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
 }
 
-// Item n: its tile of 128 rows, sequence and head.
+// Work items.  A unit is a tile of rows of one head of one sequence.  Units come
+// in an order that starts with the longest; the first `full` of them are one item
+// each, whole rounds of the blocks that the card holds at once; the others, which
+// would leave most of the card idle, are `parts` items each, cut along the
+// walked axis, whose 32-bit sums a second kernel joins.
 struct Item {
-    int tile, b, h;
-    __device__ __forceinline__ Item(uint32_t n, uint32_t total, uint32_t tiles, uint32_t heads)
+    int tile, b, h, part, parts;
+    uint32_t slot;  // items that are parts: their number
+    // The dispatcher deals blocks to the eight dies in turn.  Units of one length:
+    // consecutive ones, which share keys and values, go to one die, so that its L2
+    // serves them.  Causal units are numbered tile by tile, the longest first, and
+    // taken as they come: every die gets as many long ones (and the same heads,
+    // where those are a multiple of eight).
+    __device__ __forceinline__ static uint32_t order(const Plan &p, uint32_t n, uint32_t total)
     {
-        const uint32_t x = die_order(n, total), bh = x / tiles;
-        tile = uniform(x - bh * tiles);
-        b = uniform(bh / heads);
-        h = uniform(bh - bh / heads * heads);
+        if (p.rows_of_heads)
+            return n;
+        const uint32_t per = total / 8, rest = total - per * 8, die = n % 8;
+        return die * per + min(die, rest) + n / 8;
+    }
+    __device__ __forceinline__ Item(const Plan &p, uint32_t n)
+    {
+        const bool whole = n < p.full;
+        const uint32_t m = uniform(order(p, whole ? n : n - p.full, whole ? p.full : (p.units - p.full) * p.parts));
+        const uint32_t cut = uniform(m / p.parts), unit = whole ? m : p.full + cut;
+        parts = whole ? 1 : p.parts;
+        part = whole ? 0 : m - cut * p.parts;
+        slot = whole ? 0 : m;
+        const uint32_t bh = p.bh_of(unit);
+        tile = uniform(p.tile_of(unit));
+        b = uniform(bh / p.heads);
+        h = uniform(bh - bh / p.heads * p.heads);
+    }
+    // the walked tiles of this item, of `trips` of its unit
+    __device__ __forceinline__ void range(int trips, int &from, int &to) const
+    {
+        const int per = (trips + parts - 1) / parts;
+        from = min(part * per, trips);
+        to = min(from + per, trips);
     }
 };
 
@@ -138,13 +172,153 @@ __device__ __forceinline__ void hide(f32x16 &s, int key0, int limit, uint32_t se
 // forward
 // ---------------------------------------------------------------------------
 
-// One pass over the keys with a running maximum and sum per map.  Scores are
-// formed transposed (rows keys, columns queries), so a lane holds one query: its
-// statistics need one exchange with the lane 32 away per tile, and scaling the
-// sums of values, which are formed transposed too, needs none.  The maximum
-// is followed only when it grew by more than 2^8 (then the sums are scaled): the
-// probabilities are at most 2^8 then, and nothing is lost, since both sums
-// carry the same factor.
+// What a wave has of its 32 queries (a lane: query l % 32), and a step over 32
+// keys.  Scores are formed transposed (rows keys, columns queries), so a lane
+// holds one query: its statistics need an exchange with the lane 32 away alone,
+// and scaling the sums of values, which are formed transposed too, needs none.
+// The maximum is followed only when it grew by more than 2^8 (then the sums are
+// scaled): the probabilities are at most 2^8 then, and nothing is lost, since both
+// sums carry the same factor.
+// The sums of the two maps are kept apart, since their normalisers are known
+// only at the end; a first pass for those would allow one product with
+// p^0 - lambda p^1 instead of two, and take as many products and twice the
+// exponentials.
+template <class T, int DP, int DVP>
+struct Queries {
+    using S = Sizes<T, DP, DVP>;
+    uint4v q[2][S::CK];
+    f32x16 o[2][S::TV];
+    float top[2], sum[2];  // base 2; a lane's own keys' share of the sum
+
+    template <bool WIDE>
+    __device__ __forceinline__ void start(const AttnArgs &a, const T *row, bool in)
+    {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+            for (int s = 0; s < S::CK; ++s)
+                q[m][s] = memory_chunk<T, WIDE>(row + m * a.qs[3], s, a.dim, in);
+#pragma unroll
+            for (int v = 0; v < S::TV; ++v)
+                o[m][v] = f32x16{};
+            top[m] = -INFINITY;
+            sum[m] = 0.0f;
+        }
+    }
+    // keys and values from row r0 of a tile (kr, vc: this lane's places in it);
+    // `some`: keys from j0 on that are past `limit` or not in `seen` are hidden
+    __device__ __forceinline__ void step(uint32_t kr, uint32_t vc, int r0, float c, bool some, int j0, int limit,
+                                         uint32_t seen)
+    {
+        using RK = typename S::RK;
+        using RV = typename S::RV;
+        f32x16 s[2] = {};
+#pragma unroll
+        for (int x = 0; x < S::CK; ++x)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+                mma<T>(s[m], RK::row_chunk(kr, r0, m * S::CK + x), q[m][x]);
+        if (some) {
+            hide(s[0], j0, limit, seen);
+            hide(s[1], j0, limit, seen);
+        }
+        uint4v p[2][S::CP];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            float mx = s[m][0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r)
+                mx = __builtin_fmaxf(mx, s[m][r]);
+            mx *= c;
+            if (__any(mx > top[m] + 8.0f)) {
+                const float to = __builtin_fmaxf(top[m], xor32_max(mx));
+                const float f = top[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[m] - to);
+                top[m] = to;
+                sum[m] *= f;
+#pragma unroll
+                for (int v = 0; v < S::TV; ++v)
+                    o[m][v] *= f;
+            }
+            const float base = top[m] == -INFINITY ? 0.0f : top[m] - kLift<T>;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[m][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][r], c, -base));
+                sum[m] += s[m][r];
+            }
+#pragma unroll
+            for (int x = 0; x < S::CP; ++x)
+                p[m][x] = operand<T>(s[m], x);
+        }
+#pragma unroll
+        for (int x = 0; x < S::CP; ++x)
+#pragma unroll
+            for (int v = 0; v < S::TV; ++v) {
+                const uint4v vf = RV::col_chunk(vc, r0, x, 32 * v);
+                mma<T>(o[0][v], vf, p[0][x]);
+                mma<T>(o[1][v], vf, p[1][x]);
+            }
+    }
+    __device__ __forceinline__ void whole_sums()
+    {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            sum[m] = xor32_add(sum[m]);
+    }
+    // unnormalised sums and statistics of this lane's query, for a later join:
+    // o as [map][DVP], then the tops and sums
+    __device__ __forceinline__ void leave(float *sums, float *stats) const
+    {
+        const int l = lane_id();
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int v = 0; v < S::TV; ++v)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<float4v *>(sums + m * DVP + 32 * v + 8 * g + 4 * (l >> 5)) =
+                        float4v{o[m][v][4 * g], o[m][v][4 * g + 1], o[m][v][4 * g + 2], o[m][v][4 * g + 3]};
+        if (l < 32)
+            *reinterpret_cast<float4v *>(stats) = float4v{top[0], top[1], sum[0], sum[1]};
+    }
+};
+
+// a row's logarithm of its sum, from the running maximum in base 2
+template <class T>
+__device__ __forceinline__ float lse_of(float top, float sum)
+{
+    return sum != 0.0f ? (top - kLift<T> + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+}
+
+// The keys of a tile that are part of the sequence and not hidden, as bits.
+// The mask's byte of a lane's key is loaded with the tile and compared only when
+// that has arrived: a comparison before would wait for all the loads.
+struct KeyMask {
+    const uint8_t *mask;
+    int nk, next = 1;
+    __device__ __forceinline__ KeyMask(const AttnArgs &a, int b, int keys)
+        : mask(a.key_mask ? a.key_mask + (int64_t)b * a.len_k : nullptr), nk(keys)
+    {
+    }
+    template <int KT>
+    __device__ __forceinline__ void fetch(int k0)
+    {
+        const int l = lane_id(), j = k0 + l;
+        next = mask && l < KT && j < nk ? (int)mask[j] : 1;
+    }
+    template <int KT>
+    __device__ __forceinline__ uint64_t seen(int k0) const
+    {
+        const int l = lane_id();
+        return __ballot(next != 0 && l < KT && k0 + l < nk);
+    }
+};
+template <int KT>
+constexpr uint64_t kAllSeen = KT == 64 ? ~0ull : (1ull << KT) - 1;
+
+// Blocks of four waves, 128 queries of one head; the waves share the tiles.
+// Heads sizes over 64 take the values' channels 128 at a time (a.value_parts):
+// both maps' sums of 256 did not fit the registers, and spilling them cost more
+// than forming the scores twice.
 template <class T, int DP, int DVP, bool WIDE>
 __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) void k_attn_fwd(AttnArgs a)
 {
@@ -154,17 +328,18 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
     constexpr int KT = S::kKeys;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int l = lane_id(), w = wave_id();
-    const uint32_t tiles = (a.len_q + kBlockRows - 1) / kBlockRows, total = tiles * a.heads * a.batch;
     const float c = a.scale * kLog2e;
-    if (a.dim < DP || a.dim_v < DVP) {  // the channels that no load writes
+    if (a.dim < DP || a.dim_v % DVP) {  // the channels that no load writes
         for (int e = threadIdx.x; e < 2 * S::kKeyTile / 16; e += kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
-    for (uint32_t n = blockIdx.x; n < total; n += gridDim.x) {
-        const Item item(n, total, tiles, a.heads);
-        const int q0 = ((int)tiles - 1 - item.tile) * kBlockRows;  // causal: the longest first
-        const int b = item.b, h = item.h, hk = uniform(h / a.group);
+    const uint32_t items = a.plan.items();
+    for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
+        const Item item(a.plan, n);
+        const int q0 = ((int)a.plan.tiles - 1 - item.tile) * kBlockRows;  // causal: the longest first
+        const int b = item.b, h = uniform(item.h / a.value_parts), hk = uniform(h / a.group);
+        const int v0 = (item.h - h * a.value_parts) * DVP, dim_v = min(a.dim_v - v0, DVP);
         const int nq = q_len_of(a, b), nk = k_len_of(a, b);
         const int i = q0 + 32 * w + (l & 31);  // this lane's query
         const bool in = i < nq;
@@ -175,49 +350,33 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         const int end = q0 < nq ? (a.causal ? min(nk, last + nk - nq + 1) : nk) : 0;
         const int wend = q0 + 32 * w < nq ? (a.causal ? min(nk, wlast + nk - nq + 1) : nk) : 0;
         const int wall = q0 + 32 * w + 31 < nq ? (a.causal ? min(nk, q0 + 32 * w + nk - nq + 1) : nk) : 0;
-        const T *kp = uniform_ptr((const T *)a.k + b * a.ks[0] + hk * a.ks[2]);
-        const T *vp = uniform_ptr((const T *)a.v + b * a.vs[0] + hk * a.vs[2]);
+        int from, to;
+        item.range(max(end + KT - 1, 0) / KT, from, to);
+        const T *kp = uniform_ptr((const T *)a.k + b * a.ks[0] + hk * a.ks[2] + (int64_t)from * KT * a.ks[1]);
+        const T *vp = uniform_ptr((const T *)a.v + b * a.vs[0] + hk * a.vs[2] + v0 + (int64_t)from * KT * a.vs[1]);
 
-        uint4v q[2][S::CK];
-        {
-            const T *row = (const T *)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int s = 0; s < S::CK; ++s)
-                    q[m][s] = memory_chunk<T, WIDE>(row + m * a.qs[3], s, a.dim, in);
-        }
-        f32x16 o[2][S::TV] = {};
-        float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
-
-        auto issue = [&](int k0, int buf) {  // tiles in order
-            char *at = lds + buf * S::kKeyTile;
-            load_rows<T, 2 * DP, 2, KT, kAttnWaves, WIDE>(at, kp, a.ks[1], a.ks[3], nk - 1 - k0, a.dim);
-            load_rows<T, DVP, 1, KT, kAttnWaves, WIDE>(at + RK::size(KT), vp, a.vs[1], 0, nk - 1 - k0, a.dim_v);
+        Queries<T, DP, DVP> Q;
+        Q.template start<WIDE>(a, (const T *)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2], in);
+        KeyMask mask(a, b, nk);
+        auto issue = [&](int t) {  // tiles in order
+            char *at = lds + (t & 1) * S::kKeyTile;
+            mask.template fetch<KT>(t * KT);
+            load_rows<T, 2 * DP, 2, KT, kAttnWaves, WIDE>(at, kp, a.ks[1], a.ks[3], nk - 1 - t * KT, a.dim);
+            load_rows<T, DVP, 1, KT, kAttnWaves, WIDE>(at + RK::size(KT), vp, a.vs[1], 0, nk - 1 - t * KT, dim_v);
             kp = uniform_ptr(kp + KT * a.ks[1]);
             vp = uniform_ptr(vp + KT * a.vs[1]);
         };
-        const int trips = (end + KT - 1) / KT;
-        // the mask's byte of this lane's key of the next tile, compared only when
-        // that tile is there: a comparison here would wait for all the loads
-        const uint8_t *mask = a.key_mask ? a.key_mask + (int64_t)b * a.len_k : nullptr;
-        auto mask_byte = [&](int j) { return mask && l < KT && j < nk ? (int)mask[j] : 1; };
-        int next = 1;
-        if (trips > 0) {
-            next = mask_byte(l);
-            issue(0, 0);
-        }
-        for (int t = 0; t < trips; ++t) {
-            const int k0 = t * KT, buf = t & 1;
-            char *kb = lds + buf * S::kKeyTile, *vb = kb + RK::size(KT);
+        if (from < to)
+            issue(from);
+        for (int t = from; t < to; ++t) {
+            const int k0 = t * KT;
+            char *kb = lds + (t & 1) * S::kKeyTile, *vb = kb + RK::size(KT);
             wait_loads();
             __syncthreads();  // tile t is there for every wave, and tile t - 1 done with
-            const uint64_t seen = __ballot(next != 0 && l < KT && k0 + l < nk);
-            if (t + 1 < trips) {
-                next = mask_byte(k0 + KT + l);
-                issue(k0 + KT, buf ^ 1);
-            }
-            const bool some_hidden = seen != (KT == 64 ? ~0ull : (1ull << KT) - 1);
+            const uint64_t seen = mask.template seen<KT>(k0);
+            if (t + 1 < to)
+                issue(t + 1);
+            const bool some_hidden = seen != kAllSeen<KT>;
             if (some_hidden) {  // the same in every wave of the block
                 clear_rows<T, 2 * DP, KT, kAttnWaves>(kb, seen);
                 clear_rows<T, DVP, KT, kAttnWaves>(vb, seen);
@@ -227,67 +386,22 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
 #pragma unroll
             for (int kt = 0; kt < KT / 32; ++kt) {
                 const int j0 = k0 + 32 * kt;
-                if (j0 >= wend)
-                    break;
-                f32x16 s[2] = {};
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int x = 0; x < S::CK; ++x)
-                        mma<T>(s[m], RK::row_chunk(kr, 32 * kt, m * S::CK + x), q[m][x]);
-                if (some_hidden || j0 + 32 > wall) {
-                    hide(s[0], j0, limit, (uint32_t)(seen >> (32 * kt)));
-                    hide(s[1], j0, limit, (uint32_t)(seen >> (32 * kt)));
-                }
-                uint4v p[2][S::CP];
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    float mx = s[m][0];
-#pragma unroll
-                    for (int r = 1; r < 16; ++r)
-                        mx = __builtin_fmaxf(mx, s[m][r]);
-                    mx = xor32_max(mx) * c;
-                    if (__any(mx > top[m] + 8.0f)) {
-                        const float to = __builtin_fmaxf(top[m], mx);
-                        const float f = top[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[m] - to);
-                        top[m] = to;
-                        sum[m] *= f;
-#pragma unroll
-                        for (int v = 0; v < S::TV; ++v)
-                            o[m][v] *= f;
-                    }
-                    const float base = top[m] == -INFINITY ? 0.0f : top[m] - kLift<T>;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        s[m][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][r], c, -base));
-                        sum[m] += s[m][r];
-                    }
-#pragma unroll
-                    for (int x = 0; x < S::CP; ++x)
-                        p[m][x] = operand<T>(s[m], x);
-                }
-#pragma unroll
-                for (int x = 0; x < S::CP; ++x)
-#pragma unroll
-                    for (int v = 0; v < S::TV; ++v) {
-                        const uint4v vf = RV::col_chunk(vc, 32 * kt, x, 32 * v);
-                        mma<T>(o[0][v], vf, p[0][x]);
-                        mma<T>(o[1][v], vf, p[1][x]);
-                    }
+                if (j0 < wend)
+                    Q.step(kr, vc, 32 * kt, c, some_hidden || j0 + 32 > wall, j0, limit, (uint32_t)(seen >> (32 * kt)));
             }
         }
         __syncthreads();  // the next item's loads write where this one's were read
+        Q.whole_sums();
+        if (item.parts > 1) {
+            const int64_t at = ((int64_t)item.slot * kAttnWaves + w) * 32 + (l & 31);
+            Q.leave(a.part + at * 2 * DVP, a.part + (int64_t)a.plan.slots() * kBlockRows * 2 * DVP + at * 4);
+            continue;
+        }
         if (i >= a.len_q)
             continue;
-        float inv[2];
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            sum[m] = __shfl_xor(sum[m], 32) + sum[m];
-            inv[m] = sum[m] != 0.0f ? 1.0f / sum[m] : 0.0f;
-        }
+        const float inv[2] = {Q.sum[0] != 0.0f ? 1.0f / Q.sum[0] : 0.0f, Q.sum[1] != 0.0f ? 1.0f / Q.sum[1] : 0.0f};
         const float lam = (float)((const T *)a.lam)[h];
-        const int64_t row = ((int64_t)b * a.len_q + i) * a.heads + h;
-        T *out = (T *)a.out + row * a.dim_v;
+        const int64_t row = (((int64_t)b * a.len_q + i) * a.heads + h) * a.dim_v + v0;
 #pragma unroll
         for (int v = 0; v < S::TV; ++v)
 #pragma unroll
@@ -295,23 +409,275 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 float x0[4], x1[4], y[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    x0[j] = o[0][v][4 * g + j] * inv[0];
-                    x1[j] = o[1][v][4 * g + j] * inv[1];
+                    x0[j] = Q.o[0][v][4 * g + j] * inv[0];
+                    x1[j] = Q.o[1][v][4 * g + j] * inv[1];
                     y[j] = x0[j] - lam * x1[j];
                 }
                 const int ch = 32 * v + 8 * g + 4 * (l >> 5);
-                store4<T, WIDE>(out, ch, a.dim_v, y);
+                store4<T, WIDE>((T *)a.out + row, ch, dim_v, y);
                 if (a.so) {
-                    store4<T, WIDE>((T *)a.so + row * a.dim_v, ch, a.dim_v, x0);
-                    store4<T, WIDE>((T *)a.so + a.so_map + row * a.dim_v, ch, a.dim_v, x1);
+                    store4<T, WIDE>((T *)a.so + row, ch, dim_v, x0);
+                    store4<T, WIDE>((T *)a.so + a.so_map + row, ch, dim_v, x1);
                 }
             }
-        if (a.lse && l < 32) {
+        if (a.lse && l < 32 && v0 == 0) {
             const int64_t at = ((int64_t)b * a.heads + h) * a.len_q + i;
+            a.lse[at] = lse_of<T>(Q.top[0], Q.sum[0]);
+            a.lse[a.lse_map + at] = lse_of<T>(Q.top[1], Q.sum[1]);
+        }
+    }
+}
+
+// Four channels of a row, wide where the arrays allow it.
+template <class T>
+__device__ __forceinline__ void put4(const AttnArgs &a, T *row, int c, int dim, const float (&x)[4])
+{
+    if (a.wide)
+        store4<T, true>(row, c, dim, x);
+    else
+        store4<T, false>(row, c, dim, x);
+}
+
+// A row's outputs from its parts, channels ch .. ch + 3 of both maps by one
+// thread: stats(p) are part p's tops and sums, sums(p, m) its unnormalised
+// channels.
+template <class T, class GetStats, class GetSums>
+__device__ __forceinline__ void join_row(const AttnArgs &a, int parts, const GetStats &stats, const GetSums &sums, int b,
+                                         int h, int i, int v0, int ch, int dim_v)
+{
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
+    float4v o[2] = {};
+    for (int p = 0; p < parts; ++p) {
+        const float4v st = stats(p);
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
-                a.lse[m * a.lse_map + at] =
-                    sum[m] != 0.0f ? (top[m] - kLift<T> + __builtin_amdgcn_logf(sum[m])) * kLn2 : -INFINITY;
+        for (int m = 0; m < 2; ++m)
+            top[m] = st[2 + m] != 0.0f ? __builtin_fmaxf(top[m], st[m]) : top[m];
+    }
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        const float4v st = stats(p);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const float4v x = sums(p, m);
+            // a part whose top is -inf and whose sum is not 0 has a NaN in it; one
+            // whose sum is 0 saw nothing, and its channels are 0
+            const float f = st[2 + m] == 0.0f ? 0.0f : (st[m] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st[m] - top[m]));
+            sum[m] += f * st[2 + m];
+            o[m] += f * x;
+        }
+    }
+    const float i0 = sum[0] != 0.0f ? 1.0f / sum[0] : 0.0f, i1 = sum[1] != 0.0f ? 1.0f / sum[1] : 0.0f;
+    const float lam = (float)((const T *)a.lam)[h];
+    const int64_t at = (((int64_t)b * a.len_q + i) * a.heads + h) * a.dim_v + v0;
+    float x0[4], x1[4], y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x0[j] = o[0][j] * i0;
+        x1[j] = o[1][j] * i1;
+        y[j] = x0[j] - lam * x1[j];
+    }
+    put4<T>(a, (T *)a.out + at, ch, dim_v, y);
+    if (a.so) {
+        put4<T>(a, (T *)a.so + at, ch, dim_v, x0);
+        put4<T>(a, (T *)a.so + a.so_map + at, ch, dim_v, x1);
+    }
+    if (a.lse && ch == 0 && v0 == 0) {
+        const int64_t r = ((int64_t)b * a.heads + h) * a.len_q + i;
+        a.lse[r] = lse_of<T>(top[0], sum[0]);
+        a.lse[a.lse_map + r] = lse_of<T>(top[1], sum[1]);
+    }
+}
+
+// Few queries over many keys (a decoding step).  The rows of a tile are the
+// queries of all heads of a key head, 32 at a time; the waves of a block walk over
+// their own keys, without waiting for each other, and join their sums in LDS.
+// What bounds it is reading the cache: every wave has two tiles of 32 keys under
+// way.
+template <class T, int DP, int DVP, bool WIDE>
+__global__ __launch_bounds__((64 * Sizes<T, DP, DVP>::kFewWaves)) void k_attn_few(AttnArgs a)
+{
+    using S = Sizes<T, DP, DVP>;
+    using RK = typename S::RK;
+    using RV = typename S::RV;
+    constexpr int KT = 32, W = S::kFewWaves;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int l = lane_id(), w = wave_id();
+    const float c = a.scale * kLog2e;
+    char *mine = lds + w * 2 * S::kFewTile;
+    float *stats = reinterpret_cast<float *>(lds + W * 2 * S::kFewTile);
+    const uint32_t items = a.plan.items();
+    for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
+        const Item item(a.plan, n);
+        const int b = item.b, hk = uniform(item.h / a.value_parts);
+        const int v0 = (item.h - hk * a.value_parts) * DVP, dim_v = min(a.dim_v - v0, DVP);
+        const int nq = q_len_of(a, b), nk = k_len_of(a, b);
+        const int r = item.tile * 32 + (l & 31), g = r / a.len_q, i = r - g * a.len_q, h = hk * a.group + g;
+        const bool in = g < a.group && i < nq;
+        const int limit = in ? (a.causal ? min(nk, i + nk - nq + 1) : nk) : 0;
+        int wend = limit, wall = limit;  // over the wave's rows: the most, the least
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            wend = max(wend, __shfl_xor(wend, s));
+            wall = min(wall, __shfl_xor(wall, s));
+        }
+        wend = uniform(wend);
+        wall = uniform(wall);
+        int from, to;
+        item.range(max(wend + KT - 1, 0) / KT, from, to);
+        {
+            const int per = (to - from + W - 1) / W;
+            from = min(from + w * per, to);
+            to = min(from + per, to);
+        }
+        if (a.dim < DP || a.dim_v % DVP) {  // the channels that no load writes
+            for (int e = l; e < 2 * S::kFewTile / 16; e += 64)
+                store16(mine + e * 16, uint4v{0, 0, 0, 0});
+        }
+        const T *kp = uniform_ptr((const T *)a.k + b * a.ks[0] + hk * a.ks[2] + (int64_t)from * KT * a.ks[1]);
+        const T *vp = uniform_ptr((const T *)a.v + b * a.vs[0] + hk * a.vs[2] + v0 + (int64_t)from * KT * a.vs[1]);
+        Queries<T, DP, DVP> Q;
+        KeyMask mask(a, b, nk);
+        auto issue = [&](int t) {
+            char *at = mine + (t & 1) * S::kFewTile;
+            mask.template fetch<KT>(t * KT);
+            load_rows<T, 2 * DP, 2, KT, 1, WIDE>(at, kp, a.ks[1], a.ks[3], nk - 1 - t * KT, a.dim);
+            load_rows<T, DVP, 1, KT, 1, WIDE>(at + RK::size(KT), vp, a.vs[1], 0, nk - 1 - t * KT, dim_v);
+            kp = uniform_ptr(kp + KT * a.ks[1]);
+            vp = uniform_ptr(vp + KT * a.vs[1]);
+        };
+        wave_fence();
+        if (from < to)
+            issue(from);
+        Q.template start<WIDE>(a, (const T *)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2], in);
+        for (int t = from; t < to; ++t) {
+            const int k0 = t * KT;
+            char *kb = mine + (t & 1) * S::kFewTile, *vb = kb + RK::size(KT);
+            wait_loads();
+            wave_fence();
+            const uint64_t seen = mask.template seen<KT>(k0);
+            if (t + 1 < to)
+                issue(t + 1);
+            const bool some_hidden = seen != kAllSeen<KT>;
+            if (some_hidden) {
+                clear_rows<T, 2 * DP, KT, 1>(kb, seen);
+                clear_rows<T, DVP, KT, 1>(vb, seen);
+                wave_fence();
+            }
+            Q.step(lds_address(kb) + RK::row_lane(), lds_address(vb) + RV::col_lane(), 0, c,
+                   some_hidden || k0 + KT > wall, k0, limit, (uint32_t)seen);
+            wave_fence();
+        }
+        Q.whole_sums();
+        // [row][map][DVP] of this wave where its tiles were
+        float *sums = reinterpret_cast<float *>(mine);
+        static_assert(32 * 2 * DVP * 4 <= 2 * S::kFewTile, "a wave's sums fit its tiles");
+        Q.leave(sums + (l & 31) * 2 * DVP, stats + (w * 32 + (l & 31)) * 4);
+        __syncthreads();
+        auto sums_of = [&](int p, int row, int at) {
+            return *reinterpret_cast<const float4v *>(reinterpret_cast<const float *>(lds + p * 2 * S::kFewTile) +
+                                                      row * 2 * DVP + at);
+        };
+        auto stats_of = [&](int p, int row) { return *reinterpret_cast<const float4v *>(stats + (p * 32 + row) * 4); };
+        const int rows = min(a.group * a.len_q - item.tile * 32, 32);
+        for (int e = threadIdx.x; e < rows * (DVP / 4); e += 64 * W) {
+            const int row = e / (DVP / 4), ch = e % (DVP / 4) * 4;
+            const int rr = item.tile * 32 + row, gg = rr / a.len_q, ii = rr - gg * a.len_q;
+            if (item.parts == 1) {
+                join_row<T>(
+                    a, W, [&](int p) { return stats_of(p, row); },
+                    [&](int p, int m) { return sums_of(p, row, m * DVP + ch); }, b, hk * a.group + gg, ii, v0, ch, dim_v);
+            } else {  // the block's sums, relative to the largest top of its waves
+                float4v st = {-INFINITY, -INFINITY, 0.0f, 0.0f};
+                const int64_t at = (int64_t)item.slot * 32 + row;
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    for (int p = 0; p < W; ++p)
+                        if (stats_of(p, row)[2 + m] != 0.0f)
+                            st[m] = __builtin_fmaxf(st[m], stats_of(p, row)[m]);
+                    float4v y = {};
+                    for (int p = 0; p < W; ++p) {
+                        const float4v sp = stats_of(p, row);
+                        const float f =
+                            sp[2 + m] == 0.0f ? 0.0f : (sp[m] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sp[m] - st[m]));
+                        st[2 + m] += f * sp[2 + m];
+                        y += f * sums_of(p, row, m * DVP + ch);
+                    }
+                    *reinterpret_cast<float4v *>(a.part + at * 2 * DVP + m * DVP + ch) = y;
+                }
+                if (ch == 0)
+                    *reinterpret_cast<float4v *>(a.part + (int64_t)a.plan.slots() * 32 * 2 * DVP + at * 4) = st;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins the parts of a launch's last units: a thread per four channels of a row;
+// FEW (up to 256 parts of few rows): a block per row, eight threads per four
+// channels that take every eighth part each.
+template <class T, int DVP, bool FEW>
+__global__ __launch_bounds__(kAttnThreads) void k_attn_join(AttnArgs a)
+{
+    constexpr int ROWS = FEW ? 32 : kBlockRows, QUADS = DVP / 4;
+    const uint32_t rows = (a.plan.units - a.plan.full) * ROWS;
+    const float *stats = a.part + (int64_t)a.plan.slots() * ROWS * 2 * DVP;
+    auto stats_of = [&](int64_t at) { return *reinterpret_cast<const float4v *>(stats + at * 4); };
+    auto sums_of = [&](int64_t at, int m, int ch) {
+        return *reinterpret_cast<const float4v *>(a.part + at * 2 * DVP + m * DVP + ch);
+    };
+    if constexpr (FEW) {
+        constexpr int G = kAttnThreads / QUADS;
+        __shared__ float4v gs[G], go[G][2][QUADS];
+        const int g = threadIdx.x / QUADS, ch = threadIdx.x % QUADS * 4;
+        for (uint32_t x = blockIdx.x; x < rows; x += gridDim.x) {
+            const uint32_t u = x / ROWS, row = x % ROWS, unit = a.plan.full + u;
+            const uint32_t bh = a.plan.bh_of(unit), tile = a.plan.tile_of(unit);
+            const int b = bh / a.plan.heads, hv = bh - b * a.plan.heads, hk = hv / a.value_parts;
+            const int v0 = (hv - hk * a.value_parts) * DVP;
+            const int r = tile * 32 + row, q = r / a.len_q, i = r - q * a.len_q, h = hk * a.group + q;
+            if (q >= a.group)  // the same in every thread of the block
+                continue;
+            auto at = [&](int p) { return ((int64_t)u * a.plan.parts + p) * ROWS + row; };
+            float4v st = {-INFINITY, -INFINITY, 0.0f, 0.0f}, o[2] = {};
+            for (int p = g; p < (int)a.plan.parts; p += G) {
+                const float4v sp = stats_of(at(p)), x0 = sums_of(at(p), 0, ch), x1 = sums_of(at(p), 1, ch);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    if (sp[2 + m] == 0.0f)  // saw nothing
+                        continue;
+                    const float to = __builtin_fmaxf(st[m], sp[m]);
+                    const float f0 = st[m] == -INFINITY ? (st[2 + m] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(st[m] - to);
+                    const float f1 = sp[m] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sp[m] - to);
+                    o[m] = o[m] * f0 + (m ? x1 : x0) * f1;
+                    st[2 + m] = st[2 + m] * f0 + sp[2 + m] * f1;
+                    st[m] = to;
+                }
+            }
+            __syncthreads();
+            if (ch == 0)
+                gs[g] = st;
+            go[g][0][ch / 4] = o[0];
+            go[g][1][ch / 4] = o[1];
+            __syncthreads();
+            if (g == 0)
+                join_row<T>(
+                    a, G, [&](int p) { return gs[p]; }, [&](int p, int m) { return go[p][m][ch / 4]; }, b, h, i, v0, ch,
+                    min(a.dim_v - v0, DVP));
+        }
+    } else {
+        for (uint32_t e = blockIdx.x * kAttnThreads + threadIdx.x; e < rows * QUADS; e += gridDim.x * kAttnThreads) {
+            const uint32_t x = e / QUADS, ch = e % QUADS * 4;
+            const uint32_t u = x / ROWS, row = x % ROWS, unit = a.plan.full + u;
+            const uint32_t bh = a.plan.bh_of(unit), tile = a.plan.tile_of(unit);
+            const int b = bh / a.plan.heads, hv = bh - b * a.plan.heads, h = hv / a.value_parts;
+            const int v0 = (hv - h * a.value_parts) * DVP;
+            const int i = (a.plan.tiles - 1 - tile) * kBlockRows + row;
+            if (i >= a.len_q)
+                continue;
+            auto at = [&](int p) { return ((int64_t)u * a.plan.parts + p) * ROWS + row; };
+            join_row<T>(
+                a, a.plan.parts, [&](int p) { return stats_of(at(p)); },
+                [&](int p, int m) { return sums_of(at(p), m, ch); }, b, h, i, v0, ch, min(a.dim_v - v0, DVP));
         }
     }
 }
@@ -332,16 +698,16 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
     constexpr int KT = S::kKeys;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int l = lane_id(), w = wave_id();
-    const uint32_t tiles = (a.len_q + kBlockRows - 1) / kBlockRows, total = tiles * a.heads * a.batch;
     const float c = a.scale * kLog2e;
     if (a.dim < DP || a.dim_v < DVP) {
         for (int e = threadIdx.x; e < 2 * S::kKeyTile / 16; e += kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
-    for (uint32_t n = blockIdx.x; n < total; n += gridDim.x) {
-        const Item item(n, total, tiles, a.heads);
-        const int q0 = ((int)tiles - 1 - item.tile) * kBlockRows;  // causal: the longest first
+    const uint32_t items = a.plan.items();
+    for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
+        const Item item(a.plan, n);
+        const int q0 = ((int)a.plan.tiles - 1 - item.tile) * kBlockRows;
         const int b = item.b, h = item.h, hk = uniform(h / a.group);
         const int nq = q_len_of(a, b), nk = k_len_of(a, b);
         const int i = q0 + 32 * w + (l & 31);
@@ -351,28 +717,24 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         const int end = q0 < nq ? (a.causal ? min(nk, last + nk - nq + 1) : nk) : 0;
         const int wend = q0 + 32 * w < nq ? (a.causal ? min(nk, wlast + nk - nq + 1) : nk) : 0;
         const int wall = q0 + 32 * w + 31 < nq ? (a.causal ? min(nk, q0 + 32 * w + nk - nq + 1) : nk) : 0;
-        const T *kp = uniform_ptr((const T *)a.k + b * a.ks[0] + hk * a.ks[2]);
-        const T *vp = uniform_ptr((const T *)a.v + b * a.vs[0] + hk * a.vs[2]);
+        int from, to;
+        item.range(max(end + KT - 1, 0) / KT, from, to);
+        const T *kp = uniform_ptr((const T *)a.k + b * a.ks[0] + hk * a.ks[2] + (int64_t)from * KT * a.ks[1]);
+        const T *vp = uniform_ptr((const T *)a.v + b * a.vs[0] + hk * a.vs[2] + (int64_t)from * KT * a.vs[1]);
         const int64_t row = ((int64_t)b * a.len_q + i) * a.heads + h,
                       at = ((int64_t)b * a.heads + h) * a.len_q + i;
 
-        auto issue = [&](int k0, int buf) {  // tiles in order
-            char *to = lds + buf * S::kKeyTile;
-            load_rows<T, 2 * DP, 2, KT, kAttnWaves, WIDE>(to, kp, a.ks[1], a.ks[3], nk - 1 - k0, a.dim);
-            load_rows<T, DVP, 1, KT, kAttnWaves, WIDE>(to + RK::size(KT), vp, a.vs[1], 0, nk - 1 - k0, a.dim_v);
+        KeyMask mask(a, b, nk);
+        auto issue = [&](int t) {  // tiles in order
+            char *at = lds + (t & 1) * S::kKeyTile;
+            mask.template fetch<KT>(t * KT);
+            load_rows<T, 2 * DP, 2, KT, kAttnWaves, WIDE>(at, kp, a.ks[1], a.ks[3], nk - 1 - t * KT, a.dim);
+            load_rows<T, DVP, 1, KT, kAttnWaves, WIDE>(at + RK::size(KT), vp, a.vs[1], 0, nk - 1 - t * KT, a.dim_v);
             kp = uniform_ptr(kp + KT * a.ks[1]);
             vp = uniform_ptr(vp + KT * a.vs[1]);
         };
-        const int trips = (end + KT - 1) / KT;
-        // the mask's byte of this lane's key of the next tile, compared only when
-        // that tile is there: a comparison here would wait for all the loads
-        const uint8_t *mask = a.key_mask ? a.key_mask + (int64_t)b * a.len_k : nullptr;
-        auto mask_byte = [&](int j) { return mask && l < KT && j < nk ? (int)mask[j] : 1; };
-        int next = 1;
-        if (trips > 0) {
-            next = mask_byte(l);
-            issue(0, 0);
-        }
+        if (from < to)
+            issue(from);
         uint4v q[2][S::CK], g[S::CV];
         const T *qrow = (const T *)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
 #pragma unroll
@@ -397,7 +759,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 const float x = a.lse[m * a.lse_map + at];
                 lse[m] = x == -INFINITY ? INFINITY : x * kLog2e;
             }
-            if (l < 32 && i < a.len_q) {
+            if (l < 32 && i < a.len_q && item.part == 0) {
                 a.stats[m * a.lse_map + at] = lse[m];
                 a.stats[(2 + m) * a.lse_map + at] = D[m];
             }
@@ -405,17 +767,15 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         f32x16 acc[2][S::TK] = {};
         float dlam = 0.0f;
         Range range;
-        for (int t = 0; t < trips; ++t) {
-            const int k0 = t * KT, buf = t & 1;
-            char *kb = lds + buf * S::kKeyTile, *vb = kb + RK::size(KT);
+        for (int t = from; t < to; ++t) {
+            const int k0 = t * KT;
+            char *kb = lds + (t & 1) * S::kKeyTile, *vb = kb + RK::size(KT);
             wait_loads();
             __syncthreads();
-            const uint64_t seen = __ballot(next != 0 && l < KT && k0 + l < nk);
-            if (t + 1 < trips) {
-                next = mask_byte(k0 + KT + l);
-                issue(k0 + KT, buf ^ 1);
-            }
-            const bool some_hidden = seen != (KT == 64 ? ~0ull : (1ull << KT) - 1);
+            const uint64_t seen = mask.template seen<KT>(k0);
+            if (t + 1 < to)
+                issue(t + 1);
+            const bool some_hidden = seen != kAllSeen<KT>;
             if (some_hidden) {
                 clear_rows<T, 2 * DP, KT, kAttnWaves>(kb, seen);
                 clear_rows<T, DVP, KT, kAttnWaves>(vb, seen);
@@ -430,9 +790,9 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                     break;
                 f32x16 s[2] = {}, dp = {};
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int x = 0; x < S::CK; ++x)
 #pragma unroll
-                    for (int x = 0; x < S::CK; ++x)
+                    for (int m = 0; m < 2; ++m)
                         mma<T>(s[m], RK::row_chunk(kr, 32 * kt, m * S::CK + x), q[m][x]);
 #pragma unroll
                 for (int x = 0; x < S::CV; ++x)
@@ -474,9 +834,14 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             }
         }
         __syncthreads();
+        dlam = lanes_sum<64>(dlam);
+        if (l == 0)
+            a.dlam[(item.parts > 1 ? a.plan.full + item.slot : a.plan.unit(b * a.heads + h, item.tile)) * (int64_t)kAttnWaves + w] =
+                dlam;
         if (i >= a.len_q)
             continue;
         const float lam = (float)((const T *)a.lam)[h];
+        float *part = a.part + (((int64_t)item.slot * kAttnWaves + w) * 32 + (l & 31)) * 2 * DP;
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             const float f = (m ? -lam * a.scale : a.scale) * range.down();
@@ -486,12 +851,13 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 for (int y = 0; y < 4; ++y) {
                     const float x[4] = {acc[m][v][4 * y] * f, acc[m][v][4 * y + 1] * f, acc[m][v][4 * y + 2] * f,
                                         acc[m][v][4 * y + 3] * f};
-                    store4<T, WIDE>((T *)a.gq + (row * 2 + m) * a.dim, 32 * v + 8 * y + 4 * (l >> 5), a.dim, x);
+                    const int ch = 32 * v + 8 * y + 4 * (l >> 5);
+                    if (item.parts > 1)
+                        store4<float, true>(part + m * DP, ch, DP, x);
+                    else
+                        store4<T, WIDE>((T *)a.gq + (row * 2 + m) * a.dim, ch, a.dim, x);
                 }
         }
-        dlam += __shfl_xor(dlam, 32);
-        if (l < 32)
-            a.dlam[at] = dlam;
     }
 }
 
@@ -499,11 +865,11 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
 // backward: keys and values
 // ---------------------------------------------------------------------------
 
-// dk and dv of 128 keys, over the queries of every head of the key head; or of
-// one head (a.parts: 32-bit sums per head, added up by k_attn_parts), where the
-// key heads alone are too few blocks.  Scores are formed with queries as rows
-// here: a lane holds one key.
-template <class T, int DP, int DVP, bool WIDE>
+// dk and dv of 128 keys, over the queries of every head of the key head.  Scores
+// are formed with queries as rows here: a lane holds one key.  WHAT: both (3), or
+// dv (1) and dk (2) by themselves: head sizes over 64 have no registers for the
+// sums of both, and form the scores twice.
+template <class T, int DP, int DVP, bool WIDE, int WHAT>
 __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) void k_attn_dkv(AttnArgs a)
 {
     using S = Sizes<T, DP, DVP>;
@@ -512,19 +878,17 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
     constexpr int QT = S::kQueries;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int l = lane_id(), w = wave_id();
-    const int heads = a.parts ? a.heads : a.kv_heads;
-    const uint32_t tiles = (a.len_k + kBlockRows - 1) / kBlockRows, total = tiles * heads * a.batch;
     const float c = a.scale * kLog2e;
     if (a.dim < DP || a.dim_v < DVP) {
         for (int e = threadIdx.x; e < (2 * S::kQueryTile + S::kValues) / 16; e += kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
-    for (uint32_t n = blockIdx.x; n < total; n += gridDim.x) {
-        const Item item(n, total, tiles, heads);
+    const uint32_t items = a.key_plan.items();
+    for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
+        const Item item(a.key_plan, n);
         const int k0 = item.tile * kBlockRows;  // causal: the longest first
-        const int b = item.b, hx = item.h, hk = a.parts ? uniform(hx / a.group) : hx;
-        const int h0 = a.parts ? hx : hx * a.group, h1 = a.parts ? hx + 1 : h0 + a.group;
+        const int b = item.b, hk = item.h, h0 = hk * a.group, h1 = h0 + a.group;
         const int nq = q_len_of(a, b), nk = k_len_of(a, b);
         const int j = k0 + 32 * w + (l & 31);  // this lane's key
         const bool seen = key_seen(a, b, nk, j);
@@ -549,7 +913,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         // for them and reads them again and again, through the caches.)
         char *vrows = lds + 2 * S::kQueryTile + RV::size(32) * w;
         const T *vrow = (const T *)a.v + b * a.vs[0] + j * a.vs[1] + hk * a.vs[2];
-        if constexpr (S::kKeepValues)
+        if constexpr (S::kKeepValues && (WHAT & 2))
             for (int s = 0; s < S::CV; ++s)
                 store16(vrows + RV::at(l & 31, 2 * s + (l >> 5)), memory_chunk<T, WIDE>(vrow, s, a.dim_v, seen));
         f32x16 gk[2][S::TK] = {}, gv[S::TV] = {};
@@ -567,14 +931,18 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
 
         // tiles of all heads in one run, loads a tile ahead
         const int per = nk > k0 && nq > first ? (nq - first + QT - 1) / QT : 0;
-        const int trips = per * (h1 - h0);
-        int nh = h0, ni = first;  // head and first query of the next tile to load
+        int t0, t1;
+        item.range(per * a.group, t0, t1);
+        // head and first query of the next tile to load
+        int nh = h0 + (per ? t0 / per : 0), ni = first + (per ? t0 % per : 0) * QT;
+        nh = uniform(nh);
+        ni = uniform(ni);
         const T *qp, *gp;
         const float *sp;
         auto head = [&](int h) {
-            qp = uniform_ptr((const T *)a.q + b * a.qs[0] + first * a.qs[1] + h * a.qs[2]);
-            gp = uniform_ptr((const T *)a.dout + b * a.dos[0] + first * a.dos[1] + h * a.dos[2]);
-            sp = uniform_ptr(a.stats + ((int64_t)b * a.heads + h) * a.len_q + first);
+            qp = uniform_ptr((const T *)a.q + b * a.qs[0] + ni * a.qs[1] + h * a.qs[2]);
+            gp = uniform_ptr((const T *)a.dout + b * a.dos[0] + ni * a.dos[1] + h * a.dos[2]);
+            sp = uniform_ptr(a.stats + ((int64_t)b * a.heads + h) * a.len_q + ni);
         };
         auto issue = [&](int buf) {
             char *to = lds + buf * S::kQueryTile;
@@ -595,13 +963,13 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 head(nh);
             }
         };
-        if (trips > 0) {
-            head(h0);
-            issue(0);
+        int i0 = ni - QT, ch = nh;  // of the tile at hand
+        if (t0 < t1) {
+            head(nh);
+            issue(t0 & 1);
         }
-        int i0 = first - QT, ch = h0;  // of the tile at hand
-        float lam = -uniform_float((float)((const T *)a.lam)[h0]);
-        for (int t = 0; t < trips; ++t) {
+        float lam = -uniform_float((float)((const T *)a.lam)[min(ch, a.heads - 1)]);
+        for (int t = t0; t < t1; ++t) {
             const int buf = t & 1;
             char *qb = lds + buf * S::kQueryTile, *gb = qb + RK::size(QT);
             const float *st = reinterpret_cast<const float *>(gb + RV::size(QT));
@@ -612,7 +980,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             }
             wait_loads();
             __syncthreads();
-            if (t + 1 < trips)
+            if (t + 1 < t1)
                 issue(buf ^ 1);
             const bool tail = i0 + QT > nq;
             if (tail) {  // rows past the sequence
@@ -631,12 +999,12 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                         s[0][r] = s[1][r] = lifted;
                 }
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int x = 0; x < S::CK; ++x)
 #pragma unroll
-                    for (int x = 0; x < S::CK; ++x)
+                    for (int m = 0; m < 2; ++m)
                         mma<T>(s[m], RK::row_chunk(qr, 0, m * S::CK + x), kf[m][x]);
 #pragma unroll
-                for (int x = 0; x < S::CV; ++x)
+                for (int x = 0; x < ((WHAT & 2) ? S::CV : 0); ++x)
                     if constexpr (S::kKeepValues)
                         mma<T>(dp, RV::row_chunk(gr, 0, x), RV::row_chunk(vr, 0, x));
                     else
@@ -671,13 +1039,14 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                             s[1][r] = p1 * (dp[r] - d1[y]);
                         }
                     }
-                    wf[x] = operand<T>(wt, x);
-                    if constexpr (!std::is_same<T, f16>::value) {
+                    if constexpr (WHAT & 1)
+                        wf[x] = operand<T>(wt, x);
+                    if constexpr (!std::is_same<T, f16>::value && (WHAT & 2)) {
                         ds[0][x] = operand<T>(s[0], x);
                         ds[1][x] = operand<T>(s[1], x);
                     }
                 }
-                if constexpr (std::is_same<T, f16>::value) {
+                if constexpr (std::is_same<T, f16>::value && (WHAT & 2)) {
                     range.fit(s, [&](float f) {
 #pragma unroll
                         for (int m = 0; m < 2; ++m)
@@ -694,10 +1063,10 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
 #pragma unroll
                 for (int x = 0; x < S::CP; ++x) {
 #pragma unroll
-                    for (int v = 0; v < S::TV; ++v)
+                    for (int v = 0; v < ((WHAT & 1) ? S::TV : 0); ++v)
                         mma<T>(gv[v], RV::col_chunk(gc, 0, x, 32 * v), wf[x]);
 #pragma unroll
-                    for (int m = 0; m < 2; ++m)
+                    for (int m = 0; m < ((WHAT & 2) ? 2 : 0); ++m)
 #pragma unroll
                         for (int v = 0; v < S::TK; ++v)
                             mma<T>(gk[m][v], RK::col_chunk(qc, 0, x, m * DP + 32 * v), ds[m][x]);
@@ -707,47 +1076,51 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         __syncthreads();
         if (j >= a.len_k)
             continue;
-        const int64_t row = ((int64_t)b * a.len_k + j) * heads + hx;
-        auto put = [&](auto *to, const f32x16 &x, int v, int dim, float f) {
+        const int64_t row = ((int64_t)b * a.len_k + j) * a.kv_heads + hk;
+        float *part = a.key_part + (((int64_t)item.slot * kAttnWaves + w) * 32 + (l & 31)) * (2 * DP + DVP);
+        auto put = [&](T *to, float *to_part, const f32x16 &x, int v, int dim, float f) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const float y[4] = {x[4 * g] * f, x[4 * g + 1] * f, x[4 * g + 2] * f, x[4 * g + 3] * f};
-                store4<std::remove_reference_t<decltype(*to)>, WIDE>(to, 32 * v + 8 * g + 4 * (l >> 5), dim, y);
+                const int at = 32 * v + 8 * g + 4 * (l >> 5);
+                if (item.parts > 1)
+                    store4<float, true>(to_part, at, 1 << 20, y);
+                else
+                    store4<T, WIDE>(to, at, dim, y);
             }
         };
         const float fv = __builtin_amdgcn_exp2f(-lift), fk = a.scale * range.down() * fv;
+        if constexpr (WHAT & 2) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int v = 0; v < S::TK; ++v) {
-                if (a.parts)
-                    put(a.parts + (row * 2 + m) * a.dim, gk[m][v], v, a.dim, fk);
-                else
-                    put((T *)a.gk + (row * 2 + m) * a.dim, gk[m][v], v, a.dim, fk);
-            }
+                for (int v = 0; v < S::TK; ++v)
+                    put((T *)a.gk + (row * 2 + m) * a.dim, part + m * DP, gk[m][v], v, a.dim, fk);
+        }
+        if constexpr (WHAT & 1) {
 #pragma unroll
-        for (int v = 0; v < S::TV; ++v) {
-            if (a.parts)
-                put(a.parts + a.parts_v + row * a.dim_v, gv[v], v, a.dim_v, fv);
-            else
-                put((T *)a.gv + row * a.dim_v, gv[v], v, a.dim_v, fv);
+            for (int v = 0; v < S::TV; ++v)
+                put((T *)a.gv + row * a.dim_v, part + 2 * DP, gv[v], v, a.dim_v, fv);
         }
     }
 }
 
-// Sums of the heads' parts of a key head, in order, and of grad_lambda's rows.
-// Blocks up to `heads` take one lambda each, the others the parts.
-template <class T>
+// What is left after both passes, in a fixed order: grad_lambda, a block per
+// head; and the sums of the parts of both passes' last units.
+template <class T, int DP, int DVP>
 __global__ __launch_bounds__(kAttnThreads) void k_attn_finish(AttnArgs a)
 {
     if ((int)blockIdx.x < a.heads) {
         __shared__ float s[kAttnWaves];
-        const int h = blockIdx.x;
+        const uint32_t h = blockIdx.x, tiles = a.plan.tiles;
         float y = 0.0f;
-        for (int b = 0; b < a.batch; ++b) {
-            const float *x = a.dlam + ((int64_t)b * a.heads + h) * a.len_q;
-            for (int i = threadIdx.x; i < a.len_q; i += kAttnThreads)
-                y += x[i];
+        for (uint32_t e = threadIdx.x; e < (uint32_t)a.batch * tiles; e += kAttnThreads) {
+            const uint32_t b = e / tiles, unit = a.plan.unit(b * a.heads + h, e - b * tiles);
+            const bool one = unit < a.plan.full;
+            const uint32_t from = one ? unit : a.plan.full + (unit - a.plan.full) * a.plan.parts;
+            const uint32_t n = (one ? 1 : a.plan.parts) * kAttnWaves;
+            for (uint32_t x = 0; x < n; ++x)
+                y += a.dlam[(int64_t)from * kAttnWaves + x];
         }
         y = lanes_sum<64>(y);
         if (lane_id() == 0)
@@ -757,21 +1130,34 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_finish(AttnArgs a)
             ((T *)a.glam)[h] = (T)(-(((s[0] + s[1]) + s[2]) + s[3]));
         return;
     }
-    const int64_t rows = (int64_t)a.batch * a.len_k * a.kv_heads;
-    const int wk = 2 * a.dim, wv = a.dim_v;
-    const int64_t nk = rows * wk, total = nk + rows * wv;
-    for (int64_t e = (int64_t)(blockIdx.x - a.heads) * kAttnThreads + threadIdx.x; e < total;
-         e += (int64_t)(gridDim.x - a.heads) * kAttnThreads) {
-        const bool key = e < nk;
-        const int64_t x = key ? e : e - nk;
-        const int width = key ? wk : wv;
-        const int64_t row = x / width;
-        const int ch = (int)(x - row * width);
-        const float *p = a.parts + (key ? 0 : a.parts_v) + row * a.group * width + ch;
-        float y = 0.0f;
-        for (int g = 0; g < a.group; ++g)
-            y += p[(int64_t)g * width];
-        ((T *)(key ? a.gk : a.gv))[x] = (T)y;
+    constexpr int WQ = 2 * DP, WK = 2 * DP + DVP;
+    const uint32_t nq = a.plan.parts > 1 ? (a.plan.units - a.plan.full) * kBlockRows * (WQ / 4) : 0;
+    const uint32_t nk = a.key_plan.parts > 1 ? (a.key_plan.units - a.key_plan.full) * kBlockRows * (WK / 4) : 0;
+    for (uint32_t e = (blockIdx.x - a.heads) * kAttnThreads + threadIdx.x; e < nq + nk;
+         e += (gridDim.x - a.heads) * kAttnThreads) {
+        const bool key = e >= nq;
+        const Plan &p = key ? a.key_plan : a.plan;
+        const int width = key ? WK : WQ;
+        const uint32_t x = key ? e - nq : e;
+        const uint32_t at = key ? x / (WK / 4) : x / (WQ / 4), ch = (x - at * (width / 4)) * 4;
+        const uint32_t u = at / kBlockRows, row = at % kBlockRows, unit = p.full + u;
+        const uint32_t bh = p.bh_of(unit), tile = p.tile_of(unit), b = bh / p.heads, h = bh - b * p.heads;
+        const int len = key ? a.len_k : a.len_q, i = (key ? tile : p.tiles - 1 - tile) * kBlockRows + row;
+        const bool value = ch >= 2 * DP;
+        const uint32_t m = value ? 0 : ch / DP, cc = value ? ch - 2 * DP : ch % DP;
+        if (i >= len || (int)cc >= (value ? a.dim_v : a.dim))
+            continue;
+        const float *from = (key ? a.key_part : a.part) + ((int64_t)u * p.parts * kBlockRows + row) * width + ch;
+        float4v s = {};
+#pragma unroll 4
+        for (uint32_t q = 0; q < p.parts; ++q)
+            s += *reinterpret_cast<const float4v *>(from + (int64_t)q * kBlockRows * width);
+        const float y[4] = {s[0], s[1], s[2], s[3]};
+        const int64_t out = ((int64_t)b * len + i) * p.heads + h;
+        if (value)
+            put4<T>(a, (T *)a.gv + out * a.dim_v, cc, a.dim_v, y);
+        else
+            put4<T>(a, (T *)(key ? a.gk : a.gq) + (out * 2 + m) * a.dim, cc, a.dim, y);
     }
 }
 
@@ -783,7 +1169,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_finish(AttnArgs a)
 inline unsigned item_blocks(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 23); }
 
 template <class K>
-hipError_t launch_lds(K kernel, unsigned blocks, int lds, const AttnArgs &a, hipStream_t s)
+hipError_t launch_lds(K kernel, unsigned blocks, unsigned threads, int lds, const AttnArgs &a, hipStream_t s)
 {
     if (lds > (64 << 10)) {
         const hipError_t e =
@@ -791,16 +1177,33 @@ hipError_t launch_lds(K kernel, unsigned blocks, int lds, const AttnArgs &a, hip
         if (e != hipSuccess)
             return e;
     }
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kAttnThreads), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, s, a);
     return hipGetLastError();
 }
 
+inline unsigned sum_blocks(int64_t sums)
+{
+    return (unsigned)std::min<int64_t>((sums + kAttnThreads - 1) / kAttnThreads, 8192);
+}
+
 template <class T, int DP, int DVP, bool WIDE>
-hipError_t fwd_class(const AttnArgs &a, hipStream_t s)
+hipError_t fwd_class(const AttnArgs &a, bool few, hipStream_t s)
 {
     using S = Sizes<T, DP, DVP>;
-    const int64_t items = (int64_t)((a.len_q + kBlockRows - 1) / kBlockRows) * a.heads * a.batch;
-    return launch_lds(k_attn_fwd<T, DP, DVP, WIDE>, item_blocks(items), 2 * S::kKeyTile, a, s);
+    hipError_t e;
+    if (few)
+        e = launch_lds(k_attn_few<T, DP, DVP, WIDE>, item_blocks(a.plan.items()), 64 * S::kFewWaves,
+                       S::kFewWaves * (2 * S::kFewTile + 32 * 16), a, s);
+    else
+        e = launch_lds(k_attn_fwd<T, DP, DVP, WIDE>, item_blocks(a.plan.items()), kAttnThreads, 2 * S::kKeyTile, a, s);
+    if (e != hipSuccess || a.plan.parts == 1)
+        return e;
+    const unsigned blocks = sum_blocks((int64_t)(a.plan.units - a.plan.full) * kBlockRows * DVP / 4);
+    if (few)
+        hipLaunchKernelGGL((k_attn_join<T, DVP, true>), dim3((a.plan.units - a.plan.full) * 32), dim3(kAttnThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_attn_join<T, DVP, false>), dim3(blocks), dim3(kAttnThreads), 0, s, a);
+    return hipGetLastError();
 }
 
 template <class T, int DP, int DVP, bool WIDE>
@@ -808,47 +1211,60 @@ hipError_t bwd_class(const AttnArgs &a, hipStream_t s)
 {
     using S = Sizes<T, DP, DVP>;
     hipError_t e = hipSuccess;
-    const int64_t rows = (int64_t)((a.len_q + kBlockRows - 1) / kBlockRows) * a.heads * a.batch;
+    const unsigned rows = item_blocks(a.plan.items()), keys = item_blocks(a.key_plan.items());
     if (rows)
-        e = launch_lds(k_attn_dq<T, DP, DVP, WIDE>, item_blocks(rows), 2 * S::kKeyTile, a, s);
-    const int64_t keys = (int64_t)((a.len_k + kBlockRows - 1) / kBlockRows) * (a.parts ? a.heads : a.kv_heads) * a.batch;
-    if (e == hipSuccess && keys)
-        e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE>, item_blocks(keys), 2 * S::kQueryTile + S::kValues, a, s);
-    return e;
+        e = launch_lds(k_attn_dq<T, DP, DVP, WIDE>, rows, kAttnThreads, 2 * S::kKeyTile, a, s);
+    if (e != hipSuccess)
+        return e;
+    constexpr int lds = 2 * S::kQueryTile + S::kValues;
+    if constexpr (DP <= 64) {
+        if (keys)
+            e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE, 3>, keys, kAttnThreads, lds, a, s);
+    } else if (keys) {
+        e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE, 1>, keys, kAttnThreads, lds, a, s);
+        if (e == hipSuccess)
+            e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE, 2>, keys, kAttnThreads, lds, a, s);
+    }
+    if (e != hipSuccess)
+        return e;
+    int64_t sums = 0;
+    if (a.plan.parts > 1)
+        sums += (int64_t)(a.plan.units - a.plan.full) * kBlockRows * 2 * DP;
+    if (a.key_plan.parts > 1)
+        sums += (int64_t)(a.key_plan.units - a.key_plan.full) * kBlockRows * (2 * DP + DVP);
+    hipLaunchKernelGGL((k_attn_finish<T, DP, DVP>), dim3(a.heads + sum_blocks(sums / 4)), dim3(kAttnThreads), 0, s, a);
+    return hipGetLastError();
 }
 
-// The class is the smallest that holds both head sizes.
-template <class F>
-hipError_t with_class(const AttnArgs &a, const F &f)
+// by the class of head sizes that attn_class names
+template <class T, bool WIDE>
+hipError_t fwd_wide(const AttnArgs &a, bool few, hipStream_t s)
 {
-    using std::integral_constant;
-    if (a.dim <= 32 && a.dim_v <= 64)
-        return f(integral_constant<int, 32>(), integral_constant<int, 64>());
-    if (a.dim <= 64 && a.dim_v <= 128)
-        return f(integral_constant<int, 64>(), integral_constant<int, 128>());
-    return f(integral_constant<int, 128>(), integral_constant<int, 256>());
+    switch (attn_class(a.dim, a.dim_v)) {
+    case 0: return fwd_class<T, 32, 64, WIDE>(a, few, s);
+    case 1: return fwd_class<T, 64, 128, WIDE>(a, few, s);
+    default: return fwd_class<T, 128, 128, WIDE>(a, few, s);
+    }
+}
+template <class T, bool WIDE>
+hipError_t bwd_wide(const AttnArgs &a, hipStream_t s)
+{
+    switch (attn_class(a.dim, a.dim_v)) {
+    case 0: return bwd_class<T, 32, 64, WIDE>(a, s);
+    case 1: return bwd_class<T, 64, 128, WIDE>(a, s);
+    default: return bwd_class<T, 128, 256, WIDE>(a, s);
+    }
 }
 
 template <class T>
-hipError_t attn_fwd(const AttnArgs &a, bool wide, hipStream_t s)
+hipError_t attn_fwd(const AttnArgs &a, bool wide, bool few, hipStream_t s)
 {
-    return with_class(a, [&](auto d, auto dv) {
-        return wide ? fwd_class<T, d, dv, true>(a, s) : fwd_class<T, d, dv, false>(a, s);
-    });
+    return wide ? fwd_wide<T, true>(a, few, s) : fwd_wide<T, false>(a, few, s);
 }
-
 template <class T>
 hipError_t attn_bwd(const AttnArgs &a, bool wide, hipStream_t s)
 {
-    const hipError_t e = with_class(a, [&](auto d, auto dv) {
-        return wide ? bwd_class<T, d, dv, true>(a, s) : bwd_class<T, d, dv, false>(a, s);
-    });
-    if (e != hipSuccess)
-        return e;
-    const int64_t sums = a.parts ? (int64_t)a.batch * a.len_k * a.kv_heads * (2 * a.dim + a.dim_v) : 0;
-    const unsigned blocks = (unsigned)std::min<int64_t>((sums + kAttnThreads - 1) / kAttnThreads, 4096);
-    hipLaunchKernelGGL(k_attn_finish<T>, dim3(a.heads + blocks), dim3(kAttnThreads), 0, s, a);
-    return hipGetLastError();
+    return wide ? bwd_wide<T, true>(a, s) : bwd_wide<T, false>(a, s);
 }
 
 }  // namespace

@@ -92,33 +92,38 @@ __device__ __forceinline__ uint4v operand(const f32x16 &p, int s)
 }
 
 // Rows of NC channels in LDS.  The loads that write LDS directly fill 1024
-// bytes in order, so rows cannot be padded one by one: the 16-byte pieces of a
-// row are permuted by an exclusive or with 0, 2, 4 or 6, which depends on the
-// row, and 128 bytes are left free after every four rows of 256 bytes or more.
-// Eight lanes that read one piece of eight rows, and sixteen that read two
-// pieces of four rows, then meet every bank once; and the addresses of a
-// lane's pieces differ by constants in all but two bits, which keeps them in few
-// registers.
+// bytes in order, so rows cannot be padded: the 16-byte pieces of a row are
+// permuted by an exclusive or with a number that depends on the row.  LDS serves
+// 256 bytes of different banks at a time.  The numbers are such that
+//   - sixteen lanes that read one piece each of sixteen rows (row_chunk),
+//   - 32 that read four pieces of four rows (the transposing read), and
+//   - fp32: 64 that read eight pieces of two rows four apart (col_chunk)
+// meet every bank once: 4.1, 2.3 and 1 cycles (measured: 8.1 and 4.1 with four
+// numbers and 128 bytes left free after every fourth row of 256).
 template <class T, int NC>
 struct Rows {
     static constexpr int kBytes = NC * sizeof(T);  // per row
     static constexpr int kPieces = kBytes / 16;
-    static constexpr int kGap = kPieces == 8 ? 0 : 128;
     static_assert(kPieces >= (sizeof(T) == 4 ? 16 : 8), "rows of 128 bytes (fp32: 256) at least");
-    static constexpr int size(int rows) { return rows * kBytes + rows / 4 * kGap; }
+    static constexpr int size(int rows) { return rows * kBytes; }
     __device__ __forceinline__ static int turn(int row)
     {
-        return kPieces == 8 ? (row & 6) : ((row & 3) << 1);
+        if constexpr (sizeof(T) == 4)
+            return ((row & 4) << 1) | ((row & 3) << 1) | ((row >> 3) & 1);
+        else if constexpr (kPieces == 8)
+            return ((row & 2) << 1) | ((row >> 2) & 3);
+        else
+            return ((row & 3) << 2) | ((row >> 2) & 3);
     }
-    __device__ __forceinline__ static int at(int row) { return row * kBytes + (row >> 2) * kGap; }
+    __device__ __forceinline__ static int at(int row) { return row * kBytes; }
     __device__ __forceinline__ static int at(int row, int piece) { return at(row) + ((piece ^ turn(row)) << 4); }
     // A lane's place in a tile, to be added to the tile's address once, and the
-    // chunks that follow from the sum (tiles start at multiples of 128 bytes):
+    // chunks that follow from the sum (tiles start at multiples of 256 bytes):
     // chunk s of channels of row (row0 + lane % 32)
     __device__ __forceinline__ static uint32_t row_lane() { return at(lane_id() & 31, lane_id() >> 5); }
     __device__ __forceinline__ static uint4v row_chunk(uint32_t tile_lane, int row0, int s)
     {
-        return *lds_at<uint4v>((tile_lane ^ ((2 * s & 7) << 4)) + at(row0) + ((2 * s >> 3) << 7));
+        return *lds_at<uint4v>((tile_lane ^ ((2 * s & 15) << 4)) + at(row0) + ((2 * s >> 4) << 8));
     }
     // chunk s of the rows from row0 on, column c0 + lane % 32 (c0 a multiple of 32)
     __device__ __forceinline__ static uint32_t col_lane()
@@ -136,12 +141,13 @@ struct Rows {
             uint4v r;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                r[j] = *lds_at<uint32_t>((tile_lane ^ (j << 5)) + j * kBytes + at(row0 + 8 * s) + (c0 << 2));
+                r[j] = *lds_at<uint32_t>((tile_lane ^ (j << 5) ^ ((s & 1) << 4) ^ ((c0 & 32) << 2)) + j * kBytes +
+                                         at(row0 + 8 * s) + ((c0 >> 6) << 8));
             return r;
         } else {
-            const uint32_t p = (tile_lane ^ ((c0 & 32) << 1)) + at(row0 + 16 * s) + ((c0 >> 6) << 7);
-            const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<short4v>(p));
-            const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<short4v>(p + at(8)));
+            const uint32_t p = tile_lane ^ ((c0 & 96) << 1), far = at(row0 + 16 * s) + ((c0 >> 7) << 8);
+            const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<short4v>(p + far));
+            const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<short4v>((p ^ 32) + far + at(8)));
             const uint2v x = __builtin_bit_cast(uint2v, a), y = __builtin_bit_cast(uint2v, b);
             return uint4v{x[0], x[1], y[0], y[1]};
         }
@@ -157,7 +163,7 @@ __device__ __forceinline__ P *uniform_ptr(P *p)
     return (P *)((uint64_t)hi << 32 | lo);
 }
 
-// Brings ROWS rows of PARTS parts (maps) of up to NC / PARTS channels from
+// Brings, by WAVES waves (1: each wave for itself), ROWS rows of PARTS parts (maps) of up to NC / PARTS channels from
 // memory to LDS.  Rows past `last` repeat row `last` (they are cleared, or
 // their products thrown away, by the caller); channels past `dim` of a part are
 // not written: the caller has cleared the buffer once.
@@ -174,13 +180,13 @@ __device__ __forceinline__ void load_rows(char *lds, const T *from, int64_t row_
     if constexpr (WIDE) {
         constexpr int kLoads = ROWS * R::kBytes / 1024, kStep = WAVES * 64 / R::kPieces;  // rows between a wave's loads
         static_assert(kLoads % WAVES == 0, "whole loads per wave");
-        const int w = wave_id();
+        const int w = WAVES == 1 ? 0 : wave_id();
         const uint32_t at = w * 64 + again(lane_id());
         const int row0 = at / R::kPieces;
 #pragma unroll
         for (int n = 0; n < kLoads / WAVES; ++n) {
             const int row = row0 + n * kStep;
-            const uint32_t piece = (at % R::kPieces) ^ R::turn(kStep % 4 == 0 ? row0 : row);
+            const uint32_t piece = (at % R::kPieces) ^ R::turn(kStep % 16 == 0 ? row0 : row);
             const int part = piece / kPart, ch = (piece % kPart) * per;
             const uint32_t off = (uint32_t)(min(row, last) * (int)row_stride + part * (int)part_stride + ch);
             if (ch < dim)
@@ -189,7 +195,7 @@ __device__ __forceinline__ void load_rows(char *lds, const T *from, int64_t row_
                     (PAM_LDS void *)(lds + R::at((n * WAVES + w) * 64 / R::kPieces)), 16, 0, 0);
         }
     } else {
-        for (int e = again(threadIdx.x); e < ROWS * PARTS * dim; e += 64 * WAVES) {
+        for (int e = again(WAVES == 1 ? lane_id() : (int)threadIdx.x); e < ROWS * PARTS * dim; e += 64 * WAVES) {
             const int c = e % dim, part = e / dim % PARTS, row = e / dim / PARTS;
             const int ch = part * (NC / PARTS) + c;
             *reinterpret_cast<T *>(lds + R::at(row, ch / per) + (ch % per) * sizeof(T)) =
@@ -203,9 +209,9 @@ template <class T, int NC, int ROWS, int WAVES>
 __device__ __forceinline__ void clear_rows(char *lds, uint64_t seen)
 {
     using R = Rows<T, NC>;
-    for (int e = again(threadIdx.x); e < ROWS * R::kPieces; e += 64 * WAVES)
+    for (int e = again(WAVES == 1 ? lane_id() : (int)threadIdx.x); e < ROWS * R::kPieces; e += 64 * WAVES)
         if (!(seen >> (e / R::kPieces) & 1))
-            store16(lds + R::at(e / R::kPieces) + e % R::kPieces * 16, uint4v{0, 0, 0, 0});
+            store16(lds + e * 16, uint4v{0, 0, 0, 0});
 }
 
 // A row as an operand, straight from memory: chunk s of channels of `row` for
