@@ -48,7 +48,8 @@ struct AttnArgs {
     const void *dout;
     int64_t dos[3];
     void *gq, *gk, *gv, *glam;
-    float *stats;     // lse^0 and lse^1 (base 2; infinity where a row sees nothing), D^0, D^1, each laid out as lse
+    float *stats;     // (sequence, head) x 4 x len_q: lse^0 and lse^1 (base 2; infinity where a row sees nothing), D^0,
+                      // D^1
     float *dlam;      // sum_ij p^1 dp of every wave of every item of the queries' pass
 };
 

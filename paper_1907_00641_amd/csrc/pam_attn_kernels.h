@@ -760,8 +760,9 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 lse[m] = x == -INFINITY ? INFINITY : x * kLog2e;
             }
             if (l < 32 && i < a.len_q && item.part == 0) {
-                a.stats[m * a.lse_map + at] = lse[m];
-                a.stats[(2 + m) * a.lse_map + at] = D[m];
+                float *st = a.stats + ((int64_t)b * a.heads + h) * 4 * a.len_q + i;
+                st[(int64_t)m * a.len_q] = lse[m];
+                st[(int64_t)(2 + m) * a.len_q] = D[m];
             }
         }
         f32x16 acc[2][S::TK] = {};
@@ -942,7 +943,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         auto head = [&](int h) {
             qp = uniform_ptr((const T *)a.q + b * a.qs[0] + ni * a.qs[1] + h * a.qs[2]);
             gp = uniform_ptr((const T *)a.dout + b * a.dos[0] + ni * a.dos[1] + h * a.dos[2]);
-            sp = uniform_ptr(a.stats + ((int64_t)b * a.heads + h) * a.len_q + ni);
+            sp = uniform_ptr(a.stats + ((int64_t)b * a.heads + h) * 4 * a.len_q + ni);
         };
         auto issue = [&](int buf) {
             char *to = lds + buf * S::kQueryTile;
@@ -950,9 +951,9 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             load_rows<T, DVP, 1, QT, kAttnWaves, WIDE>(to + RK::size(QT), gp, a.dos[1], 0, nq - 1 - ni, a.dim_v);
             if (w < 2) {  // 4 statistics of 32 queries: a wave takes two of them
                 const int y = again(l);
-                const float *p = sp + (2 * w + (y >> 5)) * a.lse_map + min(y & 31, nq - 1 - ni);
-                __builtin_amdgcn_global_load_lds((const PAM_GLOBAL void *)p,
-                                                 (PAM_LDS void *)(to + RK::size(QT) + RV::size(QT) + w * 256), 4, 0, 0);
+                load_lds4(uniform_ptr(sp + 2 * w * (int64_t)a.len_q),
+                          4u * (uint32_t)((y >> 5) * a.len_q + min(y & 31, nq - 1 - ni)),
+                          lds_address(to + RK::size(QT) + RV::size(QT)) + w * 256);
             }
             ni += QT;
             qp = uniform_ptr(qp + QT * a.qs[1]);

@@ -163,6 +163,26 @@ __device__ __forceinline__ P *uniform_ptr(P *p)
     return (P *)((uint64_t)hi << 32 | lo);
 }
 
+// 16 (4) bytes per lane from `base` + off straight to LDS, at `to` + 16 (4) times the
+// lane.  Written as assembly without outputs: the compiler, which sees that such a
+// load writes LDS but not where, waits for all of them before it reads any other
+// part of LDS, and the tile ahead would be waited for in the middle of the one at
+// hand.  wait_loads and a barrier stand between a tile's loads and its reads.
+__device__ __forceinline__ void load_lds16(const void *base, uint32_t off, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base)
+                 : "memory");
+}
+__device__ __forceinline__ void load_lds4(const void *base, uint32_t off, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base)
+                 : "memory");
+}
+
 // Brings, by WAVES waves (1: each wave for itself), ROWS rows of PARTS parts (maps) of up to NC / PARTS channels from
 // memory to LDS.  Rows past `last` repeat row `last` (they are cleared, or
 // their products thrown away, by the caller); channels past `dim` of a part are
@@ -190,9 +210,8 @@ __device__ __forceinline__ void load_rows(char *lds, const T *from, int64_t row_
             const int part = piece / kPart, ch = (piece % kPart) * per;
             const uint32_t off = (uint32_t)(min(row, last) * (int)row_stride + part * (int)part_stride + ch);
             if (ch < dim)
-                __builtin_amdgcn_global_load_lds(
-                    (const PAM_GLOBAL void *)((const char *)from + (uint32_t)(off * sizeof(T))),
-                    (PAM_LDS void *)(lds + R::at((n * WAVES + w) * 64 / R::kPieces)), 16, 0, 0);
+                load_lds16(from, (uint32_t)(off * sizeof(T)),
+                           lds_address(lds) + R::at((n * WAVES + w) * 64 / R::kPieces));
         }
     } else {
         for (int e = again(WAVES == 1 ? lane_id() : (int)threadIdx.x); e < ROWS * PARTS * dim; e += 64 * WAVES) {
