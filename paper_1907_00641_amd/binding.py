@@ -188,7 +188,7 @@ def _check(status: int, where: str):
 
 def _stream_ptr(stream) -> int:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return int(stream.cuda_stream)
 
 
@@ -456,44 +456,54 @@ def _dtype_of(t: torch.Tensor, name: str) -> int:
     return _DTYPES[t.dtype]
 
 
-def _rows_ptr(t: torch.Tensor, like: torch.Tensor, name: str) -> int:
-    """Pointer of a strided tensor whose last axis is contiguous, of ``like``'s type and device."""
-    if not t.is_cuda:
+def _device_of(t: torch.Tensor, name: str) -> int:
+    """Number of the current device, which ``t`` must be on."""
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError(f"{name} must be a device tensor")
-    if t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name} must be {like.dtype} on {like.device}")
-    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} must be on the current device")
+    return dev
+
+
+def _rows_ptr(t: torch.Tensor, dtype, dev: int, name: str) -> int:
+    """Pointer of a strided tensor whose last axis is contiguous."""
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be a device tensor of {dtype} on device {dev}")
+    if t.stride(-1) != 1 and t.numel() and t.shape[-1] > 1:
         raise ValueError(f"the last axis of {name} must be contiguous")
     return t.data_ptr()
 
 
-def _shaped_ptr(t: torch.Tensor | None, shape, dtype, like: torch.Tensor, name: str) -> int | None:
-    """Pointer of a contiguous tensor of the given shape and type on ``like``'s device (None: NULL)."""
+def _shaped_ptr(t: torch.Tensor | None, shape, dtype, dev: int, name: str) -> int | None:
+    """Pointer of a contiguous tensor of the given shape and type (None: NULL)."""
     if t is None:
         return None
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.device != like.device:
-        raise ValueError(f"{name} must be on {like.device}")
-    return _dev_ptr(t, dtype, name)
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be a device tensor of {dtype} on device {dev}")
+    raise ValueError(f"{name} must be contiguous")
 
 
-class _on_stream:
-    """New tensors belong to the stream that writes them: with a stream given,
-    memory freed after the call is not handed out while the stream uses it."""
+def _new(stream, make):
+    """What ``make`` allocates, on the stream that writes it: memory freed after the
+    call is not handed out again while that stream uses it."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
 
-    def __init__(self, stream, like: torch.Tensor):
-        if like.is_cuda and like.device.index != torch.cuda.current_device():
-            raise ValueError("the tensors must be on the current device")
-        self.ctx = None if stream is None else torch.cuda.stream(stream)
 
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
+_SIZE_MAX = ctypes.c_size_t(-1).value
 
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+
+def _workspace_bytes(n: int, where: str) -> int:
+    if n == _SIZE_MAX:
+        raise PamError(PAM_ERR_INVALID_ARGUMENT, where, last_error())
+    return n
 
 
 def _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask):
@@ -501,21 +511,21 @@ def _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask):
     if q.dim() != 5 or q.shape[3] != 2 or k.dim() != 5 or k.shape[3] != 2 or v.dim() != 4:
         raise ValueError("q must be B x Lq x H x 2 x d, k B x Lk x Hk x 2 x d, v B x Lk x Hk x dv")
     B, lq, H, _, d = q.shape
-    lk, hk, dv = k.shape[1], k.shape[2], v.shape[3]
-    if k.shape[0] != B or k.shape[4] != d or tuple(v.shape[:3]) != (B, lk, hk):
+    _, lk, hk, dv = v.shape
+    if k.shape != (B, lk, hk, 2, d) or v.shape[0] != B:
         raise ValueError("q, k and v do not agree in sequences, lengths, key heads or head size")
-    dtype = _dtype_of(q, "q")
-    ptrs = [_rows_ptr(q, q, "q"), _rows_ptr(k, q, "k"), _rows_ptr(v, q, "v"),
-            _shaped_ptr(lam, (H,), q.dtype, q, "lam"), _shaped_ptr(q_len, (B,), torch.int32, q, "q_len"),
-            _shaped_ptr(k_len, (B,), torch.int32, q, "k_len"), None]
+    dt = q.dtype
+    code, dev = _dtype_of(q, "q"), _device_of(q, "q")
+    ptrs = [_rows_ptr(q, dt, dev, "q"), _rows_ptr(k, dt, dev, "k"), _rows_ptr(v, dt, dev, "v"),
+            _shaped_ptr(lam, (H,), dt, dev, "lam"), _shaped_ptr(q_len, (B,), torch.int32, dev, "q_len"),
+            _shaped_ptr(k_len, (B,), torch.int32, dev, "k_len"), None]
     if key_mask is not None:
         if key_mask.dtype not in (torch.bool, torch.uint8):
             raise ValueError("key_mask must be bool or uint8")
-        ptrs[6] = _shaped_ptr(key_mask, (B, lk), key_mask.dtype, q, "key_mask")
-    qs, ks, vs = q.stride(), k.stride(), v.stride()
-    desc = DiffAttnDesc(dtype, B, H, hk, d, dv, lq, lk, PAM_ATTN_CAUSAL if causal else 0,
-                        d ** -0.5 if scale is None else scale, qs[:4], ks[:4], vs[:3])
-    return desc, ptrs
+        ptrs[6] = _shaped_ptr(key_mask, (B, lk), key_mask.dtype, dev, "key_mask")
+    desc = DiffAttnDesc(code, B, H, hk, d, dv, lq, lk, PAM_ATTN_CAUSAL if causal else 0,
+                        d ** -0.5 if scale is None else scale, q.stride()[:4], k.stride()[:4], v.stride()[:3])
+    return desc, ptrs, dev
 
 
 def pam_diff_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: torch.Tensor, *,
@@ -528,21 +538,19 @@ def pam_diff_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: to
     contiguous), ``lam`` H values of q's type; ``scale`` 1 / sqrt(d) if not given; ``q_len``, ``k_len`` B int32
     and ``key_mask`` B x Lk (bool or uint8) on the device.  Returns ``out`` (B x Lq x H x dv); with ``save``
     (out, saved), saved being what pam_diff_attn_bwd takes."""
-    desc, ptrs = _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask)
-    L = lib()
-    B, lq, H, dv = desc.batch, desc.len_q, desc.heads, desc.dim_v
-    ws_bytes = L.pam_diff_attn_fwd_workspace(ctypes.byref(desc))
-    if ws_bytes == ctypes.c_size_t(-1).value:
-        raise PamError(PAM_ERR_INVALID_ARGUMENT, "pam_diff_attn_fwd", last_error())
-    with _on_stream(stream, q):
-        out = torch.empty((B, lq, H, dv), dtype=q.dtype, device=q.device)
-        so = lse = ws = None
-        if save:
-            so = torch.empty((2, B, lq, H, dv), dtype=q.dtype, device=q.device)
-            lse = torch.empty((2, B, H, lq), dtype=torch.float32, device=q.device)
-        if ws_bytes:
-            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
-    _check(L.pam_diff_attn_fwd(ctypes.byref(desc), *ptrs, out.data_ptr(), so.data_ptr() if save else None,
+    desc, ptrs, _ = _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask)
+    L, d = lib(), ctypes.byref(desc)
+    shape = (*q.shape[:3], v.shape[3])
+    ws_bytes = _workspace_bytes(L.pam_diff_attn_fwd_workspace(d), "pam_diff_attn_fwd")
+
+    def make():
+        out = q.new_empty(shape)
+        so = q.new_empty((2, *shape)) if save else None
+        lse = q.new_empty((2, shape[0], shape[2], shape[1]), dtype=torch.float32) if save else None
+        return out, so, lse, q.new_empty(ws_bytes, dtype=torch.uint8) if ws_bytes else None
+
+    out, so, lse, ws = _new(stream, make)
+    _check(L.pam_diff_attn_fwd(d, *ptrs, out.data_ptr(), so.data_ptr() if save else None,
                                lse.data_ptr() if save else None, ws.data_ptr() if ws_bytes else None,
                                _stream_ptr(stream)), "pam_diff_attn_fwd")
     return (out, (so, lse)) if save else out
@@ -554,24 +562,22 @@ def pam_diff_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: to
                       key_mask: torch.Tensor | None = None, stream=None):
     """Gradients (q, k, v, lam) of pam_diff_attn_fwd with the same arguments,
     from its ``saved`` and ``grad_out`` (B x Lq x H x dv, any strides)."""
-    desc, ptrs = _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask)
-    L = lib()
-    B, lq, H, dv = desc.batch, desc.len_q, desc.heads, desc.dim_v
+    desc, ptrs, dev = _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask)
+    L, d = lib(), ctypes.byref(desc)
+    shape = (*q.shape[:3], v.shape[3])
     so, lse = saved
-    pso = _shaped_ptr(so, (2, B, lq, H, dv), q.dtype, q, "saved o")
-    plse = _shaped_ptr(lse, (2, B, H, lq), torch.float32, q, "saved lse")
-    if tuple(grad_out.shape) != (B, lq, H, dv):
-        raise ValueError(f"grad_out has shape {tuple(grad_out.shape)}, expected {(B, lq, H, dv)}")
-    pdo = _rows_ptr(grad_out, q, "grad_out")
-    ws_bytes = L.pam_diff_attn_bwd_workspace(ctypes.byref(desc))
-    if ws_bytes == ctypes.c_size_t(-1).value:
-        raise PamError(PAM_ERR_INVALID_ARGUMENT, "pam_diff_attn_bwd", last_error())
-    with _on_stream(stream, q):
-        gq, gk, gv, gl = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v, lam))
-        ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=q.device)
-    _check(L.pam_diff_attn_bwd(ctypes.byref(desc), *ptrs, pso, plse, pdo, (_i64 * 3)(*grad_out.stride()[:3]),
-                               gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), gl.data_ptr(), ws.data_ptr(),
-                               _stream_ptr(stream)), "pam_diff_attn_bwd")
+    pso = _shaped_ptr(so, (2, *shape), q.dtype, dev, "saved o")
+    plse = _shaped_ptr(lse, (2, shape[0], shape[2], shape[1]), torch.float32, dev, "saved lse")
+    if grad_out.shape != shape:
+        raise ValueError(f"grad_out has shape {tuple(grad_out.shape)}, expected {shape}")
+    pdo = _rows_ptr(grad_out, q.dtype, dev, "grad_out")
+    ws_bytes = _workspace_bytes(L.pam_diff_attn_bwd_workspace(d), "pam_diff_attn_bwd")
+    gq, gk, gv, gl, ws = _new(stream, lambda: (
+        q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(v.shape), q.new_empty(lam.shape),
+        q.new_empty(max(ws_bytes, 16), dtype=torch.uint8)))
+    _check(L.pam_diff_attn_bwd(d, *ptrs, pso, plse, pdo, (_i64 * 3)(*grad_out.stride()[:3]), gq.data_ptr(),
+                               gk.data_ptr(), gv.data_ptr(), gl.data_ptr(), ws.data_ptr(), _stream_ptr(stream)),
+           "pam_diff_attn_bwd")
     return gq, gk, gv, gl
 
 
@@ -603,11 +609,11 @@ def pam_rotary_table(freq: torch.Tensor, entries: int | None = None, coord: torc
         entries, axes = coord.shape
     elif entries is None:
         raise ValueError("give entries or coord")
-    pf = _dev_ptr(freq, torch.float64, "freq")
-    pc = _shaped_ptr(coord, (entries, axes), torch.float32, freq, "coord")
-    pa = _shaped_ptr(axis, (pairs,), torch.int32, freq, "axis")
-    with _on_stream(stream, freq):
-        table = torch.empty((max(entries, 0), pairs, 2), dtype=torch.float32, device=freq.device)
+    dev = _device_of(freq, "freq")
+    pf = _shaped_ptr(freq, (pairs,), torch.float64, dev, "freq")
+    pc = _shaped_ptr(coord, (entries, axes), torch.float32, dev, "coord")
+    pa = _shaped_ptr(axis, (pairs,), torch.int32, dev, "axis")
+    table = _new(stream, lambda: freq.new_empty((max(entries, 0), pairs, 2), dtype=torch.float32))
     _check(lib().pam_rotary_table(pf, pc, pa, entries, pairs, axes, magnitude, table.data_ptr(),
                                   _stream_ptr(stream)), "pam_rotary_table")
     return table
@@ -628,16 +634,15 @@ def pam_rotary(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, *, 
     flags = (PAM_ROTARY_INTERLEAVED if interleaved else 0) | (PAM_ROTARY_INVERSE if inverse else 0)
     desc = RotaryDesc(_dtype_of(q, "q"), B, n, H, hk, d, table.shape[1], flags, start, table.shape[0],
                       q.stride()[:3], (0, 0, 0) if k is None else k.stride()[:3])
-    pq, pk = _rows_ptr(q, q, "q"), None if k is None else _rows_ptr(k, q, "k")
-    pt = _shaped_ptr(table, table.shape, torch.float32, q, "table")
-    pp = _shaped_ptr(pos, (B, n), torch.int32, q, "pos")
-    with _on_stream(stream, q):
-        if out is None:
-            out = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-                   None if k is None else torch.empty(k.shape, dtype=q.dtype, device=q.device))
+    dt, dev = q.dtype, _device_of(q, "q")
+    pq, pk = _rows_ptr(q, dt, dev, "q"), None if k is None else _rows_ptr(k, dt, dev, "k")
+    pt = _shaped_ptr(table, table.shape, torch.float32, dev, "table")
+    pp = _shaped_ptr(pos, (B, n), torch.int32, dev, "pos")
+    if out is None:
+        out = _new(stream, lambda: (q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)))
     qo, ko = out
-    pqo = _shaped_ptr(qo, q.shape, q.dtype, q, "q_out")
-    pko = None if k is None else _shaped_ptr(ko, k.shape, q.dtype, q, "k_out")
+    pqo = _shaped_ptr(qo, q.shape, dt, dev, "q_out")
+    pko = None if k is None else _shaped_ptr(ko, k.shape, dt, dev, "k_out")
     _check(lib().pam_rotary(ctypes.byref(desc), pq, pk, pt, pp, pqo, pko, _stream_ptr(stream)), "pam_rotary")
     return qo, ko
 
@@ -646,13 +651,12 @@ def pam_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, out: torc
                 stream=None) -> torch.Tensor:
     """x times 1 / (1 - p) where the numbers that Philox4x32-10 makes of (seed, offset, element) keep it, else 0.
     The gradient is the same call on the upstream gradient.  ``out`` may be ``x``."""
-    dtype = _dtype_of(x, "x")
-    px = _dev_ptr(x, x.dtype, "x")
-    with _on_stream(stream, x):
-        if out is None:
-            out = torch.empty_like(x)
-    po = _shaped_ptr(out, x.shape, x.dtype, x, "out")
-    _check(lib().pam_dropout(px, x.numel(), dtype, p, seed, offset, po, _stream_ptr(stream)), "pam_dropout")
+    code, dev = _dtype_of(x, "x"), _device_of(x, "x")
+    px = _shaped_ptr(x, x.shape, x.dtype, dev, "x")
+    if out is None:
+        out = _new(stream, lambda: torch.empty_like(x))
+    po = _shaped_ptr(out, x.shape, x.dtype, dev, "out")
+    _check(lib().pam_dropout(px, x.numel(), code, p, seed, offset, po, _stream_ptr(stream)), "pam_dropout")
     return out
 
 
@@ -668,16 +672,16 @@ def _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, se
                 (gate.shape[0] and n % gate.shape[0]):
             raise ValueError("gate must be rows x channels, its rows dividing x's")
         gate_rows = n // gate.shape[0] if gate.shape[0] else 1
+    dt, f32 = x.dtype, torch.float32
     desc = NormDesc(_dtype_of(x, "x"), NORMS[norm], n, c, eps, gate_rows, x.stride(0),
                     x.stride(0) if z is None else z.stride(0), p, seed, offset)
-    f32 = torch.float32
-    ptrs = {"x": _rows_ptr(x, x, "x"), "z": None if z is None else _rows_ptr(z, x, "z"),
-            "w_post": _shaped_ptr(w_post, (c,), f32, x, "w_post"),
-            "b_post": _shaped_ptr(b_post, (c,), f32, x, "b_post"),
-            "gate": None if gate is None else _shaped_ptr(gate, gate.shape, x.dtype, x, "gate"),
-            "scale": _shaped_ptr(scale, (c,), f32, x, "scale"), "w_pre": _shaped_ptr(w_pre, (c,), f32, x, "w_pre"),
-            "b_pre": _shaped_ptr(b_pre, (c,), f32, x, "b_pre")}
-    return desc, ptrs
+    dev = _device_of(x, "x")
+    ptrs = [_rows_ptr(x, dt, dev, "x"), None if z is None else _rows_ptr(z, dt, dev, "z"),
+            _shaped_ptr(w_post, (c,), f32, dev, "w_post"), _shaped_ptr(b_post, (c,), f32, dev, "b_post"),
+            None if gate is None else _shaped_ptr(gate, gate.shape, dt, dev, "gate"),
+            _shaped_ptr(scale, (c,), f32, dev, "scale"), _shaped_ptr(w_pre, (c,), f32, dev, "w_pre"),
+            _shaped_ptr(b_pre, (c,), f32, dev, "b_pre")]
+    return desc, ptrs, dev
 
 
 def pam_norm_gate_fwd(x: torch.Tensor, *, z: torch.Tensor | None = None, w_post: torch.Tensor | None = None,
@@ -689,11 +693,10 @@ def pam_norm_gate_fwd(x: torch.Tensor, *, z: torch.Tensor | None = None, w_post:
 
     ``x``, ``z`` rows x channels (``z`` None: r is x), ``gate`` G x channels (each row for rows / G consecutive
     rows), vectors fp32.  Returns (r, h); r is None without z, h without ``next_norm``."""
-    desc, ptr = _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, seed, offset)
-    with _on_stream(stream, x):
-        r = None if z is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if next_norm else None
-    _check(lib().pam_norm_gate_fwd(ctypes.byref(desc), *ptr.values(), None if r is None else r.data_ptr(),
+    desc, ptrs, _ = _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, seed, offset)
+    r, h = _new(stream, lambda: (None if z is None else x.new_empty(x.shape),
+                                 x.new_empty(x.shape) if next_norm else None))
+    _check(lib().pam_norm_gate_fwd(ctypes.byref(desc), *ptrs, None if r is None else r.data_ptr(),
                                    None if h is None else h.data_ptr(), _stream_ptr(stream)), "pam_norm_gate_fwd")
     return r, h
 
@@ -706,22 +709,14 @@ def pam_norm_gate_bwd(x: torch.Tensor, *, grad_r: torch.Tensor | None, grad_h: t
                       seed: int = 0, offset: int = 0, stream=None) -> dict:
     """Gradients of pam_norm_gate_fwd with the same arguments, by the arguments' names (None for those not
     given), from ``grad_r`` (None: 0) and ``grad_h`` (None: the forward call had no next norm)."""
-    desc, ptr = _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, seed, offset)
-    L = lib()
-    pr = _shaped_ptr(grad_r, x.shape, x.dtype, x, "grad_r")
-    ph = _shaped_ptr(grad_h, x.shape, x.dtype, x, "grad_h")
-    ws_bytes = L.pam_norm_gate_bwd_workspace(ctypes.byref(desc))
-    if ws_bytes == ctypes.c_size_t(-1).value:
-        raise PamError(PAM_ERR_INVALID_ARGUMENT, "pam_norm_gate_bwd", last_error())
-    given = {"x": x, "z": z, "w_post": w_post, "b_post": b_post, "gate": gate, "scale": scale, "w_pre": w_pre,
-             "b_pre": b_pre}
-    with _on_stream(stream, x):
-        grads = {name: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
-                 for name, t in given.items()}
-        ws = torch.empty(max(ws_bytes, 16), dtype=torch.uint8, device=x.device)
-    out = {name: None if t is None else t.data_ptr() for name, t in grads.items()}
-    _check(L.pam_norm_gate_bwd(ctypes.byref(desc), *(ptr[a] for a in ("x", "z", "w_post", "b_post", "gate", "scale",
-                                                                      "w_pre")), pr, ph,
-                               *(out[a] for a in ("x", "z", "w_post", "b_post", "gate", "scale", "w_pre", "b_pre")),
+    desc, ptrs, dev = _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, seed, offset)
+    L, d = lib(), ctypes.byref(desc)
+    pr = _shaped_ptr(grad_r, x.shape, x.dtype, dev, "grad_r")
+    ph = _shaped_ptr(grad_h, x.shape, x.dtype, dev, "grad_h")
+    ws_bytes = _workspace_bytes(L.pam_norm_gate_bwd_workspace(d), "pam_norm_gate_bwd")
+    given = (x, z, w_post, b_post, gate, scale, w_pre, b_pre)
+    *grads, ws = _new(stream, lambda: [None if t is None else t.new_empty(t.shape) for t in given] + [
+        x.new_empty(max(ws_bytes, 16), dtype=torch.uint8)])
+    _check(L.pam_norm_gate_bwd(d, *ptrs[:7], pr, ph, *(None if t is None else t.data_ptr() for t in grads),
                                ws.data_ptr(), _stream_ptr(stream)), "pam_norm_gate_bwd")
-    return grads
+    return dict(zip(("x", "z", "w_post", "b_post", "gate", "scale", "w_pre", "b_pre"), grads))

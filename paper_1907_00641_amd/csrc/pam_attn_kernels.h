@@ -10,6 +10,7 @@
 #pragma once
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "pam_attn_tiles.h"
@@ -1169,17 +1170,31 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_finish(AttnArgs a)
 // blocks of a launch: fewer than 2^32 work items, the rest in turns
 inline unsigned item_blocks(int64_t items) { return (unsigned)std::min<int64_t>(items, 1 << 23); }
 
+// `done`: devices that know of the kernel's LDS beyond 64 KB
 template <class K>
-hipError_t launch_lds(K kernel, unsigned blocks, unsigned threads, int lds, const AttnArgs &a, hipStream_t s)
+hipError_t launch_lds(K kernel, unsigned blocks, unsigned threads, int lds, const AttnArgs &a, hipStream_t s,
+                      std::atomic<uint64_t> &done)
 {
     if (lds > (64 << 10)) {
-        const hipError_t e =
-            hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+        if (e == hipSuccess && !(done.load(std::memory_order_relaxed) & bit)) {
+            e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            if (e == hipSuccess)
+                done.fetch_or(bit, std::memory_order_relaxed);
+        }
         if (e != hipSuccess)
             return e;
     }
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, s, a);
     return hipGetLastError();
+}
+template <auto K>
+hipError_t launch_lds(unsigned blocks, unsigned threads, int lds, const AttnArgs &a, hipStream_t s)
+{
+    static std::atomic<uint64_t> done{0};
+    return launch_lds(K, blocks, threads, lds, a, s, done);
 }
 
 inline unsigned sum_blocks(int64_t sums)
@@ -1193,10 +1208,10 @@ hipError_t fwd_class(const AttnArgs &a, bool few, hipStream_t s)
     using S = Sizes<T, DP, DVP>;
     hipError_t e;
     if (few)
-        e = launch_lds(k_attn_few<T, DP, DVP, WIDE>, item_blocks(a.plan.items()), 64 * S::kFewWaves,
+        e = launch_lds<k_attn_few<T, DP, DVP, WIDE>>(item_blocks(a.plan.items()), 64 * S::kFewWaves,
                        S::kFewWaves * (2 * S::kFewTile + 32 * 16), a, s);
     else
-        e = launch_lds(k_attn_fwd<T, DP, DVP, WIDE>, item_blocks(a.plan.items()), kAttnThreads, 2 * S::kKeyTile, a, s);
+        e = launch_lds<k_attn_fwd<T, DP, DVP, WIDE>>(item_blocks(a.plan.items()), kAttnThreads, 2 * S::kKeyTile, a, s);
     if (e != hipSuccess || a.plan.parts == 1)
         return e;
     const unsigned blocks = sum_blocks((int64_t)(a.plan.units - a.plan.full) * kBlockRows * DVP / 4);
@@ -1214,17 +1229,17 @@ hipError_t bwd_class(const AttnArgs &a, hipStream_t s)
     hipError_t e = hipSuccess;
     const unsigned rows = item_blocks(a.plan.items()), keys = item_blocks(a.key_plan.items());
     if (rows)
-        e = launch_lds(k_attn_dq<T, DP, DVP, WIDE>, rows, kAttnThreads, 2 * S::kKeyTile, a, s);
+        e = launch_lds<k_attn_dq<T, DP, DVP, WIDE>>(rows, kAttnThreads, 2 * S::kKeyTile, a, s);
     if (e != hipSuccess)
         return e;
     constexpr int lds = 2 * S::kQueryTile + S::kValues;
     if constexpr (DP <= 64) {
         if (keys)
-            e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE, 3>, keys, kAttnThreads, lds, a, s);
+            e = launch_lds<k_attn_dkv<T, DP, DVP, WIDE, 3>>(keys, kAttnThreads, lds, a, s);
     } else if (keys) {
-        e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE, 1>, keys, kAttnThreads, lds, a, s);
+        e = launch_lds<k_attn_dkv<T, DP, DVP, WIDE, 1>>(keys, kAttnThreads, lds, a, s);
         if (e == hipSuccess)
-            e = launch_lds(k_attn_dkv<T, DP, DVP, WIDE, 2>, keys, kAttnThreads, lds, a, s);
+            e = launch_lds<k_attn_dkv<T, DP, DVP, WIDE, 2>>(keys, kAttnThreads, lds, a, s);
     }
     if (e != hipSuccess)
         return e;
