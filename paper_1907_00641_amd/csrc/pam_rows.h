@@ -103,6 +103,12 @@ __device__ __forceinline__ float lanes_sum(float x)
     return x;
 }
 
+// a / b of numbers that are not negative, in 32 bits where they fit
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)
+{
+    return ((a | b) >> 32) ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 // Philox4x32-10 (Salmon, Moraes, Dror and Shaw 2011, "Parallel random
 // numbers: as easy as 1, 2, 3"): ten rounds of two 32 x 32 -> 64 bit products,
 // the key stepped by Weyl constants.
