@@ -151,6 +151,32 @@ def test_attention_matches_oracle(shape, t, causal):
     c.compare(*c.run())
 
 
+PART_SHAPES = [  # few tiles over a long axis, cut into parts that are joined
+    (2, 300, 700, 4, 2, 32, 64),
+    (1, 200, 600, 3, 1, 64, 128),
+    (1, 150, 520, 2, 1, 128, 256),
+    (1, 700, 300, 2, 2, 40, 80),
+    (13, 140, 300, 20, 20, 8, 16),  # whole rounds of blocks, and then some
+]
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", PART_SHAPES, ids=str)
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_in_parts(shape, t, causal):
+    log(f"[attn parts] {shape} {t} causal={causal}")
+    c = Case(5, *shape, t, causal=causal)
+    c.compare(*c.run())
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_parts_that_see_nothing(t, causal):
+    log(f"[attn empty parts] {t} causal={causal}")
+    c = Case(6, 4, 300, 900, 4, 2, 32, 64, t, causal=causal, q_len=[0, 300, 130, 257], k_len=[900, 20, 0, 641], mask=0.5)
+    c.compare(*c.run())
+
+
 @pytest.mark.parametrize("t", ["f32", "bf16"])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("q_len,k_len,mask", [([0, 70, 33], [0, 90, 91], None), ([70, 1, 64], [1, 0, 64], None),
