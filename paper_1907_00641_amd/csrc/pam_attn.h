@@ -11,6 +11,7 @@ struct Plan {
     uint32_t units, full, parts;
     uint32_t rows_of_heads;  // 0: units are numbered head by head; else the number of heads in all sequences, and
                              // units are numbered tile by tile
+    uint32_t fold;           // units [fold, 2 fold) are taken in reverse; 0: none
     __host__ __device__ uint32_t unit(uint32_t bh, uint32_t tile) const
     {
         return rows_of_heads ? tile * rows_of_heads + bh : bh * tiles + tile;

@@ -119,11 +119,13 @@ struct Item {
     // consecutive ones, which share keys and values, go to one die, so that its L2
     // serves them.  Causal units are numbered tile by tile, the longest first, and
     // taken as they come: every die gets as many long ones (and the same heads,
-    // where those are a multiple of eight).
+    // where those are a multiple of eight).  Where two blocks share a CU, the
+    // second ones of the first round are taken in reverse: the longest unit is
+    // paired with the shortest of the round.
     __device__ __forceinline__ static uint32_t order(const Plan &p, uint32_t n, uint32_t total)
     {
         if (p.rows_of_heads)
-            return n;
+            return n >= p.fold && n < 2 * p.fold ? 3 * p.fold - 1 - n : n;
         const uint32_t per = total / 8, rest = total - per * 8, die = n % 8;
         return die * per + min(die, rest) + n / 8;
     }
