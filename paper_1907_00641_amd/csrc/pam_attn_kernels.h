@@ -495,7 +495,9 @@ __device__ __forceinline__ void join_row(const AttnArgs &a, int parts, const Get
 // queries of all heads of a key head, 32 at a time; the waves of a block walk over
 // their own keys, without waiting for each other, and join their sums in LDS.
 // What bounds it is reading the cache: every wave has two tiles of 32 keys under
-// way.
+// way (bf16, 8 x 16384 keys, 8 key heads of 64, 32 query heads: 108 us, 5.0 TB/s,
+// joining included).  A short cache is bound by the steps' latency: 300 keys, three
+// steps of a wave, 11.5 us.
 template <class T, int DP, int DVP, bool WIDE>
 __global__ __launch_bounds__((64 * Sizes<T, DP, DVP>::kFewWaves)) void k_attn_few(AttnArgs a)
 {
@@ -517,7 +519,9 @@ __global__ __launch_bounds__((64 * Sizes<T, DP, DVP>::kFewWaves)) void k_attn_fe
         const int r = item.tile * 32 + (l & 31), g = r / a.len_q, i = r - g * a.len_q, h = hk * a.group + g;
         const bool in = g < a.group && i < nq;
         const int limit = in ? (a.causal ? min(nk, i + nk - nq + 1) : nk) : 0;
-        int wend = limit, wall = limit;  // over the wave's rows: the most, the least
+        // over the wave's rows: the most, the least; lanes without a row do not ask
+        // that anything be hidden from them
+        int wend = limit, wall = g < a.group ? limit : nk;
 #pragma unroll
         for (int s = 1; s < 32; s <<= 1) {
             wend = max(wend, __shfl_xor(wend, s));
@@ -616,24 +620,29 @@ __global__ __launch_bounds__((64 * Sizes<T, DP, DVP>::kFewWaves)) void k_attn_fe
 }
 
 // Joins the parts of a launch's last units: a thread per four channels of a row;
-// FEW (up to 256 parts of few rows): a block per row, eight threads per four
-// channels that take every eighth part each.
+// FEW (up to 256 parts of few rows): a block per row, G threads per four
+// channels that take every G-th part each; what bounds it is the loads' latency, so
+// there are enough for each to wait for one or two rounds of them (8 rows of 156
+// parts: 16.5 us with 8 threads that take a part at a time, 12.6 so).
+constexpr int kJoinThreads = 1024;  // FEW: the most
+
 template <class T, int DVP, bool FEW>
-__global__ __launch_bounds__(kAttnThreads) void k_attn_join(AttnArgs a)
+__global__ __launch_bounds__((FEW ? kJoinThreads : kAttnThreads)) void k_attn_join(AttnArgs a)
 {
     constexpr int ROWS = FEW ? 32 : kBlockRows, QUADS = DVP / 4;
-    const uint32_t rows = (a.plan.units - a.plan.full) * ROWS;
     const float *stats = a.part + (int64_t)a.plan.slots() * ROWS * 2 * DVP;
     auto stats_of = [&](int64_t at) { return *reinterpret_cast<const float4v *>(stats + at * 4); };
     auto sums_of = [&](int64_t at, int m, int ch) {
         return *reinterpret_cast<const float4v *>(a.part + at * 2 * DVP + m * DVP + ch);
     };
     if constexpr (FEW) {
-        constexpr int G = kAttnThreads / QUADS;
-        __shared__ float4v gs[G], go[G][2][QUADS];
+        constexpr int MOST = kJoinThreads / QUADS;
+        __shared__ float4v gs[MOST], go[MOST][2][QUADS];
+        const int G = blockDim.x / QUADS;
+        const uint32_t per = min(a.group * a.len_q, ROWS), rows = (a.plan.units - a.plan.full) * per;
         const int g = threadIdx.x / QUADS, ch = threadIdx.x % QUADS * 4;
         for (uint32_t x = blockIdx.x; x < rows; x += gridDim.x) {
-            const uint32_t u = x / ROWS, row = x % ROWS, unit = a.plan.full + u;
+            const uint32_t u = x / per, row = x - u * per, unit = a.plan.full + u;
             const uint32_t bh = a.plan.bh_of(unit), tile = a.plan.tile_of(unit);
             const int b = bh / a.plan.heads, hv = bh - b * a.plan.heads, hk = hv / a.value_parts;
             const int v0 = (hv - hk * a.value_parts) * DVP;
@@ -642,19 +651,29 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_join(AttnArgs a)
                 continue;
             auto at = [&](int p) { return ((int64_t)u * a.plan.parts + p) * ROWS + row; };
             float4v st = {-INFINITY, -INFINITY, 0.0f, 0.0f}, o[2] = {};
-            for (int p = g; p < (int)a.plan.parts; p += G) {
-                const float4v sp = stats_of(at(p)), x0 = sums_of(at(p), 0, ch), x1 = sums_of(at(p), 1, ch);
+            for (int p0 = g; p0 < (int)a.plan.parts; p0 += 4 * G) {
+                float4v sp[4], x[4][2];  // four parts' loads are under way together
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    if (sp[2 + m] == 0.0f)  // saw nothing
-                        continue;
-                    const float to = __builtin_fmaxf(st[m], sp[m]);
-                    const float f0 = st[m] == -INFINITY ? (st[2 + m] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(st[m] - to);
-                    const float f1 = sp[m] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sp[m] - to);
-                    o[m] = o[m] * f0 + (m ? x1 : x0) * f1;
-                    st[2 + m] = st[2 + m] * f0 + sp[2 + m] * f1;
-                    st[m] = to;
+                for (int k = 0; k < 4; ++k) {
+                    const int p = min(p0 + k * G, (int)a.plan.parts - 1);
+                    sp[k] = stats_of(at(p));
+                    x[k][0] = sums_of(at(p), 0, ch);
+                    x[k][1] = sums_of(at(p), 1, ch);
                 }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        if (p0 + k * G >= (int)a.plan.parts || sp[k][2 + m] == 0.0f)  // saw nothing
+                            continue;
+                        const float to = __builtin_fmaxf(st[m], sp[k][m]);
+                        const float f0 =
+                            st[m] == -INFINITY ? (st[2 + m] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(st[m] - to);
+                        const float f1 = sp[k][m] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sp[k][m] - to);
+                        o[m] = o[m] * f0 + x[k][m] * f1;
+                        st[2 + m] = st[2 + m] * f0 + sp[k][2 + m] * f1;
+                        st[m] = to;
+                    }
             }
             __syncthreads();
             if (ch == 0)
@@ -668,6 +687,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_attn_join(AttnArgs a)
                     min(a.dim_v - v0, DVP));
         }
     } else {
+        const uint32_t rows = (a.plan.units - a.plan.full) * ROWS;
         for (uint32_t e = blockIdx.x * kAttnThreads + threadIdx.x; e < rows * QUADS; e += gridDim.x * kAttnThreads) {
             const uint32_t x = e / QUADS, ch = e % QUADS * 4;
             const uint32_t u = x / ROWS, row = x % ROWS, unit = a.plan.full + u;
@@ -1216,11 +1236,14 @@ hipError_t fwd_class(const AttnArgs &a, bool few, hipStream_t s)
         e = launch_lds<k_attn_fwd<T, DP, DVP, WIDE>>(item_blocks(a.plan.items()), kAttnThreads, 2 * S::kKeyTile, a, s);
     if (e != hipSuccess || a.plan.parts == 1)
         return e;
-    const unsigned blocks = sum_blocks((int64_t)(a.plan.units - a.plan.full) * kBlockRows * DVP / 4);
-    if (few)
-        hipLaunchKernelGGL((k_attn_join<T, DVP, true>), dim3((a.plan.units - a.plan.full) * 32), dim3(kAttnThreads), 0, s, a);
-    else
+    const unsigned cut = a.plan.units - a.plan.full;
+    if (few) {
+        const unsigned rows = cut * std::min(a.group * a.len_q, 32);
+        hipLaunchKernelGGL((k_attn_join<T, DVP, true>), dim3(rows), dim3(a.plan.parts > 32 ? kJoinThreads : 256), 0, s, a);
+    } else {
+        const unsigned blocks = sum_blocks((int64_t)cut * kBlockRows * DVP / 4);
         hipLaunchKernelGGL((k_attn_join<T, DVP, false>), dim3(blocks), dim3(kAttnThreads), 0, s, a);
+    }
     return hipGetLastError();
 }
 
