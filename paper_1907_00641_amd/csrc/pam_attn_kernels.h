@@ -40,6 +40,12 @@ struct Sizes {
     // for the scores
     static constexpr bool kSmall = (sizeof(T) == 2 && DP <= 64) || (sizeof(T) == 4 && DP <= 32);
     static constexpr int kWavesPerSimd = kSmall ? 2 : 1;
+    // Whether a wave skips the part of a tile that none of its rows sees.  With one
+    // wave the sums lie in registers that only the matrix units reach, and a
+    // branch around the products costs a copy of them all for every tile: those
+    // classes form the products and hide them (bf16, 2 x 4800, 8 heads of 128,
+    // backward: 2810 us for 3254).
+    static constexpr bool kSkip = kSmall;
     // LDS: a tile of keys and values; of queries and dout with 4 statistics
     // each; the block's values of the keys' pass
     static constexpr int kKeyTile = RK::size(kKeys) + RV::size(kKeys);
@@ -389,7 +395,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
 #pragma unroll
             for (int kt = 0; kt < KT / 32; ++kt) {
                 const int j0 = k0 + 32 * kt;
-                if (j0 < wend)
+                if (!S::kSkip || j0 < wend)
                     Q.step(kr, vc, 32 * kt, c, some_hidden || j0 + 32 > wall, j0, limit, (uint32_t)(seen >> (32 * kt)));
             }
         }
@@ -810,7 +816,8 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
 #pragma unroll
             for (int kt = 0; kt < KT / 32; ++kt) {
                 const int j0 = k0 + 32 * kt;
-                if (j0 >= wend)
+                // (fp16's branch in Range costs the copies anyhow)
+                if ((S::kSkip || std::is_same<T, f16>::value) && j0 >= wend)
                     break;
                 f32x16 s[2] = {}, dp = {};
 #pragma unroll
@@ -1012,7 +1019,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 clear_rows<T, DVP, QT, kAttnWaves>(gb, (1ull << (nq - i0)) - 1);
                 __syncthreads();
             }
-            if (wany && i0 + QT > wfirst) {
+            if (!S::kSkip || (wany && i0 + QT > wfirst)) {
                 const uint32_t qr = lds_address(qb) + RK::row_lane(), qc = lds_address(qb) + RK::col_lane();
                 const uint32_t gr = lds_address(gb) + RV::row_lane(), gc = lds_address(gb) + RV::col_lane();
                 const uint32_t vr = lds_address(vrows) + RV::row_lane();
