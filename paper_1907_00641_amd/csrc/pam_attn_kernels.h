@@ -163,17 +163,19 @@ __device__ __forceinline__ bool key_seen(const AttnArgs &a, int b, int nk, int j
     return j < nk && (!a.key_mask || a.key_mask[(int64_t)b * a.len_k + j]);
 }
 
-// scores of this lane's keys to -inf where they are not seen: keys from
-// `limit` on and those whose bit in `seen` (bit 0: the first key of the 32) is 0
-__device__ __forceinline__ void hide(f32x16 &s, int key0, int limit, uint32_t seen)
+// The lowest n of 32 bits.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1; }
+
+// Both maps' scores of this lane's rows to -inf where a bit is 0.  bits: of the
+// 32 rows; a lane holds rows 8 x + y + 4 (l / 32).
+__device__ __forceinline__ void hide(f32x16 (&s)[2], uint32_t bits)
 {
-    const int h4 = 4 * (lane_id() >> 5);
-    const uint32_t bits = seen >> h4;
-    const int lim = limit - key0 - h4;
+    bits >>= 4 * (lane_id() >> 5);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        const int j = 8 * (r >> 2) + (r & 3);
-        s[r] = (j < lim && (bits >> j & 1)) ? s[r] : -INFINITY;
+        const bool see = bits >> (8 * (r >> 2) + (r & 3)) & 1;
+        s[0][r] = see ? s[0][r] : -INFINITY;
+        s[1][r] = see ? s[1][r] : -INFINITY;
     }
 }
 
@@ -227,10 +229,8 @@ struct Queries {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
                 mma<T>(s[m], RK::row_chunk(kr, r0, m * S::CK + x), q[m][x]);
-        if (some) {
-            hide(s[0], j0, limit, seen);
-            hide(s[1], j0, limit, seen);
-        }
+        if (some)
+            hide(s, seen & low_bits(limit - j0));
         uint4v p[2][S::CP];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -828,10 +828,8 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
 #pragma unroll
                 for (int x = 0; x < S::CV; ++x)
                     mma<T>(dp, RV::row_chunk(vr, 32 * kt, x), g[x]);
-                if (some_hidden || j0 + 32 > wall) {
-                    hide(s[0], j0, limit, (uint32_t)(seen >> (32 * kt)));
-                    hide(s[1], j0, limit, (uint32_t)(seen >> (32 * kt)));
-                }
+                if (some_hidden || j0 + 32 > wall)
+                    hide(s, (uint32_t)(seen >> (32 * kt)) & low_bits(limit - j0));
                 uint4v ds[2][S::CP];
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
@@ -1040,15 +1038,8 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                         mma<T>(dp, RV::row_chunk(gr, 0, x), RV::row_chunk(vr, 0, x));
                     else
                         mma<T>(dp, RV::row_chunk(gr, 0, x), memory_chunk<T, WIDE>(vrow, x, a.dim_v, seen));
-                if (!all || i0 < wfirst + 31 || tail) {
-                    const int lim = from - i0 - 4 * (l >> 5), rows = nq - i0 - 4 * (l >> 5);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const bool see = 8 * (r >> 2) + (r & 3) >= lim && 8 * (r >> 2) + (r & 3) < rows;
-                        s[0][r] = see ? s[0][r] : -INFINITY;
-                        s[1][r] = see ? s[1][r] : -INFINITY;
-                    }
-                }
+                if (!all || i0 < wfirst + 31 || tail)
+                    hide(s, low_bits(nq - i0) & ~low_bits(from > i0 ? from - i0 : 0));
                 uint4v wf[S::CP], ds[2][S::CP];
                 f32x16 wt;
 #pragma unroll
