@@ -386,8 +386,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             if (t + 1 < to)
                 issue(t + 1);
             const bool some_hidden = seen != kAllSeen<KT>;
-            if (some_hidden) {  // the same in every wave of the block
-                clear_rows<T, 2 * DP, KT, kAttnWaves>(kb, seen);
+            if (some_hidden) {  // the same in every wave of the block; of keys, the scores are hidden
                 clear_rows<T, DVP, KT, kAttnWaves>(vb, seen);
                 __syncthreads();
             }
@@ -572,7 +571,6 @@ __global__ __launch_bounds__((64 * Sizes<T, DP, DVP>::kFewWaves)) void k_attn_fe
                 issue(t + 1);
             const bool some_hidden = seen != kAllSeen<KT>;
             if (some_hidden) {
-                clear_rows<T, 2 * DP, KT, 1>(kb, seen);
                 clear_rows<T, DVP, KT, 1>(vb, seen);
                 wave_fence();
             }
