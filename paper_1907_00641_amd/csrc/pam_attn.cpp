@@ -76,15 +76,19 @@ int64_t at_once(const pam_diff_attn_desc_t &d)
 }
 
 // Units beyond whole rounds of `room` blocks are cut into parts that fill one
-// more round, of at least `least` of the unit's `trips` each (`slow`: in fp32).
+// more round, of at least `least` of the unit's `trips` each (`slow`: in fp32), or
+// of `shortest` where they do not come to one block per CU: waiting for a longer
+// part takes longer there than joining more of them.  (fp32, 1 x 500, 8 heads of
+// 64: 43 us for 74, backward 79 for 160; bf16, backward, 44 for 54, but 4 x 500, a
+// block per CU without it, 74 for 67.)
 // Causal units are of unequal lengths: from a round and a half on (a quarter, with
 // two blocks on a CU) they fill the rounds by themselves, longest first; fewer
 // would wait for the longest, so they are all cut, where two blocks share a CU if
 // they are long.
 // bf16, 8 heads of 64, 8192 tokens: 320 us cut for 338 whole, backward 715 for 903;
 // 2 x 4800: 209 for 186; fp32, 4096 tokens (one block per CU): 538 for 933.
-Plan plan_of(int64_t tiles, int64_t heads, int64_t batch, int64_t room, int64_t trips, int64_t least, bool causal,
-             bool slow)
+Plan plan_of(int64_t tiles, int64_t heads, int64_t batch, int64_t room, int64_t trips, int64_t least, int64_t shortest,
+             bool causal, bool slow)
 {
     Plan p{};
     p.tiles = (uint32_t)tiles;
@@ -97,7 +101,7 @@ Plan plan_of(int64_t tiles, int64_t heads, int64_t batch, int64_t room, int64_t 
     const bool two = room == 2 * kCUs;
     const bool enough = causal && (units >= (two ? room * 5 / 4 : room * 3 / 2) || (two && units >= room && most < 20));
     p.fold = enough && two ? (uint32_t)kCUs : 0;
-    if (units == 0 || most < 2 || enough)
+    if (units == 0 || trips / shortest < 2 || enough)
         return p;
     const int64_t full = causal ? 0 : units / room * room, rest = units - full;
     if (rest == 0)
@@ -106,8 +110,8 @@ Plan plan_of(int64_t tiles, int64_t heads, int64_t batch, int64_t room, int64_t 
     // more would cost more: short units of 16-bit types with two blocks on a CU
     // (bf16, 3 x 1000, 8 heads of 64: 48 us for 61; 1 x 4000, backward: 249 for 235)
     const bool one_round = two && !slow && most < 12;
-    const int64_t parts =
-        std::min(most, causal ? std::max<int64_t>((one_round ? room : 2 * room) / rest, 2) : room / rest);
+    const int64_t fill = causal ? std::max<int64_t>((one_round ? room : 2 * room) / rest, 2) : room / rest;
+    const int64_t parts = std::max(std::min(most, fill), std::min(trips / shortest, kCUs / rest));
     if (parts < 2)
         return p;
     p.full = (uint32_t)full;
@@ -137,11 +141,11 @@ FwdPlan fwd_plan(const pam_diff_attn_desc_t &d)
         f.rows = 32;
         const int64_t tiles = ceil_div((int64_t)(d.heads / d.kv_heads) * d.len_q, 32);
         // a block's four waves take a part each already
-        f.plan = plan_of(tiles, (int64_t)d.kv_heads * f.value_parts, d.batch, kCUs, ceil_div(d.len_k, 128), 2, false, false);
+        f.plan = plan_of(tiles, (int64_t)d.kv_heads * f.value_parts, d.batch, kCUs, ceil_div(d.len_k, 128), 2, 2, false, false);
     } else {
         f.rows = 128;
         f.plan = plan_of(ceil_div(d.len_q, 128), (int64_t)d.heads * f.value_parts, d.batch, at_once(d),
-                         ceil_div(d.len_k, 64), 4, causal, d.dtype == PAM_F32);
+                         ceil_div(d.len_k, 64), 4, d.dtype == PAM_F32 ? 1 : 4, causal, d.dtype == PAM_F32);
     }
     return f;
 }
@@ -156,10 +160,10 @@ BwdPlan bwd_plan(const pam_diff_attn_desc_t &d)
     BwdPlan p;
     const bool causal = d.flags & PAM_ATTN_CAUSAL;
     const int cls = attn_class(d.dim, d.dim_v), dp = cls == 0 ? 32 : (cls == 1 ? 64 : 128);
-    p.rows = plan_of(ceil_div(d.len_q, 128), d.heads, d.batch, at_once(d), ceil_div(d.len_k, 64), 4,
-                     causal, d.dtype == PAM_F32);
+    p.rows = plan_of(ceil_div(d.len_q, 128), d.heads, d.batch, at_once(d), ceil_div(d.len_k, 64), 4, 1, causal,
+                     d.dtype == PAM_F32);
     p.keys = plan_of(ceil_div(d.len_k, 128), d.kv_heads, d.batch, at_once(d),
-                     ceil_div(d.len_q, 32) * (d.heads / d.kv_heads), 8, causal, d.dtype == PAM_F32);
+                     ceil_div(d.len_q, 32) * (d.heads / d.kv_heads), 8, 2, causal, d.dtype == PAM_F32);
     p.stats = 4 * (int64_t)d.batch * d.heads * d.len_q;
     p.dlam = (int64_t)p.rows.items() * 4;
     p.row_part = (int64_t)p.rows.slots() * 128 * 2 * dp;

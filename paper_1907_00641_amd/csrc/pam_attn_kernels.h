@@ -514,7 +514,7 @@ __device__ __forceinline__ void join_row(const AttnArgs &a, int parts, const Get
 // What bounds it is reading the cache: every wave has two tiles of 32 keys under
 // way (bf16, 8 x 16384 keys, 8 key heads of 64, 32 query heads: 108 us, 5.0 TB/s,
 // joining included).  A short cache is bound by the steps' latency: 300 keys, three
-// steps of a wave, 11.5 us.
+// steps of a wave, 10.5 us.
 template <class T, int DP, int DVP, bool WIDE>
 __global__ __launch_bounds__((64 * Sizes<T, DP, DVP>::kFewWaves)) void k_attn_few(AttnArgs a)
 {
