@@ -639,10 +639,12 @@ def pam_rotary(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, *, 
     pt = _shaped_ptr(table, table.shape, torch.float32, dev, "table")
     pp = _shaped_ptr(pos, (B, n), torch.int32, dev, "pos")
     if out is None:
-        out = _new(stream, lambda: (q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)))
-    qo, ko = out
-    pqo = _shaped_ptr(qo, q.shape, dt, dev, "q_out")
-    pko = None if k is None else _shaped_ptr(ko, k.shape, dt, dev, "k_out")
+        qo, ko = _new(stream, lambda: (q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)))
+        pqo, pko = qo.data_ptr(), None if k is None else ko.data_ptr()
+    else:
+        qo, ko = out
+        pqo = _shaped_ptr(qo, q.shape, dt, dev, "q_out")
+        pko = None if k is None else _shaped_ptr(ko, k.shape, dt, dev, "k_out")
     _check(lib().pam_rotary(ctypes.byref(desc), pq, pk, pt, pp, pqo, pko, _stream_ptr(stream)), "pam_rotary")
     return qo, ko
 
@@ -654,8 +656,10 @@ def pam_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, out: torc
     code, dev = _dtype_of(x, "x"), _device_of(x, "x")
     px = _shaped_ptr(x, x.shape, x.dtype, dev, "x")
     if out is None:
-        out = _new(stream, lambda: torch.empty_like(x))
-    po = _shaped_ptr(out, x.shape, x.dtype, dev, "out")
+        out = _new(stream, lambda: x.new_empty(x.shape))
+        po = out.data_ptr()
+    else:
+        po = _shaped_ptr(out, x.shape, x.dtype, dev, "out")
     _check(lib().pam_dropout(px, x.numel(), code, p, seed, offset, po, _stream_ptr(stream)), "pam_dropout")
     return out
 

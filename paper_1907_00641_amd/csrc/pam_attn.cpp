@@ -141,7 +141,8 @@ FwdPlan fwd_plan(const pam_diff_attn_desc_t &d)
         f.rows = 32;
         const int64_t tiles = ceil_div((int64_t)(d.heads / d.kv_heads) * d.len_q, 32);
         // a block's four waves take a part each already
-        f.plan = plan_of(tiles, (int64_t)d.kv_heads * f.value_parts, d.batch, kCUs, ceil_div(d.len_k, 128), 2, 2, false, false);
+        f.plan = plan_of(tiles, (int64_t)d.kv_heads * f.value_parts, d.batch, kCUs, ceil_div(d.len_k, 128), 2,
+                         d.dtype == PAM_F32 ? 1 : 2, false, false);
     } else {
         f.rows = 128;
         f.plan = plan_of(ceil_div(d.len_q, 128), (int64_t)d.heads * f.value_parts, d.batch, at_once(d),
