@@ -214,6 +214,27 @@ def test_attention_hidden_places_may_hold_anything(t, lq):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,dv", [(64, 128), (128, 256), (20, 40)])
+@pytest.mark.parametrize("lq,causal", [(200, False), (200, True), (3, False)])
+def test_attention_hidden_places_of_every_class(t, d, dv, lq, causal):
+    """As above, for the other classes of head sizes, and over an axis that is cut into parts."""
+    import torch
+
+    c = Case(79, 2, lq, 330, 4, 2, d, dv, t, causal=causal, k_len=[330, 201], q_len=[lq, max(lq - 90, 1)], mask=0.3)
+    want = c.run()
+    hide = torch.from_numpy(~c.mask).cuda()
+    hide[1, 201:] = True
+    c.k[hide], c.v[hide] = float("nan"), float("inf")
+    c.k[1, 220:] = -float("inf")
+    c.v[1, 230:] = float("nan")
+    c.q[1, max(lq - 90, 1):], c.g[1, max(lq - 90, 1):] = float("nan"), float("inf")
+    got = c.run()
+    for a, b in zip([want[0], *want[1], *want[2]], [got[0], *got[1], *got[2]]):
+        assert torch.equal(a, b)
+    c.compare(*want)
+
+
 def test_attention_visible_nan_is_seen():
     """A NaN value that a row does see makes that row NaN and no other."""
     import torch
