@@ -134,15 +134,25 @@ FwdPlan fwd_plan(const pam_diff_attn_desc_t &d)
     const int cls = attn_class(d.dim, d.dim_v);
     f.dvp = cls == 0 ? 64 : 128;
     f.value_parts = (int)ceil_div(d.dim_v, f.dvp);
-    // a block of 128 rows of one head would be half empty
-    f.few = d.len_q <= 64;
+    // The kernel for few queries: a block of 128 rows of one head would be half
+    // empty, or (16-bit types) all its blocks of 32 rows fit the card at once and
+    // the keys are few, so that nothing has to be cut and joined (bf16, 1 x 500, 8
+    // heads of 64: 22 us for 26; 4 x 500, of 32: 18 for 27; but 1 x 1000, 4 of 64,
+    // 30 for 27), or it still has more blocks for the same cut (100 x 2000, 8/2
+    // heads: 24 for 28).
+    const bool half = d.dtype != PAM_F32;
+    const int64_t tiles = ceil_div((int64_t)(d.heads / d.kv_heads) * d.len_q, 32),
+                  blocks = tiles * d.kv_heads * d.batch * f.value_parts;
+    const bool empty = d.len_q <= 64 || (half && cls < 2 && d.len_q <= 128 && blocks <= 32);
+    const bool whole = !empty && half && blocks <= (cls == 0 ? 2 : 1) * kCUs &&
+                       d.len_k <= (cls == 0 ? 1024 : (cls == 1 ? 768 : 384));
+    f.few = empty || whole;
     const bool causal = d.flags & PAM_ATTN_CAUSAL;
     if (f.few) {
         f.rows = 32;
-        const int64_t tiles = ceil_div((int64_t)(d.heads / d.kv_heads) * d.len_q, 32);
         // a block's four waves take a part each already
-        f.plan = plan_of(tiles, (int64_t)d.kv_heads * f.value_parts, d.batch, kCUs, ceil_div(d.len_k, 128), 2,
-                         d.dtype == PAM_F32 ? 1 : 2, false, false);
+        f.plan = plan_of(tiles, (int64_t)d.kv_heads * f.value_parts, d.batch, kCUs, whole ? 1 : ceil_div(d.len_k, 128),
+                         2, half ? 2 : 1, false, false);
     } else {
         f.rows = 128;
         f.plan = plan_of(ceil_div(d.len_q, 128), (int64_t)d.heads * f.value_parts, d.batch, at_once(d),

@@ -157,6 +157,10 @@ PART_SHAPES = [  # few tiles over a long axis, cut into parts that are joined
     (1, 150, 520, 2, 1, 128, 256),
     (1, 700, 300, 2, 2, 40, 80),
     (13, 140, 300, 20, 20, 8, 16),  # whole rounds of blocks, and then some
+    (1, 140, 1100, 2, 2, 32, 64),
+    (1, 300, 800, 4, 2, 64, 128),
+    (2, 100, 1500, 3, 1, 40, 80),  # the kernel for few queries, cut
+    (3, 250, 250, 14, 2, 64, 100),
 ]
 
 
