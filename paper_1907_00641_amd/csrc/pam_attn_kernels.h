@@ -329,7 +329,7 @@ constexpr uint64_t kAllSeen = KT == 64 ? ~0ull : (1ull << KT) - 1;
 // probabilities never leave the registers: the scores' layout, rounded, is the
 // operand of the second product.  They are rounded to the activations' type
 // for it, before they are divided by their sum (by a relative 2^-9 at most in bf16,
-// and at random: less than rounding the output takes); the sums are of the 32-bit
+// and at random: about what rounding the output takes); the sums are of the 32-bit
 // values.
 // Head sizes over 64 take the values' channels 128 at a time (a.value_parts):
 // both maps' sums of 256 did not fit the registers, and spilling them cost more
