@@ -161,6 +161,7 @@ PART_SHAPES = [  # few tiles over a long axis, cut into parts that are joined
     (1, 300, 800, 4, 2, 64, 128),
     (2, 100, 1500, 3, 1, 40, 80),  # the kernel for few queries, cut
     (3, 250, 250, 14, 2, 64, 100),
+    (20, 130, 130, 16, 16, 8, 16),  # causal: more than a round, the second blocks of the CUs in reverse
 ]
 
 
@@ -237,6 +238,40 @@ def test_attention_hidden_places_of_every_class(t, d, dv, lq, causal):
     for a, b in zip([want[0], *want[1], *want[2]], [got[0], *got[1], *got[2]]):
         assert torch.equal(a, b)
     c.compare(*want)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("d,dv", [(32, 64), (64, 128), (128, 256), (20, 36)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_many_masked_keys(t, d, dv, causal):
+    """Lengths, masks and NaN in hidden places where the keys are too many for the kernel for few queries."""
+    import torch
+
+    c = Case(80, 3, 150, 1100, 2, 1, d, dv, t, causal=causal, k_len=[1100, 0, 777], q_len=[150, 150, 41], mask=0.4)
+    want = c.run()
+    c.compare(*want)
+    hide = torch.from_numpy(~c.mask).cuda()
+    hide[2, 777:] = True
+    c.k[hide], c.v[hide] = float("nan"), float("inf")
+    c.k[1], c.v[1] = float("inf"), float("nan")
+    c.q[2, 41:], c.g[2, 41:] = float("nan"), float("inf")
+    got = c.run()
+    for a, b in zip([want[0], *want[1], *want[2]], [got[0], *got[1], *got[2]]):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+def test_attention_many_keys_at_odd_strides(t):
+    """Rows that start anywhere, NaN between them."""
+    import torch
+
+    c = Case(81, 1, 200, 1200, 3, 1, 40, 72, t, causal=True)
+    for name in ("q", "k", "v"):
+        x = getattr(c, name)
+        wide = torch.full((*x.shape[:-1], x.shape[-1] + 5), float("nan"), dtype=x.dtype, device="cuda")
+        wide[..., 3:-2] = x
+        setattr(c, name, wide[..., 3:-2])
+    c.compare(*c.run())
 
 
 def test_attention_visible_nan_is_seen():
