@@ -572,6 +572,7 @@ def test_dropout_elements_past_32_bits():
 NORM_SHAPES = [  # rows, channels, gate rows (0: none)
     (1, 1, 0), (5, 18, 0), (24, 64, 8), (12, 75, 4), (33, 128, 33), (40, 256, 1), (10, 512, 5), (6, 771, 3),
     (9, 1024, 0), (4, 2048, 2), (5, 4096, 0), (3, 8192, 3), (3, 8001, 1), (2500, 32, 2), (1500, 40, 1), (700, 16, 350),
+    (300, 8192, 1), (520, 4099, 2), (1100, 700, 1), (900, 1600, 1),  # more gate rows than blocks
 ]
 
 
