@@ -249,11 +249,13 @@ struct Queries {
                     o[m][v] *= f;
             }
             const float base = top[m] == -INFINITY ? 0.0f : top[m] - kLift<T>;
+            float add = 0.0f;  // a step's sum first: shorter chains of rounded additions
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[m][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][r], c, -base));
-                sum[m] += s[m][r];
+                add += s[m][r];
             }
+            sum[m] += add;
 #pragma unroll
             for (int x = 0; x < S::CP; ++x)
                 p[m][x] = operand<T>(s[m], x);
@@ -847,15 +849,17 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 if (some_hidden || j0 + 32 > wall)
                     hide(s, (uint32_t)(seen >> (32 * kt)) & low_bits(limit - j0));
                 uint4v ds[2][S::CP];
+                float add = 0.0f;  // a step's sum first: shorter chains of rounded additions
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][r], c, -lse[m]));
                         if (m == 1)
-                            dlam = __builtin_fmaf(p, dp[r], dlam);
+                            add = __builtin_fmaf(p, dp[r], add);
                         s[m][r] = p * (dp[r] - D[m]);
                     }
+                dlam += add;
                 if constexpr (std::is_same<T, f16>::value)
                     range.fit(s, [&](float f) {
 #pragma unroll
