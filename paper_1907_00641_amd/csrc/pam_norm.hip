@@ -174,10 +174,11 @@ struct Team {
 };
 
 // t to N(t) in place (0 outside the row); returns the reciprocal deviation.
-// The mean is taken out before the squares are summed.
+// The mean is taken out before the squares are summed.  `ok` false: the team has no
+// row, t is 0 and stays 0, also with eps 0, since the vectors' sums run over it.
 template <class TM>
-__device__ __forceinline__ float normalise(const TM &tm, bool layer, float (&t)[8], float eps, float inv_c, float *lds,
-                                           int &turn)
+__device__ __forceinline__ float normalise(const TM &tm, bool ok, bool layer, float (&t)[8], float eps, float inv_c,
+                                           float *lds, int &turn)
 {
     if (layer) {
         float s = 0.0f;
@@ -193,7 +194,8 @@ __device__ __forceinline__ float normalise(const TM &tm, bool layer, float (&t)[
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         s += t[j] * t[j];
-    const float rd = 1.0f / __builtin_sqrtf(tm.sum(s, lds, turn) * inv_c + eps);
+    const float deviation = __builtin_sqrtf(tm.sum(s, lds, turn) * inv_c + eps);
+    const float rd = ok ? 1.0f / deviation : 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         t[j] *= rd;
@@ -269,7 +271,7 @@ __global__ __launch_bounds__((W > 4 ? 64 * W : 256)) void k_norm_fwd(NormArgs a)
         fetch(row + step);
         if (a.z) {
             const uint32_t bits = a.dropping ? tm.kept_bits(a.drop, row) : 255u;
-            normalise(tm, a.layer, u, a.eps, inv_c, lds, turn);
+            normalise(tm, ok, a.layer, u, a.eps, inv_c, lds, turn);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float y = u[j] * k1[j] + k0[j];
@@ -282,7 +284,7 @@ __global__ __launch_bounds__((W > 4 ? 64 * W : 256)) void k_norm_fwd(NormArgs a)
                 tm.store((T *)a.r + row * a.channels, x);
         }
         if (a.h) {
-            normalise(tm, a.layer, x, a.eps, inv_c, lds, turn);
+            normalise(tm, ok, a.layer, x, a.eps, inv_c, lds, turn);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 x[j] = x[j] * wp[j] + bp[j];
@@ -394,8 +396,8 @@ __global__ __launch_bounds__((W > 4 ? 64 * W : 256)) void k_norm_bwd(NormArgs a)
             float rz = 0.0f;
             uint32_t bits = 0;
             if (a.z) {
-                bits = a.dropping ? tm.kept_bits(a.drop, row) : 255u;
-                rz = normalise(tm, a.layer, n, a.eps, inv_c, lds, turn);
+                bits = !ok ? 0u : (a.dropping ? tm.kept_bits(a.drop, row) : 255u);
+                rz = normalise(tm, ok, a.layer, n, a.eps, inv_c, lds, turn);
                 float y[8], b[8];
                 tm.take(k1, y);
                 tm.take(k0, b);
@@ -410,12 +412,12 @@ __global__ __launch_bounds__((W > 4 ? 64 * W : 256)) void k_norm_bwd(NormArgs a)
                 }
             }
             if (a.grad_h) {
-                const float rr = normalise(tm, a.layer, x, a.eps, inv_c, lds, turn);
+                const float rr = normalise(tm, ok, a.layer, x, a.eps, inv_c, lds, turn);
                 float m[8];
                 tm.take(wp, m);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    P1[j] += d[j] * x[j];  // 0 past the last row: so is d
+                    P1[j] += d[j] * x[j];  // both are 0 past the last row
                     P0[j] += d[j];
                     d[j] *= m[j];
                 }
@@ -436,7 +438,7 @@ __global__ __launch_bounds__((W > 4 ? 64 * W : 256)) void k_norm_bwd(NormArgs a)
             if (a.z) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float t = ok && (bits >> j & 1) ? d[j] * a.drop.keep : 0.0f;
+                    const float t = (bits >> j & 1) ? d[j] * a.drop.keep : 0.0f;
                     T1[j] += t * n[j];
                     T0[j] += t;
                     d[j] = t;

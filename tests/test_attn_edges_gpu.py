@@ -1,0 +1,60 @@
+"""Edges of the operators around an attention layer against the 64-bit oracle
+(bounds: tests/test_attn_gpu.py)."""
+import numpy as np
+import pytest
+
+from helpers import log
+from oracle import attn as A
+from test_attn_gpu import TINY, U, _cuda, check, dev  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------
+# norms, gate, residual scale
+# ---------------------------------------------------------------------------
+
+def norm_case(n, c, gate_rows, norm, t, eps, p=0.0, with_z=True, seed=0):
+    """Forward and backward of one call against the oracle."""
+    import paper_1907_00641_amd as P
+
+    rng = np.random.default_rng(seed)
+    T, H = {}, {}
+    T["x"], H["x"] = dev(2 * rng.standard_normal((n, c)), t)
+    if with_z:
+        T["z"], H["z"] = dev(rng.standard_normal((n, c)), t)
+        if gate_rows:
+            T["gate"], H["gate"] = dev(rng.standard_normal((n // gate_rows, c)), t)
+    vecs = [("w_post", 1), ("b_post", 0), ("scale", 0.5)] if with_z else []
+    for k, mid in vecs + [("w_pre", 1), ("b_pre", 0)]:
+        T[k], H[k] = dev(mid + 0.3 * rng.standard_normal(c))
+    dr, drh = dev(rng.standard_normal((n, c)), t)
+    dh, dhh = dev(rng.standard_normal((n, c)), t)
+    drop = dict(p=p, seed=99, offset=1 << 40)
+    m = A.dropout_factors(n * c, p, 99, 1 << 40).reshape(n, c) if p else None
+    full = {k: H.get(k) for k in ("x", "z", "w_post", "b_post", "gate", "scale", "w_pre", "b_pre")}
+    res, mag = A.norm_gate(**full, layer=norm == "layer", eps=float(np.float32(eps)), m=m, grad_r=drh, grad_h=dhh)
+    how = dict(norm=norm, eps=eps, **drop, **{k: v for k, v in T.items() if k != "x"})
+    r, h = P.pam_norm_gate_fwd(T["x"], **how)
+    grads = P.pam_norm_gate_bwd(T["x"], grad_r=dr, grad_h=dh, **how)
+    u, e = U[t], 256 * 2.0 ** -24
+    for name, y in (("r", r), ("h", h)):
+        if y is not None:
+            check(name, y, res[name], u * np.abs(res[name]) + e * mag[name] + TINY[t])
+    for k in T:
+        vec = k not in ("x", "z", "gate")
+        bound = (0 if vec else u) * np.abs(res[k]) + (e + (n * 2.0 ** -24 if vec or k == "gate" else 0)) * mag[k]
+        check("d" + k, grads[k], res[k], bound + (TINY[t] if not vec else 0))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("n,c,gate_rows,with_z", [
+    (33, 64, 0, True), (33, 64, 11, True), (33, 64, 0, False),  # 32 teams a block, the last trip with one row
+    (7, 500, 0, True), (9, 771, 3, True), (5, 1024, 0, False),  # two and four teams, rows that start anywhere
+    (2501, 40, 1, True), (1502, 40, 2, True),                   # gate rows dealt whole to the teams, the last without
+], ids=str)
+def test_norm_without_eps(n, c, gate_rows, with_z, norm, t):
+    """eps 0: rows that are not zero have well-defined results, and teams without a row add nothing to the sums."""
+    log(f"[norm eps=0] {n}x{c} gate rows {gate_rows} {norm} {t} z={with_z}")
+    norm_case(n, c, gate_rows, norm, t, 0.0, with_z=with_z, seed=n)
