@@ -275,6 +275,9 @@ struct Queries {
         for (int m = 0; m < 2; ++m)
             sum[m] = xor32_add(sum[m]);
     }
+    // A channel's sum, after whole_sums.  A query that saw nothing has 0 times its
+    // tiles' values there, which others may see and which need not be finite.
+    __device__ __forceinline__ float value(int m, int v, int r) const { return sum[m] != 0.0f ? o[m][v][r] : 0.0f; }
     // unnormalised sums and statistics of this lane's query, for a later join:
     // o as [map][DVP], then the tops and sums
     __device__ __forceinline__ void leave(float *sums, float *stats) const
@@ -287,7 +290,7 @@ struct Queries {
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
                     *reinterpret_cast<float4v *>(sums + m * DVP + 32 * v + 8 * g + 4 * (l >> 5)) =
-                        float4v{o[m][v][4 * g], o[m][v][4 * g + 1], o[m][v][4 * g + 2], o[m][v][4 * g + 3]};
+                        float4v{value(m, v, 4 * g), value(m, v, 4 * g + 1), value(m, v, 4 * g + 2), value(m, v, 4 * g + 3)};
         if (l < 32)
             *reinterpret_cast<float4v *>(stats) = float4v{top[0], top[1], sum[0], sum[1]};
     }
@@ -431,8 +434,8 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 float x0[4], x1[4], y[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    x0[j] = Q.o[0][v][4 * g + j] * inv[0];
-                    x1[j] = Q.o[1][v][4 * g + j] * inv[1];
+                    x0[j] = Q.value(0, v, 4 * g + j) * inv[0];
+                    x1[j] = Q.value(1, v, 4 * g + j) * inv[1];
                     y[j] = x0[j] - lam * x1[j];
                 }
                 const int ch = 32 * v + 8 * g + 4 * (l >> 5);

@@ -5,9 +5,44 @@ import pytest
 
 from helpers import log
 from oracle import attn as A
-from test_attn_gpu import TINY, U, _cuda, check, dev  # noqa: F401
+from test_attn_gpu import TINY, U, Case, _cuda, check, dev, host  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------
+# differential attention
+# ---------------------------------------------------------------------------
+
+CLASSES = [(32, 64), (64, 128), (128, 256), (20, 36)]
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,dv", CLASSES)
+@pytest.mark.parametrize("lq,causal", [(40, False), (200, False), (200, True), (3, False), (3, True)])
+def test_attention_rows_without_keys_beside_values_that_are_not_finite(t, d, dv, lq, causal):
+    """NaN and infinities in values that some rows see: rows past q_len and rows that see nothing are 0 all the same,
+    in one piece and joined from parts."""
+    import paper_1907_00641_amd as P
+
+    log(f"[attn nothing seen] d={d} {dv} lq={lq} {t} causal={causal}")
+    for lk in (70, 900):
+        # causal: the last sequence has fewer keys than queries, so that its first rows see nothing
+        few = min(lq // 2, lk // 2)
+        c = Case(90, 3, lq, lk, 2, 1, d, dv, t, causal=causal, q_len=[lq, (lq + 1) // 2, lq], k_len=[lk, lk, few])
+        c.v[:, 0, :, 1], c.v[1, 3, :, 2], c.v[:, few - 1, :, 4] = float("nan"), float("inf"), -float("inf")
+        out, (o, lse) = P.pam_diff_attn_fwd(c.q, c.k, c.v, c.lam, save=True, **c.how)
+        nothing = ~c.see.any(axis=2)
+        assert nothing[1].any() and (nothing[2].any() or not causal)
+        assert not host(out)[nothing].any() and not host(o)[:, nothing].any()
+        assert np.isneginf(host(lse).transpose(0, 1, 3, 2)[:, nothing]).all()
+        # in rows that see every key, the channels that hold them are not finite and the others are
+        finite = np.ones((*nothing.shape, 2, dv), dtype=bool)
+        finite[..., [1, 4]], finite[1, ..., 2] = False, False
+        row = c.see.all(axis=2)
+        assert row[0].any()
+        for got in (host(out), *host(o)):
+            assert np.array_equal(np.isfinite(got)[row], finite[row])
 
 
 # ---------------------------------------------------------------------------
