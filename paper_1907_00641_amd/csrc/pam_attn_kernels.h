@@ -809,6 +809,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 const float x = a.lse[m * a.lse_map + at];
                 lse[m] = x == -INFINITY ? INFINITY : x * kLog2e;
             }
+            D[m] = lse[m] == INFINITY ? 0.0f : D[m];
             if (l < 32 && i < a.len_q && item.part == 0) {
                 float *st = a.stats + ((int64_t)b * a.heads + h) * 4 * a.len_q + i;
                 st[(int64_t)m * a.len_q] = lse[m];
@@ -886,7 +887,9 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             }
         }
         __syncthreads();
-        dlam = lanes_sum<64>(dlam);
+        // A row that sees nothing has sums of 0 times its own grad_out and its tiles' keys
+        // and values, none of which need be finite: it adds nothing, and dq is 0.
+        dlam = lanes_sum<64>(lse[1] == INFINITY ? 0.0f : dlam);
         if (l == 0)
             a.dlam[(item.parts > 1 ? a.plan.full + item.slot : a.plan.unit(b * a.heads + h, item.tile)) * (int64_t)kAttnWaves + w] =
                 dlam;
@@ -901,8 +904,10 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             for (int v = 0; v < S::TK; ++v)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    const float x[4] = {acc[m][v][4 * y] * f, acc[m][v][4 * y + 1] * f, acc[m][v][4 * y + 2] * f,
-                                        acc[m][v][4 * y + 3] * f};
+                    float x[4];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        x[z] = lse[m] == INFINITY ? 0.0f : acc[m][v][4 * y + z] * f;
                     const int ch = 32 * v + 8 * y + 4 * (l >> 5);
                     if (item.parts > 1)
                         store4<float, true>(part + m * DP, ch, DP, x);

@@ -45,6 +45,51 @@ def test_attention_rows_without_keys_beside_values_that_are_not_finite(t, d, dv,
             assert np.array_equal(np.isfinite(got)[row], finite[row])
 
 
+def unseeing_case(t, d, dv, lq, causal):
+    """Queries inside q_len that see no key: for a mask that hides the first keys from causal queries or all keys, for
+    fewer keys than queries, and for none."""
+    import torch
+
+    lk = lq + 130
+    c = Case(91, 4, lq, lk, 4, 2, d, dv, t, causal=causal, mask=0.1, q_len=[lq, lq, lq, lq - 3],
+             k_len=[lk, lq // 2, 0, lk])
+    c.mask[0, :lk - lq // 2] = False  # causal: the first half of the queries see none of the others
+    c.mask[3] = False
+    c.how["key_mask"] = torch.from_numpy(c.mask).cuda()
+    c.see = A.visible(4, lq, lk, causal, c.q_len, c.k_len, c.mask)
+    nothing = ~c.see.any(axis=2)
+    assert nothing[2:].all() and nothing[:2].any() == causal
+    return c, nothing
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,dv", CLASSES)
+@pytest.mark.parametrize("lq,causal", [(45, False), (45, True), (300, False), (300, True)])
+def test_attention_gradients_of_rows_without_keys(t, d, dv, lq, causal):
+    """NaN and infinities in queries, and in their upstream gradients, that see no key: grad_q is 0 there, and nothing
+    else of it, nor grad_lambda, changes by a bit.  The same rows beside keys and values that are not finite."""
+    import torch
+
+    log(f"[attn gradients nothing seen] d={d} {dv} lq={lq} {t} causal={causal}")
+    c, nothing = unseeing_case(t, d, dv, lq, causal)
+    at = torch.from_numpy(nothing).cuda()
+    c.q[at], c.g[at] = 0.0, 0.0
+    out, saved, want = c.run()
+    c.q[at] = float("nan")
+    c.q[2], c.g[at], c.g[3] = float("inf"), float("nan"), -float("inf")
+    out2, saved2, got = c.run()
+    for a, b in zip((out, *saved, want[0], want[3]), (out2, *saved2, got[0], got[3])):
+        assert torch.equal(a, b)
+    assert not host(got[0])[nothing].any()
+    # keys and values that other rows of the sequence see
+    c.k[:, lq // 2 - 3, :, :, 1], c.v[:, lq // 2 - 4, :, 2] = float("inf"), float("nan")
+    c.mask[:2, lq // 2 - 10:lq // 2] = True
+    c.how["key_mask"] = torch.from_numpy(c.mask).cuda()
+    nothing = ~A.visible(*c.see.shape, causal, c.q_len, c.k_len, c.mask).any(axis=2)
+    dq = host(c.run()[2][0])
+    assert not dq[nothing].any() and not np.isfinite(dq).all()
+
+
 # ---------------------------------------------------------------------------
 # norms, gate, residual scale
 # ---------------------------------------------------------------------------
