@@ -163,6 +163,17 @@ __device__ __forceinline__ bool key_seen(const AttnArgs &a, int b, int nk, int j
     return j < nk && (!a.key_mask || a.key_mask[(int64_t)b * a.len_k + j]);
 }
 
+// The first of 128 keys from k0 on of which that is so, nk if there is none; the same in
+// every lane.
+__device__ __forceinline__ int first_key_seen(const AttnArgs &a, int b, int nk, int k0)
+{
+    if (!a.key_mask)
+        return min(k0, nk);
+    const int l = lane_id();
+    const uint64_t lo = __ballot(key_seen(a, b, nk, k0 + l)), hi = __ballot(key_seen(a, b, nk, k0 + 64 + l));
+    return lo ? k0 + __builtin_ctzll(lo) : (hi ? k0 + 64 + __builtin_ctzll(hi) : nk);
+}
+
 // The lowest n of 32 bits.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1; }
 
@@ -957,10 +968,12 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         const int nq = q_len_of(a, b), nk = k_len_of(a, b);
         const int j = k0 + 32 * w + (l & 31);  // this lane's key
         const bool seen = key_seen(a, b, nk, j);
-        // the first query that sees this lane's key, the block's first, the wave's first
+        // the first query that sees this lane's key, one of the block's (the queries
+        // before it may see nothing at all), the first of its tile, the wave's first
         const int off = a.causal ? nk - nq : (1 << 30);
         const int from = seen ? j - off : 0x7fffffff;
-        const int first = max(k0 - off, 0) / QT * QT, wfirst = k0 + 32 * w - off;
+        const int key0 = first_key_seen(a, b, nk, k0);
+        const int lowest = key0 - off, first = max(lowest, 0) / QT * QT, wfirst = k0 + 32 * w - off;
         const bool all = __all(seen);
         const bool wany = __any(seen);
 
@@ -995,7 +1008,7 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         const float lifted = lift / c;  // what the scores' sums start from
 
         // tiles of all heads in one run, loads a tile ahead
-        const int per = nk > k0 && nq > first ? (nq - first + QT - 1) / QT : 0;
+        const int per = key0 < nk && nq > first ? (nq - first + QT - 1) / QT : 0;
         int t0, t1;
         item.range(per * a.group, t0, t1);
         // head and first query of the next tile to load
@@ -1048,9 +1061,10 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             if (t + 1 < t1)
                 issue(buf ^ 1);
             const bool tail = i0 + QT > nq;
-            if (tail) {  // rows past the sequence
-                clear_rows<T, 2 * DP, QT, kAttnWaves>(qb, (1ull << (nq - i0)) - 1);
-                clear_rows<T, DVP, QT, kAttnWaves>(gb, (1ull << (nq - i0)) - 1);
+            if (tail || i0 < lowest) {  // rows past the sequence, or before the first that sees a key of the block
+                const uint32_t live = low_bits(nq - i0) & ~low_bits(lowest - i0);
+                clear_rows<T, 2 * DP, QT, kAttnWaves>(qb, live);
+                clear_rows<T, DVP, QT, kAttnWaves>(gb, live);
                 __syncthreads();
             }
             if (!S::kSkip || (wany && i0 + QT > wfirst)) {
@@ -1139,7 +1153,10 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
         auto put = [&](T *to, float *to_part, const f32x16 &x, int v, int dim, float f) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const float y[4] = {x[4 * g] * f, x[4 * g + 1] * f, x[4 * g + 2] * f, x[4 * g + 3] * f};
+                float y[4];  // a hidden key has sums of 0 times what the queries hold
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+                    y[z] = seen ? x[4 * g + z] * f : 0.0f;
                 const int at = 32 * v + 8 * g + 4 * (l >> 5);
                 if (item.parts > 1)
                     store4<float, true>(to_part, at, 1 << 20, y);

@@ -90,6 +90,33 @@ def test_attention_gradients_of_rows_without_keys(t, d, dv, lq, causal):
     assert not dq[nothing].any() and not np.isfinite(dq).all()
 
 
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,dv", CLASSES)
+@pytest.mark.parametrize("lq,causal", [(45, False), (45, True), (300, False), (300, True)])
+def test_attention_key_gradients_beside_what_is_not_finite(t, d, dv, lq, causal):
+    """NaN and infinities in queries, and in their upstream gradients, that see no key change no bit of grad_k and
+    grad_v; in queries that see some, those of hidden keys are 0 all the same."""
+    import torch
+
+    log(f"[attn key gradients] d={d} {dv} lq={lq} {t} causal={causal}")
+    c, nothing = unseeing_case(t, d, dv, lq, causal)
+    at = torch.from_numpy(nothing).cuda()
+    c.q[at], c.g[at] = 0.0, 0.0
+    c.qh, c.gh = host(c.q), host(c.g)
+    out, saved, want = c.run()
+    c.compare(out, saved, want)
+    c.q[at] = float("nan")
+    c.q[2], c.g[at], c.g[3] = float("inf"), float("nan"), -float("inf")
+    _, _, got = c.run()
+    assert torch.equal(want[1], got[1]) and torch.equal(want[2], got[2])
+    c.g[0, lq - 2:] = float("inf")
+    c.q[1, lq - 2, :, :, 1] = float("nan")
+    _, _, (_, dk, dv_, _) = c.run()
+    unseen = ~c.see.any(axis=1)
+    assert unseen[:2].any() and not host(dk)[unseen].any() and not host(dv_)[unseen].any()
+    assert not np.isfinite(host(dk)[~unseen]).all() and not np.isfinite(host(dv_)[~unseen]).all()
+
+
 # ---------------------------------------------------------------------------
 # norms, gate, residual scale
 # ---------------------------------------------------------------------------
