@@ -53,7 +53,10 @@ bool span_of(const void *p, int32_t dtype, const int64_t *len, const int64_t *st
     return true;
 }
 Span bytes_at(const void *p, int64_t n) { return {(const char *)p, (const char *)p + (p ? n : 0)}; }
-bool meet(const Span &a, const Span &b) { return a.from < b.to && b.from < a.to; }
+bool meet(const Span &a, const Span &b)
+{
+    return a.from < a.to && b.from < b.to && a.from < b.to && b.from < a.to;
+}
 
 pam_status_t check_attn(const pam_diff_attn_desc_t *d)
 {

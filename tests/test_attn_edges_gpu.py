@@ -117,6 +117,25 @@ def test_attention_key_gradients_beside_what_is_not_finite(t, d, dv, lq, causal)
     assert not np.isfinite(host(dk)[~unseen]).all() and not np.isfinite(host(dv_)[~unseen]).all()
 
 
+def test_attention_workspace_of_no_bytes_may_lie_anywhere():
+    """A call that needs no workspace does not look at it."""
+    import ctypes
+
+    import torch
+
+    import paper_1907_00641_amd as P
+    import paper_1907_00641_amd.binding as B
+
+    c = Case(92, 1, 20, 20, 2, 2, 32, 64, "bf16")
+    want = P.pam_diff_attn_fwd(c.q, c.k, c.v, c.lam, **c.how)
+    desc, ptrs, _ = B._diff_attn_desc(c.q, c.k, c.v, c.lam, c.scale, False, None, None, None)
+    d, out = ctypes.byref(desc), torch.empty_like(want)
+    assert B.lib().pam_diff_attn_fwd_workspace(d) == 0
+    st = B.lib().pam_diff_attn_fwd(d, *ptrs, out.data_ptr(), None, None, c.q.data_ptr() + 64, B._stream_ptr(None))
+    assert st == B.PAM_OK, B.last_error()
+    assert torch.equal(out, want)
+
+
 # ---------------------------------------------------------------------------
 # norms, gate, residual scale
 # ---------------------------------------------------------------------------
