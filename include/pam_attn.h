@@ -172,7 +172,8 @@ pam_status_t pam_rotary_table(const double *freq, const float *coord, const int3
  *           token, head; elements), k likewise with kv_heads (NULL with
  *           kv_heads = 0: none).
  *   q_out, k_out : contiguous; they may be q and k themselves if those are
- *           contiguous, and must not overlap otherwise.
+ *           contiguous, and must not overlap otherwise, nor with table or
+ *           pos.
  * 1 <= dim <= 1024, 1 <= pairs <= dim / 2, batch length (heads + kv_heads)
  * dim < 2^40.  Asynchronous.
  */
@@ -225,7 +226,7 @@ typedef enum { PAM_NORM_RMS = 0, PAM_NORM_LAYER = 1 } pam_norm_t;
  *           rows).  NULL: 1.
  *   w_post, b_post, scale, w_pre, b_pre : channels fp32 each, NULL: 1 or 0.
  * 1 <= channels <= PAM_NORM_MAX_CHANNELS, rows channels < 2^40.  r may be x
- * or z if those are contiguous.  Asynchronous.
+ * or z if those are contiguous; outputs overlap nothing else.  Asynchronous.
  */
 typedef struct {
     int32_t dtype;
@@ -254,7 +255,8 @@ size_t pam_norm_gate_bwd_workspace(const pam_norm_desc_t *desc);
  * (contiguous), grad_gate (gate's shape), dtype; grad_w_post, grad_b_post,
  * grad_scale, grad_w_pre, grad_b_pre, channels fp32 each, summed over the rows
  * in a fixed order.  Gradients of what the call has not (z, gate, h NULL) must
- * be NULL.  grad_x may be grad_r.  Asynchronous.
+ * be NULL.  grad_x may be grad_r; outputs overlap nothing else.
+ * Asynchronous.
  */
 pam_status_t pam_norm_gate_bwd(const pam_norm_desc_t *desc, const void *x, const void *z, const float *w_post,
                                const float *b_post, const void *gate, const float *scale, const float *w_pre,

@@ -4,6 +4,9 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <initializer_list>
+
 #include "pam_internal.h"
 
 using namespace pam;
@@ -57,6 +60,13 @@ bool meet(const Span &a, const Span &b)
 {
     return a.from < a.to && b.from < b.to && a.from < b.to && b.from < a.to;
 }
+bool meet_any(const Span &a, std::initializer_list<Span> with)
+{
+    for (const Span &b : with)
+        if (meet(a, b))
+            return true;
+    return false;
+}
 
 pam_status_t check_attn(const pam_diff_attn_desc_t *d)
 {
@@ -76,8 +86,14 @@ pam_status_t check_attn(const pam_diff_attn_desc_t *d)
     return PAM_OK;
 }
 
-pam_status_t attn_spans(const pam_diff_attn_desc_t *d, const void *q, const void *k, const void *v, Span in[3])
+constexpr int kAttnInputs = 7;
+pam_status_t attn_spans(const pam_diff_attn_desc_t *d, const void *q, const void *k, const void *v, const void *lambda,
+                        const int32_t *q_len, const int32_t *k_len, const uint8_t *key_mask, Span in[kAttnInputs])
 {
+    in[3] = bytes_at(lambda, d->heads * bytes_of(d->dtype));
+    in[4] = bytes_at(q_len, d->batch * (int64_t)sizeof(int32_t));
+    in[5] = bytes_at(k_len, d->batch * (int64_t)sizeof(int32_t));
+    in[6] = bytes_at(key_mask, (int64_t)d->batch * d->len_k);
     const int64_t ql[4] = {d->batch, d->len_q, d->heads, 2}, kl[4] = {d->batch, d->len_k, d->kv_heads, 2};
     REQUIRE(span_of(q, d->dtype, ql, d->q_stride, 4, d->dim, &in[0]) &&
                 span_of(k, d->dtype, kl, d->k_stride, 4, d->dim, &in[1]) &&
@@ -128,8 +144,8 @@ pam_status_t pam_diff_attn_fwd(const pam_diff_attn_desc_t *desc, const void *q, 
     REQUIRE(!saved_o == !saved_lse, "saved_o and saved_lse must be given together");
     const size_t ws = attn_fwd_workspace(*desc);
     REQUIRE(ws == 0 || (workspace && (uintptr_t)workspace % 16 == 0), "workspace is NULL or not 16-byte aligned");
-    Span in[3];
-    if ((st = attn_spans(desc, q, k, v, in)) != PAM_OK)
+    Span in[kAttnInputs];
+    if ((st = attn_spans(desc, q, k, v, lambda, q_len, k_len, key_mask, in)) != PAM_OK)
         return st;
     const int64_t ob = rows * desc->dim_v * bytes_of(desc->dtype);
     const Span outs[4] = {bytes_at(out, ob), bytes_at(saved_o, 2 * ob), bytes_at(saved_lse, rows * 8),
@@ -163,15 +179,15 @@ pam_status_t pam_diff_attn_bwd(const pam_diff_attn_desc_t *desc, const void *q, 
     const size_t ws = attn_bwd_workspace(*desc);
     REQUIRE(ws == 0 || (workspace && (uintptr_t)workspace % 16 == 0), "workspace is NULL or not 16-byte aligned");
     const int64_t e = bytes_of(desc->dtype);
-    Span in[6];
-    if ((st = attn_spans(desc, q, k, v, in)) != PAM_OK)
+    Span in[kAttnInputs + 3] = {};
+    if ((st = attn_spans(desc, q, k, v, lambda, q_len, k_len, key_mask, in)) != PAM_OK)
         return st;
-    in[3] = in[4] = in[5] = bytes_at(nullptr, 0);
     if (rows) {
         const int64_t ol[3] = {desc->batch, desc->len_q, desc->heads};
-        REQUIRE(span_of(grad_out, desc->dtype, ol, do_stride, 3, desc->dim_v, &in[3]), "strides reach too far");
-        in[4] = bytes_at(saved_o, 2 * rows * desc->dim_v * e);
-        in[5] = bytes_at(saved_lse, rows * 8);
+        REQUIRE(span_of(grad_out, desc->dtype, ol, do_stride, 3, desc->dim_v, &in[kAttnInputs]),
+                "strides reach too far");
+        in[kAttnInputs + 1] = bytes_at(saved_o, 2 * rows * desc->dim_v * e);
+        in[kAttnInputs + 2] = bytes_at(saved_lse, rows * 8);
     }
     const Span outs[5] = {bytes_at(grad_q, rows * 2 * desc->dim * e), bytes_at(grad_k, keys * 2 * desc->dim * e),
                           bytes_at(grad_v, keys * desc->dim_v * e), bytes_at(grad_lambda, desc->heads * e),
@@ -233,6 +249,9 @@ pam_status_t pam_rotary_table(const double *freq, const float *coord, const int3
         return PAM_OK;
     REQUIRE(freq && table, "a pointer is NULL");
     REQUIRE((uintptr_t)freq % 8 == 0 && (uintptr_t)table % 8 == 0, "freq and table must be 8-byte aligned");
+    REQUIRE(!meet_any(bytes_at(table, entries * pairs * 8),
+                      {bytes_at(freq, 8ll * pairs), bytes_at(coord, entries * axes * 4), bytes_at(axis, 4ll * pairs)}),
+            "table overlaps an input");
     LAUNCH(launch_rotary_table(freq, coord, axis, entries, pairs, axes, magnitude, table, (hipStream_t)stream),
            "rotary table");
     return PAM_OK;
@@ -275,6 +294,10 @@ pam_status_t pam_rotary(const pam_rotary_desc_t *desc, const void *q, const void
     REQUIRE(!meet(outs[0], in[0]) || (q == q_out && contiguous(d.q_stride, d.heads)), "q_out overlaps q");
     REQUIRE(!meet(outs[1], in[1]) || (k == k_out && contiguous(d.k_stride, d.kv_heads)), "k_out overlaps k");
     REQUIRE(!meet(outs[0], in[1]) && !meet(outs[1], in[0]) && !meet(outs[0], outs[1]), "outputs overlap");
+    // a table of which no entry past 2^40 is reached counts as that long
+    const Span st = bytes_at(table, std::min(d.entries, (int64_t)1 << 40) * d.pairs * 8),
+               sp = bytes_at(pos, (int64_t)d.batch * d.length * 4);
+    REQUIRE(!meet_any(outs[0], {st, sp}) && !meet_any(outs[1], {st, sp}), "an output overlaps the table or pos");
     LAUNCH(launch_rotary(d, q, k, table, pos, q_out, k_out, (hipStream_t)stream), "rotary positions");
     return PAM_OK;
 }
@@ -322,10 +345,11 @@ pam_status_t pam_norm_gate_fwd(const pam_norm_desc_t *desc, const void *x, const
     REQUIRE(!meet(sr, sx) || (r == x && dense_x), "r overlaps x");
     REQUIRE(!meet(sr, sz) || (r == z && dense_z), "r overlaps z");
     REQUIRE(!meet(shh, sx) && !meet(shh, sz) && !meet(shh, sr), "h overlaps another array");
-    if (gate) {
-        const Span sg = bytes_at(gate, d.rows / d.gate_rows * d.channels * bytes_of(d.dtype));
-        REQUIRE(!meet(sr, sg) && !meet(shh, sg), "an output overlaps the gate");
-    }
+    const int64_t vec = 4ll * d.channels;
+    const std::initializer_list<Span> rest = {
+        bytes_at(gate, gate ? d.rows / d.gate_rows * d.channels * bytes_of(d.dtype) : 0), bytes_at(w_post, vec),
+        bytes_at(b_post, vec), bytes_at(scale, vec), bytes_at(w_pre, vec), bytes_at(b_pre, vec)};
+    REQUIRE(!meet_any(sr, rest) && !meet_any(shh, rest), "an output overlaps the gate or a vector");
     LAUNCH(launch_norm_fwd(d, x, z, w_post, b_post, gate, scale, w_pre, b_pre, r, h, (hipStream_t)stream),
            "norm and gate forward");
     return PAM_OK;
@@ -363,7 +387,7 @@ pam_status_t pam_norm_gate_bwd(const pam_norm_desc_t *desc, const void *x, const
     REQUIRE(none || x, "x is NULL");
     REQUIRE(workspace && (uintptr_t)workspace % 16 == 0, "workspace is NULL or not 16-byte aligned");
     const int64_t len[1] = {d.rows}, dense = d.rows * d.channels * bytes_of(d.dtype), vec = 4ll * d.channels;
-    Span in[5];
+    Span in[9];
     REQUIRE(span_of(x, d.dtype, len, &d.x_stride, 1, d.channels, &in[0]) &&
                 span_of(z, d.dtype, len, &d.z_stride, 1, z ? d.channels : 0, &in[1]),
             "strides reach too far");
@@ -373,12 +397,16 @@ pam_status_t pam_norm_gate_bwd(const pam_norm_desc_t *desc, const void *x, const
     in[3] = bytes_at(grad_h, dense);
     const int64_t gb = gate ? d.rows / d.gate_rows * d.channels * bytes_of(d.dtype) : 0;
     in[4] = bytes_at(gate, gb);
+    in[5] = bytes_at(w_post, vec);
+    in[6] = bytes_at(b_post, vec);
+    in[7] = bytes_at(scale, vec);
+    in[8] = bytes_at(w_pre, vec);
     const Span outs[9] = {bytes_at(grad_x, dense),     bytes_at(grad_z, dense),      bytes_at(grad_gate, gb),
                           bytes_at(grad_w_post, vec),  bytes_at(grad_b_post, vec),   bytes_at(grad_scale, vec),
                           bytes_at(grad_w_pre, vec),   bytes_at(grad_b_pre, vec),
                           bytes_at(workspace, (int64_t)norm_bwd_workspace(d))};
     for (int i = 0; i < 9; ++i) {
-        for (int j = 0; j < 5; ++j)
+        for (int j = 0; j < 9; ++j)
             REQUIRE(!meet(outs[i], in[j]) || (i == 0 && j == 2 && grad_x == grad_r), "an output overlaps an input");
         for (int j = 0; j < i; ++j)
             REQUIRE(!meet(outs[i], outs[j]), "outputs overlap");
