@@ -114,6 +114,14 @@ pam_status_t check_norm(const pam_norm_desc_t *d)
     return PAM_OK;
 }
 
+// z's stride means nothing without z
+pam_norm_desc_t without_z(pam_norm_desc_t d, const void *z)
+{
+    if (!z)
+        d.z_stride = d.x_stride;
+    return d;
+}
+
 }  // namespace
 
 extern "C" {
@@ -324,7 +332,7 @@ pam_status_t pam_norm_gate_fwd(const pam_norm_desc_t *desc, const void *x, const
     pam_status_t st = check_norm(desc);
     if (st != PAM_OK)
         return st;
-    const pam_norm_desc_t &d = *desc;
+    const pam_norm_desc_t d = without_z(*desc, z);
     if (d.rows == 0)
         return PAM_OK;
     REQUIRE(!gate || (d.gate_rows >= 1 && d.rows % d.gate_rows == 0), "gate_rows must divide rows");
@@ -375,7 +383,7 @@ pam_status_t pam_norm_gate_bwd(const pam_norm_desc_t *desc, const void *x, const
     pam_status_t st = check_norm(desc);
     if (st != PAM_OK)
         return st;
-    const pam_norm_desc_t &d = *desc;
+    const pam_norm_desc_t d = without_z(*desc, z);
     REQUIRE(!gate || (d.gate_rows >= 1 && d.rows % d.gate_rows == 0), "gate_rows must divide rows");
     REQUIRE(d.gate_rows >= 0 && (d.gate_rows == 0 || d.rows % d.gate_rows == 0), "gate_rows must divide rows");
     // arrays of no rows may be NULL, and the vectors' gradients are 0 then

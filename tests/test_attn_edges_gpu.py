@@ -184,3 +184,30 @@ def test_norm_without_eps(n, c, gate_rows, with_z, norm, t):
     """eps 0: rows that are not zero have well-defined results, and teams without a row add nothing to the sums."""
     log(f"[norm eps=0] {n}x{c} gate rows {gate_rows} {norm} {t} z={with_z}")
     norm_case(n, c, gate_rows, norm, t, 0.0, with_z=with_z, seed=n)
+
+
+def test_norm_without_z_looks_at_no_stride_of_it():
+    """Both directions through the C ABI, with a z_stride that was never set."""
+    import ctypes
+
+    import torch
+
+    import paper_1907_00641_amd as P
+    import paper_1907_00641_amd.binding as B
+
+    x, g = torch.randn(20, 64, device="cuda").bfloat16(), torch.randn(20, 64, device="cuda").bfloat16()
+    w = torch.rand(64, device="cuda")
+    want = P.pam_norm_gate_fwd(x, w_pre=w)[1]
+    want_x = P.pam_norm_gate_bwd(x, w_pre=w, grad_r=None, grad_h=g)["x"]
+    h, gx = torch.empty_like(x), torch.empty_like(x)
+    for stride in (1 << 62, -(1 << 62), 3):
+        d = B.NormDesc(2, 0, 20, 64, 1e-6, 0, 64, stride, 0.0, 0, 0)
+        at = ctypes.byref(d)
+        st = B.lib().pam_norm_gate_fwd(at, x.data_ptr(), *[None] * 5, w.data_ptr(), None, None, h.data_ptr(),
+                                       B._stream_ptr(None))
+        assert st == B.PAM_OK, B.last_error()
+        ws = torch.empty(B.lib().pam_norm_gate_bwd_workspace(at), dtype=torch.uint8, device="cuda")
+        st = B.lib().pam_norm_gate_bwd(at, x.data_ptr(), *[None] * 5, w.data_ptr(), None, g.data_ptr(), gx.data_ptr(),
+                                       *[None] * 7, ws.data_ptr(), B._stream_ptr(None))
+        assert st == B.PAM_OK, B.last_error()
+        assert torch.equal(h, want) and torch.equal(gx, want_x)
