@@ -488,6 +488,12 @@ def _shaped_ptr(t: torch.Tensor | None, shape, dtype, dev: int, name: str) -> in
     raise ValueError(f"{name} must be contiguous")
 
 
+def _counts(*n: int):
+    """Refuses sizes that the C ABI's 32-bit fields would take modulo 2^32."""
+    if max(n) > 0x7FFFFFFF:
+        raise ValueError("a size is 2^31 or more")
+
+
 def _new(stream, make):
     """What ``make`` allocates, on the stream that writes it: memory freed after the
     call is not handed out again while that stream uses it."""
@@ -514,6 +520,7 @@ def _diff_attn_desc(q, k, v, lam, scale, causal, q_len, k_len, key_mask):
     _, lk, hk, dv = v.shape
     if k.shape != (B, lk, hk, 2, d) or v.shape[0] != B:
         raise ValueError("q, k and v do not agree in sequences, lengths, key heads or head size")
+    _counts(B, lq, lk, H, hk, d, dv)
     dt = q.dtype
     code, dev = _dtype_of(q, "q"), _device_of(q, "q")
     ptrs = [_rows_ptr(q, dt, dev, "q"), _rows_ptr(k, dt, dev, "k"), _rows_ptr(v, dt, dev, "v"),
@@ -587,6 +594,7 @@ def pam_rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "plai
     ``scaling`` "plain", "linear", "ntk" or "yarn" for contexts longer than the trained one."""
     if scaling not in ROPE_SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+    _counts(rot)
     freq = torch.empty(max(rot // 2, 1), dtype=torch.float64)
     mag = ctypes.c_double(0.0)
     _check(lib().pam_rotary_frequencies(rot, base, ROPE_SCALINGS[scaling], factor, original_len, beta_slow, beta_fast,
@@ -609,6 +617,7 @@ def pam_rotary_table(freq: torch.Tensor, entries: int | None = None, coord: torc
         entries, axes = coord.shape
     elif entries is None:
         raise ValueError("give entries or coord")
+    _counts(pairs, axes)
     dev = _device_of(freq, "freq")
     pf = _shaped_ptr(freq, (pairs,), torch.float64, dev, "freq")
     pc = _shaped_ptr(coord, (entries, axes), torch.float32, dev, "coord")
@@ -631,6 +640,9 @@ def pam_rotary(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, *, 
         raise ValueError("table must be entries x pairs x 2")
     B, n, H, d = q.shape
     hk = 0 if k is None else k.shape[2]
+    _counts(B, n, H, hk, d, table.shape[1])
+    if not -(1 << 62) < start < 1 << 62:
+        raise ValueError("start must be less than 2^62 in size")
     flags = (PAM_ROTARY_INTERLEAVED if interleaved else 0) | (PAM_ROTARY_INVERSE if inverse else 0)
     desc = RotaryDesc(_dtype_of(q, "q"), B, n, H, hk, d, table.shape[1], flags, start, table.shape[0],
                       q.stride()[:3], (0, 0, 0) if k is None else k.stride()[:3])
@@ -670,6 +682,7 @@ def _norm_desc(x, z, w_post, b_post, gate, scale, w_pre, b_pre, norm, eps, p, se
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {sorted(NORMS)}")
     n, c = x.shape
+    _counts(c)
     gate_rows = 0
     if gate is not None:
         if gate.dim() != 2 or gate.shape[1] != c or (gate.shape[0] == 0) != (n == 0) or \
