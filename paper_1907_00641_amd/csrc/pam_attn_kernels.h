@@ -1026,12 +1026,12 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             char *to = lds + buf * S::kQueryTile;
             load_rows<T, 2 * DP, 2, QT, kAttnWaves, WIDE>(to, qp, a.qs[1], a.qs[3], nq - 1 - ni, a.dim);
             load_rows<T, DVP, 1, QT, kAttnWaves, WIDE>(to + RK::size(QT), gp, a.dos[1], 0, nq - 1 - ni, a.dim_v);
-            if (w < 2) {  // 4 statistics of 32 queries: a wave takes two of them
-                const int y = again(l);
-                load_lds4(uniform_ptr(sp + 2 * w * (int64_t)a.len_q),
-                          4u * (uint32_t)((y >> 5) * a.len_q + min(y & 31, nq - 1 - ni)),
-                          lds_address(to + RK::size(QT) + RV::size(QT)) + w * 256);
-            }
+            // 4 statistics of 32 queries, one by half of each wave: an offset from one
+            // to the next would pass 32 bits in the longest sequences
+            const int y = again(l);
+            if (y < 32)
+                load_lds4(uniform_ptr(sp + w * (int64_t)a.len_q), 4u * (uint32_t)min(y, nq - 1 - ni),
+                          lds_address(to + RK::size(QT) + RV::size(QT)) + w * 128);
             ni += QT;
             qp = uniform_ptr(qp + QT * a.qs[1]);
             gp = uniform_ptr(gp + QT * a.dos[1]);

@@ -117,6 +117,36 @@ def test_attention_key_gradients_beside_what_is_not_finite(t, d, dv, lq, causal)
     assert not np.isfinite(host(dk)[~unseen]).all() and not np.isfinite(host(dv_)[~unseen]).all()
 
 
+def test_attention_gradients_of_the_longest_sequence():
+    """2^30 - 1 queries of one key: every probability is 1, out is (1 - lam) v, grad_v (1 - lam) times the sum of
+    grad_out, and grad_q and grad_k are 0."""
+    import torch
+
+    import paper_1907_00641_amd as P
+
+    n, lam = (1 << 30) - 1, 0.5
+    if torch.cuda.mem_get_info()[0] < 64 << 30:
+        pytest.skip("needs 64 GB")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(93)
+    half = dict(dtype=torch.float16, device="cuda")
+    q = torch.randn(1, n, 1, 2, 1, generator=gen, **half)
+    k, v = torch.full((1, 1, 1, 2, 1), 1.0, **half), torch.full((1, 1, 1, 1), 0.75, **half)
+    lamt = torch.full((1,), lam, **half)
+    g = torch.zeros(1, n, 1, 1, **half)
+    at = torch.randint(0, n, (1000,), generator=gen, device="cuda").unique()
+    g[0, at] = 1.0
+    out, saved = P.pam_diff_attn_fwd(q, k, v, lamt, save=True)
+    dq, dk, dv, dlam = P.pam_diff_attn_bwd(q, k, v, lamt, saved, g)
+    # a probability is off by e, of a score of magnitude S < 7, and by u where it is rounded
+    u, e, m = U["f16"], 2.0 ** -24 * (2 * 5 * 7 + 17), len(at)
+    assert float((out - (1 - lam) * 0.75).abs().max()) <= (u + (u + e) * 3) * 0.75
+    check("dv", dv, np.full((1, 1, 1, 1), (1 - lam) * m), np.array(u * (1 - lam) * m + (u + e) * (1 + lam) * m))
+    # dp - D: D is taken from o in fp16; |q| < 7, |scale p| <= 1 + lam
+    assert float(dq.abs().max()) <= (2 * u + 3 * e) * 0.75 and float(dk.abs().max()) <= (2 * u + 3 * e) * 0.75 * 7 * m
+    check("dlam", dlam, np.array([-0.75 * m]), np.array([u * 0.75 * m + (2 * e + 2.0 ** -20) * 0.75 * m]))
+
+
 def test_attention_workspace_of_no_bytes_may_lie_anywhere():
     """A call that needs no workspace does not look at it."""
     import ctypes
