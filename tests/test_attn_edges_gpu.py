@@ -1,5 +1,7 @@
 """Edges of the operators around an attention layer against the 64-bit oracle
 (bounds: tests/test_attn_gpu.py)."""
+import functools
+
 import numpy as np
 import pytest
 
@@ -170,6 +172,11 @@ def test_attention_workspace_of_no_bytes_may_lie_anywhere():
 # norms, gate, residual scale
 # ---------------------------------------------------------------------------
 
+@functools.lru_cache(maxsize=4)
+def factors(n, p):
+    return A.dropout_factors(n, p, 99, 1 << 40)
+
+
 def norm_case(n, c, gate_rows, norm, t, eps, p=0.0, with_z=True, seed=0):
     """Forward and backward of one call against the oracle."""
     import paper_1907_00641_amd as P
@@ -187,7 +194,7 @@ def norm_case(n, c, gate_rows, norm, t, eps, p=0.0, with_z=True, seed=0):
     dr, drh = dev(rng.standard_normal((n, c)), t)
     dh, dhh = dev(rng.standard_normal((n, c)), t)
     drop = dict(p=p, seed=99, offset=1 << 40)
-    m = A.dropout_factors(n * c, p, 99, 1 << 40).reshape(n, c) if p else None
+    m = factors(n * c, p).reshape(n, c) if p else None
     full = {k: H.get(k) for k in ("x", "z", "w_post", "b_post", "gate", "scale", "w_pre", "b_pre")}
     res, mag = A.norm_gate(**full, layer=norm == "layer", eps=float(np.float32(eps)), m=m, grad_r=drh, grad_h=dhh)
     how = dict(norm=norm, eps=eps, **drop, **{k: v for k, v in T.items() if k != "x"})
@@ -214,6 +221,16 @@ def test_norm_without_eps(n, c, gate_rows, with_z, norm, t):
     """eps 0: rows that are not zero have well-defined results, and teams without a row add nothing to the sums."""
     log(f"[norm eps=0] {n}x{c} gate rows {gate_rows} {norm} {t} z={with_z}")
     norm_case(n, c, gate_rows, norm, t, 0.0, with_z=with_z, seed=n)
+
+
+@pytest.mark.parametrize("n,c,gate_rows", [(2500, 32, 2), (1500, 40, 1), (800, 77, 1), (1100, 700, 1), (34, 64, 17)],
+                         ids=str)
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_norm_dropout_with_gates(n, c, gate_rows, norm, t):
+    """Dropout with more gate rows than blocks, aligned and not, and with few."""
+    log(f"[norm dropout] {n}x{c} gate rows {gate_rows} {norm} {t}")
+    norm_case(n, c, gate_rows, norm, t, 1e-5, p=0.25, seed=n)
 
 
 def test_norm_without_z_looks_at_no_stride_of_it():
