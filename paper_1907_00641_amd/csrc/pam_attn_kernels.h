@@ -1003,7 +1003,9 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             float most = 0.0f;
             for (int h = h0; h < h1; ++h)
                 most = __builtin_fmaxf(most, __builtin_fabsf((float)((const T *)a.lam)[h]));
-            lift = (float)(14 - __builtin_amdgcn_frexp_expf(1.0f + most));
+            // (with scores so small that what their sums would start from passes 32 bits
+            // there is nothing to lift)
+            lift = c > 0x1p-100f ? (float)(14 - __builtin_amdgcn_frexp_expf(1.0f + most)) : 0.0f;
         }
         const float lifted = lift / c;  // what the scores' sums start from
 

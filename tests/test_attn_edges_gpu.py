@@ -149,6 +149,15 @@ def test_attention_gradients_of_the_longest_sequence():
     check("dlam", dlam, np.array([-0.75 * m]), np.array([u * 0.75 * m + (2 * e + 2.0 ** -20) * 0.75 * m]))
 
 
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("scale", [1e-12, 1e-38, 1e-42])
+def test_attention_scales_near_zero(scale, t):
+    """Every key counts alike; grad_v does not depend on the scores."""
+    log(f"[attn scale] {scale} {t}")
+    c = Case(94, 2, 50, 70, 2, 1, 32, 64, t, causal=True, scale=float(np.float32(scale)))
+    c.compare(*c.run())
+
+
 def test_attention_workspace_of_no_bytes_may_lie_anywhere():
     """A call that needs no workspace does not look at it."""
     import ctypes
