@@ -87,14 +87,14 @@ size_t pam_diff_attn_bwd_workspace(const pam_diff_attn_desc_t *desc);
 
 /*
  * Forward.  For a backward pass give saved_o (2 x batch x len_q x heads x
- * dim_v, dtype: o^0, then o^1) and saved_lse (2 x batch x heads x len_q fp32:
+ * dim_v fp32: o^0, then o^1) and saved_lse (2 x batch x heads x len_q fp32:
  * the logarithms of the softmax sums); both NULL otherwise.  workspace: 16-byte
  * aligned, pam_diff_attn_fwd_workspace bytes, overwritten (NULL if 0).
  * Outputs must not overlap inputs.  Asynchronous.
  */
 pam_status_t pam_diff_attn_fwd(const pam_diff_attn_desc_t *desc, const void *q, const void *k, const void *v,
                                const void *lambda, const int32_t *q_len, const int32_t *k_len,
-                               const uint8_t *key_mask, void *out, void *saved_o, float *saved_lse, void *workspace,
+                               const uint8_t *key_mask, void *out, float *saved_o, float *saved_lse, void *workspace,
                                void *stream);
 
 /*
@@ -114,7 +114,7 @@ pam_status_t pam_diff_attn_fwd(const pam_diff_attn_desc_t *desc, const void *q, 
  */
 pam_status_t pam_diff_attn_bwd(const pam_diff_attn_desc_t *desc, const void *q, const void *k, const void *v,
                                const void *lambda, const int32_t *q_len, const int32_t *k_len,
-                               const uint8_t *key_mask, const void *saved_o, const float *saved_lse,
+                               const uint8_t *key_mask, const float *saved_o, const float *saved_lse,
                                const void *grad_out, const int64_t do_stride[3], void *grad_q, void *grad_k,
                                void *grad_v, void *grad_lambda, void *workspace, void *stream);
 

@@ -552,7 +552,7 @@ def pam_diff_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: to
 
     def make():
         out = q.new_empty(shape)
-        so = q.new_empty((2, *shape)) if save else None
+        so = q.new_empty((2, *shape), dtype=torch.float32) if save else None
         lse = q.new_empty((2, shape[0], shape[2], shape[1]), dtype=torch.float32) if save else None
         return out, so, lse, q.new_empty(ws_bytes, dtype=torch.uint8) if ws_bytes else None
 
@@ -573,7 +573,7 @@ def pam_diff_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lam: to
     L, d = lib(), ctypes.byref(desc)
     shape = (*q.shape[:3], v.shape[3])
     so, lse = saved
-    pso = _shaped_ptr(so, (2, *shape), q.dtype, dev, "saved o")
+    pso = _shaped_ptr(so, (2, *shape), torch.float32, dev, "saved o")
     plse = _shaped_ptr(lse, (2, shape[0], shape[2], shape[1]), torch.float32, dev, "saved lse")
     if grad_out.shape != shape:
         raise ValueError(f"grad_out has shape {tuple(grad_out.shape)}, expected {shape}")

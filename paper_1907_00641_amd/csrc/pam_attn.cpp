@@ -197,7 +197,7 @@ size_t attn_bwd_workspace(const pam_diff_attn_desc_t &d)
 
 hipError_t launch_attn_fwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
                            const void *lam, const int32_t *q_len, const int32_t *k_len, const uint8_t *key_mask,
-                           void *out, void *so, float *lse, void *workspace, hipStream_t s)
+                           void *out, float *so, float *lse, void *workspace, hipStream_t s)
 {
     AttnArgs a = attn_args(d, q, k, v, lam, q_len, k_len, key_mask);
     a.out = out;
@@ -218,11 +218,11 @@ hipError_t launch_attn_fwd(const pam_diff_attn_desc_t &d, const void *q, const v
 
 hipError_t launch_attn_bwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
                            const void *lam, const int32_t *q_len, const int32_t *k_len, const uint8_t *key_mask,
-                           const void *so, const float *lse, const void *dout, const int64_t *dos, void *gq, void *gk,
+                           const float *so, const float *lse, const void *dout, const int64_t *dos, void *gq, void *gk,
                            void *gv, void *glam, void *workspace, hipStream_t s)
 {
     AttnArgs a = attn_args(d, q, k, v, lam, q_len, k_len, key_mask);
-    a.so = const_cast<void *>(so);
+    a.so = const_cast<float *>(so);
     a.lse = const_cast<float *>(lse);
     a.dout = dout;
     for (int i = 0; i < 3; ++i)

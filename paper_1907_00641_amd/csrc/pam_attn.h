@@ -42,7 +42,8 @@ struct AttnArgs {
     float *key_part;
     // forward
     int32_t value_parts;  // of up to 128 channels, each an item of its own
-    void *out, *so;   // so: o^0, then o^1 at so_map elements
+    void *out;
+    float *so;        // o^0, then o^1 at so_map elements
     float *lse;       // of map m at m * lse_map
     int64_t so_map, lse_map;
     // backward

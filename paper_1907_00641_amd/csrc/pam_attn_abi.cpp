@@ -138,7 +138,7 @@ size_t pam_diff_attn_bwd_workspace(const pam_diff_attn_desc_t *desc)
 
 pam_status_t pam_diff_attn_fwd(const pam_diff_attn_desc_t *desc, const void *q, const void *k, const void *v,
                                const void *lambda, const int32_t *q_len, const int32_t *k_len,
-                               const uint8_t *key_mask, void *out, void *saved_o, float *saved_lse, void *workspace,
+                               const uint8_t *key_mask, void *out, float *saved_o, float *saved_lse, void *workspace,
                                void *stream)
 {
     pam_status_t st = check_attn(desc);
@@ -156,7 +156,7 @@ pam_status_t pam_diff_attn_fwd(const pam_diff_attn_desc_t *desc, const void *q, 
     if ((st = attn_spans(desc, q, k, v, lambda, q_len, k_len, key_mask, in)) != PAM_OK)
         return st;
     const int64_t ob = rows * desc->dim_v * bytes_of(desc->dtype);
-    const Span outs[4] = {bytes_at(out, ob), bytes_at(saved_o, 2 * ob), bytes_at(saved_lse, rows * 8),
+    const Span outs[4] = {bytes_at(out, ob), bytes_at(saved_o, rows * desc->dim_v * 8), bytes_at(saved_lse, rows * 8),
                           bytes_at(workspace, (int64_t)ws)};
     for (int i = 0; i < 4; ++i) {
         for (const Span &x : in)
@@ -172,7 +172,7 @@ pam_status_t pam_diff_attn_fwd(const pam_diff_attn_desc_t *desc, const void *q, 
 
 pam_status_t pam_diff_attn_bwd(const pam_diff_attn_desc_t *desc, const void *q, const void *k, const void *v,
                                const void *lambda, const int32_t *q_len, const int32_t *k_len,
-                               const uint8_t *key_mask, const void *saved_o, const float *saved_lse,
+                               const uint8_t *key_mask, const float *saved_o, const float *saved_lse,
                                const void *grad_out, const int64_t do_stride[3], void *grad_q, void *grad_k,
                                void *grad_v, void *grad_lambda, void *workspace, void *stream)
 {
@@ -194,7 +194,7 @@ pam_status_t pam_diff_attn_bwd(const pam_diff_attn_desc_t *desc, const void *q, 
         const int64_t ol[3] = {desc->batch, desc->len_q, desc->heads};
         REQUIRE(span_of(grad_out, desc->dtype, ol, do_stride, 3, desc->dim_v, &in[kAttnInputs]),
                 "strides reach too far");
-        in[kAttnInputs + 1] = bytes_at(saved_o, 2 * rows * desc->dim_v * e);
+        in[kAttnInputs + 1] = bytes_at(saved_o, rows * desc->dim_v * 8);
         in[kAttnInputs + 2] = bytes_at(saved_lse, rows * 8);
     }
     const Span outs[5] = {bytes_at(grad_q, rows * 2 * desc->dim * e), bytes_at(grad_k, keys * 2 * desc->dim * e),

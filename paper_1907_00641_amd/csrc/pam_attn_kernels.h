@@ -452,8 +452,8 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
                 const int ch = 32 * v + 8 * g + 4 * (l >> 5);
                 store4<T, WIDE>((T *)a.out + row, ch, dim_v, y);
                 if (a.so) {
-                    store4<T, WIDE>((T *)a.so + row, ch, dim_v, x0);
-                    store4<T, WIDE>((T *)a.so + a.so_map + row, ch, dim_v, x1);
+                    store4<float, WIDE>(a.so + row, ch, dim_v, x0);
+                    store4<float, WIDE>(a.so + a.so_map + row, ch, dim_v, x1);
                 }
             }
         if (a.lse && l < 32 && v0 == 0) {
@@ -514,8 +514,8 @@ __device__ __forceinline__ void join_row(const AttnArgs &a, int parts, const Get
     }
     put4<T>(a, (T *)a.out + at, ch, dim_v, y);
     if (a.so) {
-        put4<T>(a, (T *)a.so + at, ch, dim_v, x0);
-        put4<T>(a, (T *)a.so + a.so_map + at, ch, dim_v, x1);
+        put4<float>(a, a.so + at, ch, dim_v, x0);
+        put4<float>(a, a.so + a.so_map + at, ch, dim_v, x1);
     }
     if (a.lse && ch == 0 && v0 == 0) {
         const int64_t r = ((int64_t)b * a.heads + h) * a.len_q + i;
@@ -744,10 +744,12 @@ __global__ __launch_bounds__((FEW ? kJoinThreads : kAttnThreads)) void k_attn_jo
 // D, dq and the rows' part of grad_lambda.  Transposed as the forward pass is, so
 // a lane holds one query.  sum_j p^1 dp is taken from the 32-bit probabilities and
 // dp, not from the saved o^1, whose rounding would be all its error.
-// Score gradients are rounded to the activations' type for their product, and D is
-// taken from the saved o, which is of that type: together half as much again as
-// rounding dq itself (bf16: 0.0026 for 0.0017 of its norm; with 32-bit operands
-// the product would take eight times as long).
+// D is taken from o in 32 bits: it is the difference of dp and D that counts, which
+// may be far smaller than either (o rounded to bf16, values around 4 times their
+// deviation: dq off by 0.011 of its norm, dk by 0.009).
+// Score gradients are rounded to the activations' type for their product: about as
+// much again as rounding dq itself (bf16: 0.0024 for 0.0017 of its norm; with 32-bit
+// operands the product would take eight times as long).
 // Bound as the forward pass is: bf16, 8 heads of 64, 2 x 4800: 361 us, 780 TFLOP/s;
 // 16384 causal 937, 880; heads of 128 940 us; fp32, 2197, 4 heads of 32: 79 us.
 template <class T, int DP, int DVP, bool WIDE>
@@ -810,8 +812,9 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
             g[s] = memory_chunk<T, WIDE>(grow, s, a.dim_v, in);
 #pragma unroll
             for (int m = 0; m < 2; ++m)
-                D[m] += piece_dot<T>(g[s], memory_chunk<T, WIDE>((const T *)a.so + m * a.so_map + row * a.dim_v, s,
-                                                                 a.dim_v, in));
+                D[m] += piece_dot<T, WIDE>(g[s], a.so + m * a.so_map + row * a.dim_v, s, a.dim_v, in);
+            if (sizeof(T) == 2 && s % 4 == 3)  // no more of o under way than the registers hold
+                asm volatile("" : "+v"(D[0]), "+v"(D[1]));
         }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {

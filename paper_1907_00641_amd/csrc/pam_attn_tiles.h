@@ -254,23 +254,35 @@ __device__ __forceinline__ uint4v memory_chunk(const T *row, int s, int dim, boo
     return r;
 }
 
-// the values of a chunk piece held by a lane
-template <class T>
-__device__ __forceinline__ float piece_dot(uint4v a, uint4v b)
+// Sum of the products of what memory_chunk gives of a row, its chunk s, with the
+// same channels of a row of 32-bit values.
+template <class T, bool WIDE>
+__device__ __forceinline__ float piece_dot(uint4v a, const float *row, int s, int dim, bool ok)
 {
-    float s = 0.0f;
-    if constexpr (sizeof(T) == 4) {
+    constexpr int per = 16 / sizeof(T);
+    typedef T Tp __attribute__((ext_vector_type(per)));
+    const int c = s * kChunk<T> + (lane_id() >> 5) * per;
+    const Tp x = __builtin_bit_cast(Tp, a);
+    float y[per] = {}, sum = 0.0f;
+    if constexpr (WIDE) {
+        if (ok && c < dim) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            s += __uint_as_float(a[j]) * __uint_as_float(b[j]);
+            for (int j = 0; j < per; j += 4) {
+                const float4v z = *reinterpret_cast<const float4v *>(row + c + j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    y[j + i] = z[i];
+            }
+        }
     } else {
-        typedef T T8 __attribute__((ext_vector_type(8)));
-        const T8 x = __builtin_bit_cast(T8, a), y = __builtin_bit_cast(T8, b);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            s += (float)x[j] * (float)y[j];
+        for (int j = 0; j < per; ++j)
+            y[j] = ok && c + j < dim ? row[c + j] : 0.0f;
     }
-    return s;
+#pragma unroll
+    for (int j = 0; j < per; ++j)
+        sum += (float)x[j] * y[j];
+    return sum;
 }
 
 // Four consecutive channels (registers 4 g .. 4 g + 3 of a result whose rows

@@ -258,10 +258,10 @@ size_t attn_fwd_workspace(const pam_diff_attn_desc_t &d);
 size_t attn_bwd_workspace(const pam_diff_attn_desc_t &d);
 hipError_t launch_attn_fwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
                            const void *lam, const int32_t *q_len, const int32_t *k_len, const uint8_t *key_mask,
-                           void *out, void *so, float *lse, void *workspace, hipStream_t s);
+                           void *out, float *so, float *lse, void *workspace, hipStream_t s);
 hipError_t launch_attn_bwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
                            const void *lam, const int32_t *q_len, const int32_t *k_len, const uint8_t *key_mask,
-                           const void *so, const float *lse, const void *dout, const int64_t *dos, void *gq, void *gk,
+                           const float *so, const float *lse, const void *dout, const int64_t *dos, void *gq, void *gk,
                            void *gv, void *glam, void *workspace, hipStream_t s);
 // rotary positions (pam_rotary.hip)
 hipError_t launch_rotary_table(const double *freq, const float *coord, const int32_t *axis, int64_t entries,

@@ -149,6 +149,35 @@ def test_attention_gradients_of_the_longest_sequence():
     check("dlam", dlam, np.array([-0.75 * m]), np.array([u * 0.75 * m + (2 * e + 2.0 ** -20) * 0.75 * m]))
 
 
+def offset_case(t, d, dv, lq, causal, off=50.0, **kw):
+    """Values around ``off``: dp and D are large, and their difference is that of the values' small parts."""
+    c = Case(95, 2, lq, lq + 90, 4, 2, d, dv, t, causal=causal, **kw)
+    c.v.add_(off)
+    c.vh = host(c.v)
+    return c
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,dv", CLASSES)
+@pytest.mark.parametrize("lq,causal", [(45, True), (45, False), (300, True)])
+@pytest.mark.parametrize("zero", ["q", "k"])
+def test_attention_gradients_of_values_with_a_common_part(t, d, dv, lq, causal, zero):
+    """All scores are 0, so that the probabilities that meet the values are exact: D is off by no rounding to the
+    activations' type (a bound without u times D's magnitude)."""
+    log(f"[attn common part] d={d} {dv} lq={lq} {t} causal={causal} {zero}=0")
+    c = offset_case(t, d, dv, lq, causal)
+    (c.q if zero == "q" else c.k).zero_()
+    c.qh, c.kh = host(c.q), host(c.k)
+    _, _, grads = c.run()
+    r, a = A.attention(c.qh, c.kh, c.vh, c.lamh, c.scale, c.see, c.gh)
+    lk, G, u = c.kh.shape[1], 2, U[t]
+    e, ep = 2.0 ** -24 * (16 + lk), 2.0 ** -24 * (dv + 8)
+    i, name, n = (0, "dq", lk) if zero == "q" else (1, "dk", lq * G)
+    A0, AD, AP = a[name]
+    bound = u * np.abs(r[name]) + (u + e + n * 2.0 ** -24) * A0 + (2 * e + ep) * AD + (e + ep) * AP
+    check(name, grads[i], r[name], bound + TINY[t])
+
+
 @pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("scale", [1e-12, 1e-38, 1e-42])
 def test_attention_scales_near_zero(scale, t):
