@@ -79,9 +79,10 @@ typedef struct {
     int64_t v_stride[3]; /* sequence, token, head */
 } pam_diff_attn_desc_t;
 
-/* Bytes of device workspace for pam_diff_attn_fwd (0 for most shapes: only
- * calls of few queries over many keys split the keys) and pam_diff_attn_bwd;
- * SIZE_MAX on invalid arguments. */
+/* Bytes of device workspace for pam_diff_attn_fwd and pam_diff_attn_bwd, by the
+ * descriptor alone; SIZE_MAX on invalid arguments.  Always to be asked for:
+ * where the queries do not fill the card in whole rounds, prompts and training
+ * among them, the keys are split into parts that meet there (0 elsewhere). */
 size_t pam_diff_attn_fwd_workspace(const pam_diff_attn_desc_t *desc);
 size_t pam_diff_attn_bwd_workspace(const pam_diff_attn_desc_t *desc);
 

@@ -108,7 +108,9 @@ Plan plan_of(int64_t tiles, int64_t heads, int64_t batch, int64_t room, int64_t 
         return p;
     // Parts of causal units fill two rounds, longest first, or one where joining
     // more would cost more: short units of 16-bit types with two blocks on a CU
-    // (bf16, 3 x 1000, 8 heads of 64: 48 us for 61; 1 x 4000, backward: 249 for 235)
+    // (bf16, 8 heads of 64, forward and backward, one round for two: 1 x 2000 55 us
+    // for 87 and 113 for 137, 1 x 2500 65 for 80 and 141 for 163; 1 x 2900 81 for 85
+    // and 194 for 176, 1 x 3300 92 for 88 and 218 for 187)
     const bool one_round = two && !slow && most < 12;
     const int64_t fill = causal ? std::max<int64_t>((one_round ? room : 2 * room) / rest, 2) : room / rest;
     const int64_t parts = std::max(std::min(most, fill), std::min(trips / shortest, kCUs / rest));
@@ -138,8 +140,9 @@ FwdPlan fwd_plan(const pam_diff_attn_desc_t &d)
     // empty, or (16-bit types) all its blocks of 32 rows fit the card at once and
     // the keys are few, so that nothing has to be cut and joined (bf16, 1 x 500, 8
     // heads of 64: 22 us for 26; 4 x 500, of 32: 18 for 27; but 1 x 1000, 4 of 64,
-    // 30 for 27), or it still has more blocks for the same cut (100 x 2000, 8/2
-    // heads: 24 for 28).
+    // 30 for 27), or it still has more blocks for the same cut (2000 keys, 26 blocks:
+    // 25 us for 29, 32: 26 for 28, 48: 32 for 30; 8000 keys 35 for 46, 37 for 45, 50
+    // for 51).
     const bool half = d.dtype != PAM_F32;
     const int64_t tiles = ceil_div((int64_t)(d.heads / d.kv_heads) * d.len_q, 32),
                   blocks = tiles * d.kv_heads * d.batch * f.value_parts;

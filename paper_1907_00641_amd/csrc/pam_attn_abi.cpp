@@ -1,5 +1,5 @@
 // C ABI of the operators around the attention layer (include/pam_attn.h):
-// argument checks; the kernels live in pam_attn.hip, pam_rotary.hip and
+// argument checks; the kernels live in pam_attn_kernels.h, pam_rotary.hip and
 // pam_norm.hip.
 #include <math.h>
 #include <stdint.h>

@@ -344,8 +344,9 @@ constexpr uint64_t kAllSeen = KT == 64 ? ~0ull : (1ull << KT) - 1;
 // tiles of keys and values, which are loaded straight to LDS a tile ahead.  The
 // probabilities never leave the registers: the scores' layout, rounded, is the
 // operand of the second product.  They are rounded to the activations' type
-// for it, before they are divided by their sum (by a relative 2^-9 at most in bf16,
-// and at random: about what rounding the output takes); the sums are of the 32-bit
+// for it, before they are divided by their sum (by a relative 2^-8 at most in bf16,
+// 2^-11 in fp16, and at random: about what rounding the output takes, so that out is
+// off by 1.1 to 1.45 times as much as by that alone); the sums are of the 32-bit
 // values.
 // Head sizes over 64 take the values' channels 128 at a time (a.value_parts):
 // both maps' sums of 256 did not fit the registers, and spilling them cost more
@@ -353,9 +354,9 @@ constexpr uint64_t kAllSeen = KT == 64 ? ~0ull : (1ull << KT) - 1;
 // Bound by instructions: 220 vector operations (64 of them for the softmax's
 // sums and maxima, 32 exponentials) for 24 products of 32 x 32 x 16, which take
 // as long again; two waves per SIMD hide a part of either behind the other.  bf16, 8
-// heads of 64, 2 x 4800: 322 us with its join, 880 TFLOP/s (a large product of the
-// library: 1185); 16384 causal, 2 key heads: 840 us, 980.  Heads of 128, one wave
-// per SIMD: 1486 us, 380.  fp32, 2197, 4 heads of 32: 76 us, 98 (154).
+// heads of 64, 2 x 4800: 325 us with its join, 870 TFLOP/s (a large product of the
+// library: 1185), 330 with o saved; 16384 causal, 2 key heads: 835 us, 990.  Heads of
+// 128, one wave per SIMD: 1470 us, 385.  fp32, 2197, 4 heads of 32: 75 us, 99 (154).
 template <class T, int DP, int DVP, bool WIDE>
 __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) void k_attn_fwd(AttnArgs a)
 {
@@ -528,9 +529,9 @@ __device__ __forceinline__ void join_row(const AttnArgs &a, int parts, const Get
 // queries of all heads of a key head, 32 at a time; the waves of a block walk over
 // their own keys, without waiting for each other, and join their sums in LDS.
 // What bounds it is reading the cache: every wave has two tiles of 32 keys under
-// way (bf16, 8 x 16384 keys, 8 key heads of 64, 32 query heads: 108 us, 5.0 TB/s,
-// joining included).  A short cache is bound by the steps' latency: 300 keys, three
-// steps of a wave, 10.5 us.
+// way (bf16, 8 x 16384 keys, all full, 8 key heads of 64, 32 query heads: 110 us,
+// 4.9 TB/s, joining included).  A short cache is bound by the steps' latency: 300
+// keys, three steps of a wave, 10.8 us.
 template <class T, int DP, int DVP, bool WIDE>
 __global__ __launch_bounds__((64 * Sizes<T, DP, DVP>::kFewWaves)) void k_attn_few(AttnArgs a)
 {
@@ -745,13 +746,14 @@ __global__ __launch_bounds__((FEW ? kJoinThreads : kAttnThreads)) void k_attn_jo
 // a lane holds one query.  sum_j p^1 dp is taken from the 32-bit probabilities and
 // dp, not from the saved o^1, whose rounding would be all its error.
 // D is taken from o in 32 bits: it is the difference of dp and D that counts, which
-// may be far smaller than either (o rounded to bf16, values around 4 times their
-// deviation: dq off by 0.011 of its norm, dk by 0.009).
+// may be far smaller than either (values around 4 times their deviation, bf16: dq off
+// by 0.003 of its norm, of which the rounding of the probabilities that o is made of
+// has a part; with o rounded to bf16 0.011).
 // Score gradients are rounded to the activations' type for their product: about as
 // much again as rounding dq itself (bf16: 0.0024 for 0.0017 of its norm; with 32-bit
 // operands the product would take eight times as long).
-// Bound as the forward pass is: bf16, 8 heads of 64, 2 x 4800: 361 us, 780 TFLOP/s;
-// 16384 causal 937, 880; heads of 128 940 us; fp32, 2197, 4 heads of 32: 79 us.
+// Bound as the forward pass is: bf16, 8 heads of 64, 2 x 4800: 348 us, 810 TFLOP/s;
+// 16384 causal 939, 880; heads of 128 975 us; fp32, 2197, 4 heads of 32: 81 us.
 template <class T, int DP, int DVP, bool WIDE>
 __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) void k_attn_dq(AttnArgs a)
 {
@@ -945,9 +947,9 @@ __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) v
 // atomics in an order that changes from run to run, or by parts of 32 bits as
 // large as the scores' rows over 128.
 // Bound by the same, and by LDS, which the queries, dout and the block's values
-// are read from in two orders each: bf16, 8 heads of 64, 2 x 4800: 462 us, 820
-// TFLOP/s; 16384 causal, 2 key heads 1270, 870; heads of 128, dv 711 and dk 991 us; fp32,
-// 2197, 4 heads of 32: 97 us.
+// are read from in two orders each: bf16, 8 heads of 64, 2 x 4800: 453 us, 830
+// TFLOP/s; 16384 causal, 2 key heads 1283, 860; heads of 128, dv 737 and dk 1025 us; fp32,
+// 2197, 4 heads of 32: 100 us.
 template <class T, int DP, int DVP, bool WIDE, int WHAT>
 __global__ __launch_bounds__(kAttnThreads, (Sizes<T, DP, DVP>::kWavesPerSimd)) void k_attn_dkv(AttnArgs a)
 {

@@ -25,7 +25,6 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
 #define PAM_LDS __attribute__((address_space(3)))
-#define PAM_GLOBAL __attribute__((address_space(1)))
 
 __device__ __forceinline__ int lane_id() { return threadIdx.x & 63; }
 // address of LDS memory
@@ -286,7 +285,7 @@ __device__ __forceinline__ float piece_dot(uint4v a, const float *row, int s, in
 }
 
 // Four consecutive channels (registers 4 g .. 4 g + 3 of a result whose rows
-// are channels) to a row of an array, each times f.
+// are channels) to a row of an array.
 template <class T, bool WIDE>
 __device__ __forceinline__ void store4(T *row, int c, int dim, const float (&x)[4])
 {

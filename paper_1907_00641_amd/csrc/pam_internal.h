@@ -253,7 +253,7 @@ pam_status_t abi_hip_fail(hipError_t e, const char *what) noexcept;
 // an error of earlier asynchronous work, PAM_OK if there is none
 pam_status_t abi_sticky_error() noexcept;
 
-// differential attention (pam_attn.hip); device workspaces in bytes
+// differential attention (pam_attn.cpp); device workspaces in bytes
 size_t attn_fwd_workspace(const pam_diff_attn_desc_t &d);
 size_t attn_bwd_workspace(const pam_diff_attn_desc_t &d);
 hipError_t launch_attn_fwd(const pam_diff_attn_desc_t &d, const void *q, const void *k, const void *v,
