@@ -1,5 +1,6 @@
-"""Thin Python binding of the C ABI in include/pam_lattice.h and
-include/pam_attn.h (and the benchmark's row-copy probe in include/pam_probe.h).
+"""Thin Python binding of the C ABI in include/pam_lattice.h,
+include/pam_attn.h and include/pam_packed.h (and the benchmark's row-copy
+probe in include/pam_probe.h).
 
 Argument marshalling only: every step of the filter runs in the HIP
 library ``libpam_lattice.so``.  PyTorch provides device memory and the
@@ -40,6 +41,9 @@ EXPORTS = (
     "pam_diff_attn_fwd_workspace", "pam_diff_attn_bwd_workspace", "pam_diff_attn_fwd", "pam_diff_attn_bwd",
     "pam_rotary_frequencies", "pam_rotary_table", "pam_rotary", "pam_dropout", "pam_norm_gate_fwd",
     "pam_norm_gate_bwd_workspace", "pam_norm_gate_bwd",
+    "pam_attn_fwd_workspace", "pam_attn_bwd_workspace", "pam_attn_fwd", "pam_attn_bwd",
+    "pam_head_norm_rotary_fwd", "pam_head_norm_rotary_bwd_workspace", "pam_head_norm_rotary_bwd",
+    "pam_cache_write", "pam_cache_read", "pam_paged_attn_workspace", "pam_paged_attn",
 )
 
 # pam_dtype_t
@@ -49,6 +53,8 @@ PAM_ROTARY_INTERLEAVED = 1
 PAM_ROTARY_INVERSE = 2
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3}
 NORMS = {"rms": 0, "layer": 1}
+# pam_store_t of the types that have a scale per row
+_STORES = {torch.float8_e4m3fn: 3, torch.int8: 4}
 
 
 class BlockDesc(ctypes.Structure):
@@ -81,6 +87,43 @@ class NormDesc(ctypes.Structure):
                 ("channels", ctypes.c_int32), ("eps", ctypes.c_float), ("gate_rows", ctypes.c_int64),
                 ("x_stride", ctypes.c_int64), ("z_stride", ctypes.c_int64), ("p", ctypes.c_double),
                 ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64)]
+
+
+class AttnDesc(ctypes.Structure):
+    """pam_attn_desc_t of the C header."""
+    _fields_ = [("dtype", ctypes.c_int32), ("sequences", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("dim_v", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("scale", ctypes.c_float), ("tokens", ctypes.c_int64),
+                ("keys", ctypes.c_int64), ("q_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2),
+                ("v_stride", ctypes.c_int64 * 2)]
+
+
+class HeadNormDesc(ctypes.Structure):
+    """pam_head_norm_desc_t of the C header."""
+    _fields_ = [("dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("length", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("w_per_head", ctypes.c_int32), ("eps", ctypes.c_float), ("start", ctypes.c_int64),
+                ("entries", ctypes.c_int64), ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3)]
+
+
+class CacheDesc(ctypes.Structure):
+    """pam_cache_desc_t of the C header."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("dtype", "store", "pages", "page_size", "kv_heads", "dim", "dim_v",
+                                                    "maps", "sequences", "table_width")]
+
+
+class CacheRows(ctypes.Structure):
+    """pam_cache_rows_t of the C header."""
+    _fields_ = [("rows", ctypes.c_int64), ("length", ctypes.c_int32), ("k_stride", ctypes.c_int64 * 4),
+                ("v_stride", ctypes.c_int64 * 3)]
+
+
+class PagedAttnDesc(ctypes.Structure):
+    """pam_paged_attn_desc_t of the C header."""
+    _fields_ = [("heads", ctypes.c_int32), ("len_q", ctypes.c_int32), ("key_bound", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("q_stride", ctypes.c_int64 * 4)]
+
 
 _lib = None
 _vp = ctypes.c_void_p
@@ -163,6 +206,28 @@ def lib():
     L.pam_norm_gate_bwd_workspace.argtypes = [ctypes.POINTER(NormDesc)]
     L.pam_norm_gate_bwd.restype = ctypes.c_int
     L.pam_norm_gate_bwd.argtypes = [ctypes.POINTER(NormDesc)] + [_vp] * 19
+    L.pam_attn_fwd_workspace.restype = ctypes.c_size_t
+    L.pam_attn_fwd_workspace.argtypes = [ctypes.POINTER(AttnDesc)]
+    L.pam_attn_bwd_workspace.restype = ctypes.c_size_t
+    L.pam_attn_bwd_workspace.argtypes = [ctypes.POINTER(AttnDesc)]
+    L.pam_attn_fwd.restype = ctypes.c_int
+    L.pam_attn_fwd.argtypes = [ctypes.POINTER(AttnDesc)] + [_vp] * 10
+    L.pam_attn_bwd.restype = ctypes.c_int
+    L.pam_attn_bwd.argtypes = [ctypes.POINTER(AttnDesc)] + [_vp] * 8 + [ctypes.POINTER(_i64)] + [_vp] * 5
+    L.pam_head_norm_rotary_fwd.restype = ctypes.c_int
+    L.pam_head_norm_rotary_fwd.argtypes = [ctypes.POINTER(HeadNormDesc)] + [_vp] * 9
+    L.pam_head_norm_rotary_bwd_workspace.restype = ctypes.c_size_t
+    L.pam_head_norm_rotary_bwd_workspace.argtypes = [ctypes.POINTER(HeadNormDesc)]
+    L.pam_head_norm_rotary_bwd.restype = ctypes.c_int
+    L.pam_head_norm_rotary_bwd.argtypes = [ctypes.POINTER(HeadNormDesc)] + [_vp] * 14
+    L.pam_cache_write.restype = ctypes.c_int
+    L.pam_cache_write.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(CacheRows)] + [_vp] * 11
+    L.pam_cache_read.restype = ctypes.c_int
+    L.pam_cache_read.argtypes = [ctypes.POINTER(CacheDesc), _i32] + [_vp] * 9
+    L.pam_paged_attn_workspace.restype = ctypes.c_size_t
+    L.pam_paged_attn_workspace.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(PagedAttnDesc)]
+    L.pam_paged_attn.restype = ctypes.c_int
+    L.pam_paged_attn.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(PagedAttnDesc)] + [_vp] * 12
     L.pam_lattice_destroy.restype = None
     L.pam_lattice_destroy.argtypes = [_vp]
     L.pam_status_string.restype = ctypes.c_char_p
@@ -737,3 +802,297 @@ def pam_norm_gate_bwd(x: torch.Tensor, *, grad_r: torch.Tensor | None, grad_h: t
     _check(L.pam_norm_gate_bwd(d, *ptrs[:7], pr, ph, *(None if t is None else t.data_ptr() for t in grads),
                                ws.data_ptr(), _stream_ptr(stream)), "pam_norm_gate_bwd")
     return dict(zip(("x", "z", "w_post", "b_post", "gate", "scale", "w_pre", "b_pre"), grads))
+
+
+# ---------------------------------------------------------------------------
+# attention over packed sequences and from a paged cache (include/pam_packed.h)
+# ---------------------------------------------------------------------------
+
+def _attn_desc(q, k, v, q_start, k_start, scale, causal):
+    """Descriptor of a call and the pointers that both directions take."""
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise ValueError("q must be T x H x d, k S x Hk x d, v S x Hk x dv")
+    (t, H, d), (n, hk, dv) = q.shape, v.shape
+    if k.shape != (n, hk, d):
+        raise ValueError("q, k and v do not agree in keys, key heads or head size")
+    if (q_start is None) != (k_start is None):
+        raise ValueError("q_start and k_start go together")
+    B = 1
+    if q_start is not None:
+        if q_start.dim() != 1 or q_start.shape[0] < 2:
+            raise ValueError("q_start must hold one more than the sequences")
+        B = q_start.shape[0] - 1
+    _counts(t, n, H, hk, d, dv, B)
+    dt = q.dtype
+    code, dev = _dtype_of(q, "q"), _device_of(q, "q")
+    ptrs = [_rows_ptr(q, dt, dev, "q"), _rows_ptr(k, dt, dev, "k"), _rows_ptr(v, dt, dev, "v"),
+            _shaped_ptr(q_start, (B + 1,), torch.int32, dev, "q_start"),
+            _shaped_ptr(k_start, (B + 1,), torch.int32, dev, "k_start")]
+    desc = AttnDesc(code, B, H, hk, d, dv, PAM_ATTN_CAUSAL if causal else 0, d ** -0.5 if scale is None else scale,
+                    t, n, q.stride()[:2], k.stride()[:2], v.stride()[:2])
+    return desc, ptrs, dev
+
+
+def pam_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_start: torch.Tensor | None = None,
+                 k_start: torch.Tensor | None = None, scale: float | None = None, causal: bool = False,
+                 save: bool = False, stream=None):
+    """Softmax attention over packed sequences.
+
+    ``q`` is T x H x d, ``k`` S x Hk x d, ``v`` S x Hk x dv (any strides, last axis contiguous); sequence b has the
+    queries q_start[b] .. q_start[b + 1] - 1 and the keys k_start[b] .. k_start[b + 1] - 1 (B + 1 int32 on the
+    device each; None: one sequence of all rows); ``scale`` 1 / sqrt(d) if not given; ``causal``: the last query of
+    a sequence sees all its keys, each one before it one key less.  Returns ``out`` (T x H x dv); with ``save``
+    (out, saved), saved being what pam_attn_bwd takes."""
+    desc, ptrs, _ = _attn_desc(q, k, v, q_start, k_start, scale, causal)
+    L, d = lib(), ctypes.byref(desc)
+    shape = (*q.shape[:2], v.shape[2])
+    ws_bytes = _workspace_bytes(L.pam_attn_fwd_workspace(d), "pam_attn_fwd")
+
+    def make():
+        out = q.new_empty(shape)
+        so = q.new_empty(shape, dtype=torch.float32) if save else None
+        lse = q.new_empty((shape[1], shape[0]), dtype=torch.float32) if save else None
+        return out, so, lse, q.new_empty(ws_bytes, dtype=torch.uint8) if ws_bytes else None
+
+    out, so, lse, ws = _new(stream, make)
+    _check(L.pam_attn_fwd(d, *ptrs, out.data_ptr(), so.data_ptr() if save else None, lse.data_ptr() if save else None,
+                          ws.data_ptr() if ws_bytes else None, _stream_ptr(stream)), "pam_attn_fwd")
+    return (out, (so, lse)) if save else out
+
+
+def pam_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, saved, grad_out: torch.Tensor, *,
+                 q_start: torch.Tensor | None = None, k_start: torch.Tensor | None = None, scale: float | None = None,
+                 causal: bool = False, stream=None):
+    """Gradients (q, k, v) of pam_attn_fwd with the same arguments, from its ``saved`` and ``grad_out``
+    (T x H x dv, any strides)."""
+    desc, ptrs, dev = _attn_desc(q, k, v, q_start, k_start, scale, causal)
+    L, d = lib(), ctypes.byref(desc)
+    shape = (*q.shape[:2], v.shape[2])
+    so, lse = saved
+    pso = _shaped_ptr(so, shape, torch.float32, dev, "saved o")
+    plse = _shaped_ptr(lse, (shape[1], shape[0]), torch.float32, dev, "saved lse")
+    if grad_out.shape != shape:
+        raise ValueError(f"grad_out has shape {tuple(grad_out.shape)}, expected {shape}")
+    pdo = _rows_ptr(grad_out, q.dtype, dev, "grad_out")
+    ws_bytes = _workspace_bytes(L.pam_attn_bwd_workspace(d), "pam_attn_bwd")
+    gq, gk, gv, ws = _new(stream, lambda: (q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(v.shape),
+                                           q.new_empty(max(ws_bytes, 16), dtype=torch.uint8)))
+    _check(L.pam_attn_bwd(d, *ptrs, pso, plse, pdo, (_i64 * 2)(*grad_out.stride()[:2]), gq.data_ptr(), gk.data_ptr(),
+                          gv.data_ptr(), ws.data_ptr(), _stream_ptr(stream)), "pam_attn_bwd")
+    return gq, gk, gv
+
+
+def _head_norm_desc(q, k, table, w_q, w_k, norm, eps, pos, start, interleaved):
+    if q.dim() != 4 or (k is not None and (k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3])):
+        raise ValueError("q must be B x L x H x d and k B x L x Hk x d")
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("table must be entries x pairs x 2")
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {sorted(NORMS)}")
+    if k is None and w_k is not None:
+        raise ValueError("w_k goes with k")
+    B, n, H, d = q.shape
+    hk = 0 if k is None else k.shape[2]
+    _counts(B, n, H, hk, d, table.shape[1])
+    if not -(1 << 62) < start < 1 << 62:
+        raise ValueError("start must be less than 2^62 in size")
+    # weights of every head, or of all
+    given = [w.dim() for w in (w_q, w_k) if w is not None]
+    per_head = 2 in given
+    if per_head and given != [2] * len(given):
+        raise ValueError("w_q and w_k must both have a row per head, or neither")
+    dt, dev = q.dtype, _device_of(q, "q")
+    desc = HeadNormDesc(_dtype_of(q, "q"), NORMS[norm], B, n, H, hk, d, table.shape[1],
+                        PAM_ROTARY_INTERLEAVED if interleaved else 0, per_head, eps, start, table.shape[0],
+                        q.stride()[:3], (0, 0, 0) if k is None else k.stride()[:3])
+    f32 = torch.float32
+    ptrs = [_rows_ptr(q, dt, dev, "q"), None if k is None else _rows_ptr(k, dt, dev, "k"),
+            _shaped_ptr(w_q, (H, d) if per_head else (d,), f32, dev, "w_q"),
+            _shaped_ptr(w_k, (hk, d) if per_head else (d,), f32, dev, "w_k"),
+            _shaped_ptr(table, table.shape, f32, dev, "table"), _shaped_ptr(pos, (B, n), torch.int32, dev, "pos")]
+    return desc, ptrs, dev
+
+
+def pam_head_norm_rotary_fwd(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, *,
+                             w_q: torch.Tensor | None = None, w_k: torch.Tensor | None = None, norm: str = "rms",
+                             eps: float = 1e-6, pos: torch.Tensor | None = None, start: int = 0,
+                             interleaved: bool = False, out=None, stream=None):
+    """Normalises every head of ``q`` (B x L x H x d) and ``k`` (B x L x Hk x d, or None), multiplies it by its
+    weights (fp32: d values for all heads, or a row per head) and turns its first 2 pairs channels by ``table``
+    (entries x pairs x 2), as pam_rotary does.  ``out`` = (q_out, k_out), contiguous; contiguous inputs may be their
+    own outputs.  Returns (q', k')."""
+    desc, ptrs, dev = _head_norm_desc(q, k, table, w_q, w_k, norm, eps, pos, start, interleaved)
+    if out is None:
+        qo, ko = _new(stream, lambda: (q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)))
+        pqo, pko = qo.data_ptr(), None if k is None else ko.data_ptr()
+    else:
+        qo, ko = out
+        pqo = _shaped_ptr(qo, q.shape, q.dtype, dev, "q_out")
+        pko = None if k is None else _shaped_ptr(ko, k.shape, q.dtype, dev, "k_out")
+    _check(lib().pam_head_norm_rotary_fwd(ctypes.byref(desc), *ptrs, pqo, pko, _stream_ptr(stream)),
+           "pam_head_norm_rotary_fwd")
+    return qo, ko
+
+
+def pam_head_norm_rotary_bwd(q: torch.Tensor, k: torch.Tensor | None, table: torch.Tensor, grad_q: torch.Tensor,
+                             grad_k: torch.Tensor | None, *, w_q: torch.Tensor | None = None,
+                             w_k: torch.Tensor | None = None, norm: str = "rms", eps: float = 1e-6,
+                             pos: torch.Tensor | None = None, start: int = 0, interleaved: bool = False,
+                             stream=None) -> dict:
+    """Gradients of pam_head_norm_rotary_fwd with the same arguments by the names "q", "k", "w_q", "w_k" (None for
+    those not given), from ``grad_q`` and ``grad_k`` of its outputs."""
+    desc, ptrs, dev = _head_norm_desc(q, k, table, w_q, w_k, norm, eps, pos, start, interleaved)
+    L, d = lib(), ctypes.byref(desc)
+    if (grad_k is None) != (k is None):
+        raise ValueError("grad_k goes with k")
+    pgq = _shaped_ptr(grad_q, q.shape, q.dtype, dev, "grad_q")
+    pgk = None if k is None else _shaped_ptr(grad_k, k.shape, q.dtype, dev, "grad_k")
+    ws_bytes = _workspace_bytes(L.pam_head_norm_rotary_bwd_workspace(d), "pam_head_norm_rotary_bwd")
+    *grads, ws = _new(stream, lambda: [None if t is None else t.new_empty(t.shape) for t in (q, k, w_q, w_k)] + [
+        q.new_empty(max(ws_bytes, 16), dtype=torch.uint8)])
+    _check(L.pam_head_norm_rotary_bwd(d, *ptrs, pgq, pgk, *(None if t is None else t.data_ptr() for t in grads),
+                                      ws.data_ptr(), _stream_ptr(stream)), "pam_head_norm_rotary_bwd")
+    return dict(zip(("q", "k", "w_q", "w_k"), grads))
+
+
+class PagedCache:
+    """The tensors of a paged cache, which the caller owns.
+
+    ``k`` is pages x Hk x page x d, or pages x Hk x page x 2 x d for differential attention, ``v`` pages x Hk x page
+    x dv, contiguous, float32, float16 or bfloat16, or float8_e4m3fn or int8 with ``k_scale`` and ``v_scale``
+    (fp32, without the last axis)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
+                 v_scale: torch.Tensor | None = None):
+        if k.dim() not in (4, 5) or v.dim() != 4 or k.shape[:3] != v.shape[:3] or (k.dim() == 5 and k.shape[3] != 2):
+            raise ValueError("k must be pages x Hk x page x d or pages x Hk x page x 2 x d, v pages x Hk x page x dv")
+        if k.dtype not in _DTYPES and k.dtype not in _STORES:
+            raise ValueError("a cache is float32, float16, bfloat16, float8_e4m3fn or int8")
+        dev, f32 = k.get_device(), torch.float32
+        if dev < 0:
+            raise ValueError("k must be a device tensor")
+        if k.dtype in _STORES and (k_scale is None or v_scale is None):
+            raise ValueError(f"a cache of {k.dtype} has k_scale and v_scale")
+        if k.dtype not in _STORES and (k_scale is not None or v_scale is not None):
+            raise ValueError(f"a cache of {k.dtype} has no scales")
+        _counts(*k.shape, *v.shape)
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, dev
+        self._pool = [_shaped_ptr(k, k.shape, k.dtype, dev, "k"), _shaped_ptr(v, v.shape, k.dtype, dev, "v"),
+                      _shaped_ptr(k_scale, k.shape[:-1], f32, dev, "k_scale"),
+                      _shaped_ptr(v_scale, v.shape[:-1], f32, dev, "v_scale")]
+        self.maps = 2 if k.dim() == 5 else 1
+        self._sizes = (k.shape[0], k.shape[2], k.shape[1], k.shape[-1], v.shape[-1], self.maps)
+
+    @classmethod
+    def empty(cls, pages: int, page: int, kv_heads: int, dim: int, dim_v: int | None = None, *, maps: int = 1,
+              dtype=torch.bfloat16, device="cuda") -> "PagedCache":
+        """A new cache of zeros; ``dim_v`` is maps dim if not given."""
+        lead = (pages, kv_heads, page)
+        k = torch.zeros(*lead, *((2, dim) if maps == 2 else (dim,)), dtype=torch.uint8, device=device) \
+            if dtype in _STORES else torch.zeros(*lead, *((2, dim) if maps == 2 else (dim,)), dtype=dtype, device=device)
+        v = torch.zeros(*lead, maps * dim if dim_v is None else dim_v, dtype=k.dtype, device=device)
+        if dtype not in _STORES:
+            return cls(k, v)
+        return cls(k.view(dtype), v.view(dtype), torch.zeros(k.shape[:-1], device=device),
+                   torch.zeros(v.shape[:-1], device=device))
+
+    def _call(self, dtype, table, k_len):
+        """Descriptor and the pointers of table, lengths and pool of a call with activations of ``dtype``."""
+        if self.device != torch._C._cuda_getDevice():
+            raise ValueError("the cache must be on the current device")
+        store = _STORES.get(self.k.dtype)
+        if store is None:
+            if dtype is not self.k.dtype:
+                raise ValueError(f"a cache of {self.k.dtype} goes with activations of that type, not {dtype}")
+            store = _DTYPES[dtype]
+        elif dtype not in _DTYPES:
+            raise ValueError("activations are float32, float16 or bfloat16")
+        if table.dim() != 2:
+            raise ValueError("table must be B x pages of a sequence")
+        B, width = table.shape
+        _counts(B, width)
+        pt = _shaped_ptr(table, (B, width), torch.int32, self.device, "table")
+        pn = _shaped_ptr(k_len, (B,), torch.int32, self.device, "k_len")
+        return CacheDesc(_DTYPES[dtype], store, *self._sizes, B, width), pt, pn
+
+
+def pam_cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_len: torch.Tensor, *,
+                    starts: torch.Tensor | None = None, new_len: torch.Tensor | None = None, stream=None):
+    """Writes the last tokens of every sequence to its pages, quantised if the cache is.
+
+    ``table`` (B x pages of a sequence, int32) names them, ``k_len`` (B int32) counts each sequence's tokens, the new
+    ones included.  ``k`` is B x L x Hk x d (or B x L x Hk x 2 x d) and ``v`` B x L x Hk x dv, of which sequence b's
+    first new_len[b] rows are new (B int32; None: L); with ``starts`` (B + 1 int32) they are packed, without the
+    first axis: sequence b has rows starts[b] .. starts[b + 1] - 1.  Any strides with the last axis contiguous."""
+    pages, page, hk, d, dv, maps = cache._sizes
+    lead = 1 if starts is not None else 2
+    tail = (hk, 2, d) if maps == 2 else (hk, d)
+    if k.shape[lead:] != tail or v.shape[lead:] != (hk, dv) or k.shape[:lead] != v.shape[:lead] or \
+            k.dim() != lead + len(tail) or v.dim() != lead + 2:
+        raise ValueError("k and v must be B x L (with starts: rows) x the cache's heads and channels")
+    desc, pt, pn = cache._call(k.dtype, table, k_len)
+    B, dev = desc.sequences, cache.device
+    if starts is not None and new_len is not None:
+        raise ValueError("new_len does not go with starts")
+    if lead == 2 and k.shape[0] != B:
+        raise ValueError("k, v and table do not agree in sequences")
+    _counts(*k.shape[:lead])
+    ks, vs = k.stride()[:-1], v.stride()[:-1]
+    if lead == 1:
+        ks, vs = (0, *ks), (0, *vs)
+    rows = CacheRows(k.shape[0] if lead == 1 else 0, k.shape[1] if lead == 2 else 0, ks if maps == 2 else (*ks, 0), vs)
+    _check(lib().pam_cache_write(
+        ctypes.byref(desc), ctypes.byref(rows), _rows_ptr(k, k.dtype, dev, "k"), _rows_ptr(v, k.dtype, dev, "v"),
+        _shaped_ptr(starts, (B + 1,), torch.int32, dev, "starts"), _shaped_ptr(new_len, (B,), torch.int32, dev, "new_len"),
+        pt, pn, *cache._pool, _stream_ptr(stream)), "pam_cache_write")
+
+
+def pam_cache_read(cache: PagedCache, table: torch.Tensor, k_len: torch.Tensor, length: int, *, dtype=None,
+                   stream=None):
+    """The first ``length`` positions of every sequence: k (B x length x Hk x d, or x 2 x d) and v (B x length x Hk x
+    dv) of type ``dtype`` (the cache's own if not given), 0 from k_len[b] on."""
+    dtype = cache.k.dtype if dtype is None else dtype
+    desc, pt, pn = cache._call(dtype, table, k_len)
+    _counts(length)
+    if length < 0:
+        raise ValueError("length must not be negative")
+    pages, page, hk, d, dv, maps = cache._sizes
+    lead = (desc.sequences, length, hk)
+    k, v = _new(stream, lambda: (cache.k.new_empty((*lead, 2, d) if maps == 2 else (*lead, d), dtype=dtype),
+                                 cache.v.new_empty((*lead, dv), dtype=dtype)))
+    _check(lib().pam_cache_read(ctypes.byref(desc), length, pt, pn, *cache._pool, k.data_ptr(), v.data_ptr(),
+                                _stream_ptr(stream)), "pam_cache_read")
+    return k, v
+
+
+def pam_paged_attn(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, k_len: torch.Tensor, *,
+                   lam: torch.Tensor | None = None, q_len: torch.Tensor | None = None, scale: float | None = None,
+                   key_bound: int = 0, stream=None) -> torch.Tensor:
+    """Causal attention of new tokens over a cache that holds their keys and values already.
+
+    ``q`` is B x L x H x d, or B x L x H x 2 x d for a cache of two maps, with ``lam`` (H values of q's type): then
+    out = (P1 - lam P2) v as pam_diff_attn_fwd has it.  ``q_len`` (B int32; None: L): new tokens of a sequence, of
+    which the last sees all its k_len[b] keys.  ``scale`` 1 / sqrt(d) if not given.  ``key_bound``: a length that
+    sequences hardly pass, for speed alone (0: what the table holds).  Returns B x L x H x dv."""
+    pages, page, hk, d, dv, maps = cache._sizes
+    if q.dim() != 3 + maps or q.shape[-1] != d or (maps == 2 and q.shape[3] != 2):
+        raise ValueError("q must be B x L x H x d, or B x L x H x 2 x d for a cache of two maps")
+    if (lam is None) != (maps == 1):
+        raise ValueError("lam goes with a cache of two maps")
+    desc, pt, pn = cache._call(q.dtype, table, k_len)
+    B, n, H = q.shape[:3]
+    if desc.sequences != B:
+        raise ValueError("q and table do not agree in sequences")
+    _counts(B, n, H, key_bound)
+    dev = cache.device
+    attn = PagedAttnDesc(H, n, key_bound, d ** -0.5 if scale is None else scale,
+                         (q.stride()[:4] if maps == 2 else (*q.stride()[:3], 0)))
+    L, c, a = lib(), ctypes.byref(desc), ctypes.byref(attn)
+    pq, pl = _rows_ptr(q, q.dtype, dev, "q"), _shaped_ptr(lam, (H,), q.dtype, dev, "lam")
+    pql = _shaped_ptr(q_len, (B,), torch.int32, dev, "q_len")
+    ws_bytes = _workspace_bytes(L.pam_paged_attn_workspace(c, a), "pam_paged_attn")
+    out, ws = _new(stream, lambda: (q.new_empty((B, n, H, dv)),
+                                    q.new_empty(ws_bytes, dtype=torch.uint8) if ws_bytes else None))
+    _check(L.pam_paged_attn(c, a, pq, pl, pql, pt, pn, *cache._pool, out.data_ptr(),
+                            ws.data_ptr() if ws_bytes else None, _stream_ptr(stream)), "pam_paged_attn")
+    return out

@@ -15,7 +15,9 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpam_lattice.so")
 SOURCES = ["pam_build.hip", "pam_filter.hip", "pam_block.hip", "pam_probe.hip", "pam_abi.cpp",
            "pam_attn_f32.hip", "pam_attn_f16.hip", "pam_attn_bf16.hip", "pam_attn.cpp",
-           "pam_rotary.hip", "pam_norm.hip", "pam_attn_abi.cpp"]
+           "pam_rotary.hip", "pam_norm.hip", "pam_attn_abi.cpp",
+           "pam_paged_f32.hip", "pam_paged_f16.hip", "pam_paged_bf16.hip", "pam_paged.cpp",
+           "pam_packed_f32.hip", "pam_packed_f16.hip", "pam_packed_bf16.hip", "pam_packed.cpp", "pam_head_norm.hip", "pam_cache.hip", "pam_packed_abi.cpp"]
 ARCH = "gfx950"
 
 

@@ -11,6 +11,7 @@
 
 #include "../../include/pam_attn.h"
 #include "../../include/pam_lattice.h"
+#include "../../include/pam_packed.h"
 #include "../../include/pam_probe.h"
 
 namespace pam {
@@ -280,5 +281,42 @@ hipError_t launch_norm_bwd(const pam_norm_desc_t &d, const void *x, const void *
                            const void *grad_r, const void *grad_h, void *grad_x, void *grad_z, float *gw_post,
                            float *gb_post, void *grad_gate, float *gscale, float *gw_pre, float *gb_pre,
                            void *workspace, hipStream_t s);
+
+// ---- attention over packed sequences and from a paged cache (pam_packed.h)
+// (pam_packed.cpp)
+size_t packed_fwd_workspace(const pam_attn_desc_t &d);
+size_t packed_bwd_workspace(const pam_attn_desc_t &d);
+hipError_t launch_packed_fwd(const pam_attn_desc_t &d, const void *q, const void *k, const void *v,
+                             const int32_t *q_start, const int32_t *k_start, void *out, float *so, float *lse,
+                             void *workspace, hipStream_t s);
+hipError_t launch_packed_bwd(const pam_attn_desc_t &d, const void *q, const void *k, const void *v,
+                             const int32_t *q_start, const int32_t *k_start, const float *so, const float *lse,
+                             const void *dout, const int64_t *dos, void *gq, void *gk, void *gv, void *workspace,
+                             hipStream_t s);
+// (pam_head_norm.hip)
+hipError_t launch_head_norm_fwd(const pam_head_norm_desc_t &d, const void *q, const void *k, const float *w_q,
+                                const float *w_k, const float *table, const int32_t *pos, void *q_out, void *k_out,
+                                hipStream_t s);
+size_t head_norm_bwd_workspace(const pam_head_norm_desc_t &d);
+hipError_t launch_head_norm_bwd(const pam_head_norm_desc_t &d, const void *q, const void *k, const float *w_q,
+                                const float *w_k, const float *table, const int32_t *pos, const void *gq_out,
+                                const void *gk_out, void *gq, void *gk, float *gw_q, float *gw_k, void *workspace,
+                                hipStream_t s);
+// A cache's pool and the sequences' pages (pam_store.h has what kernels do with it).
+struct Pool {
+    void *k, *v;
+    float *ks, *vs;
+    const int32_t *table, *k_len;
+    int32_t pages, page, kv_heads, dim, dim_v, maps, sequences, width;
+};
+// (pam_cache.hip)
+hipError_t launch_cache_write(const pam_cache_desc_t &d, const pam_cache_rows_t &rows, const Pool &pool, const void *k,
+                              const void *v, const int32_t *starts, const int32_t *new_len, hipStream_t s);
+hipError_t launch_cache_read(const pam_cache_desc_t &d, int32_t length, const Pool &pool, void *k, void *v,
+                             hipStream_t s);
+// (pam_paged.cpp)
+size_t paged_workspace(const pam_cache_desc_t &c, const pam_paged_attn_desc_t &d);
+hipError_t launch_paged(const pam_cache_desc_t &c, const pam_paged_attn_desc_t &d, const Pool &pool, const void *q,
+                        const void *lam, const int32_t *q_len, void *out, void *workspace, hipStream_t s);
 
 }  // namespace pam

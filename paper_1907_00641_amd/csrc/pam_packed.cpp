@@ -1,0 +1,155 @@
+// Attention over packed sequences: from a call's descriptor to the kernels'
+// arguments, and how the work is dealt out (pam_packed_kernels.h, compiled per
+// element type).
+#include "pam_packed.h"
+
+#include <algorithm>
+
+namespace pam {
+
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+constexpr int64_t kCUs = 256;
+
+// blocks of four waves that the card holds at once
+int64_t at_once(const pam_attn_desc_t &d)
+{
+    return kCUs * (d.dtype != PAM_F32 || packed_class(d.dim, d.dim_v) == 64 ? 2 : 1);
+}
+
+// rows: of all sequences, on the axis that is dealt out; walked: tiles of the other
+// axis that a unit of an average sequence walks over; least: tiles of a part.
+PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_t walked, int64_t least)
+{
+    PackedPlan p{};
+    p.slots = (uint32_t)(rows / kPackedRows + d.sequences);
+    p.heads = (uint32_t)heads;
+    p.parts = 1;
+    // units of sequences of the average length
+    const int64_t units = ceil_div(std::max<int64_t>(rows / d.sequences, 1), kPackedRows) * d.sequences * heads;
+    const int64_t room = at_once(d);
+    if (units < room)
+        p.parts = (uint32_t)std::max<int64_t>(1, std::min(walked / least, room / units));
+    if ((d.flags & PAM_ATTN_CAUSAL) && p.parts == 1 && room == 2 * kCUs && p.units() >= 2 * kCUs)
+        p.fold = (uint32_t)kCUs;
+    return p;
+}
+
+struct Plans {
+    PackedPlan rows, keys;
+    int64_t row_part, key_part, stats;  // floats
+};
+
+Plans plans_of(const pam_attn_desc_t &d, bool backward)
+{
+    Plans p{};
+    const int64_t cls = packed_class(d.dim, d.dim_v);
+    p.rows = plan_of(d, d.tokens, d.heads, ceil_div(d.keys / d.sequences, 64), 4);
+    p.row_part = p.rows.parts > 1 ? (int64_t)p.rows.items() * kPackedRows * (cls + (backward ? 0 : 2)) : 0;
+    if (backward) {
+        p.keys = plan_of(d, d.keys, d.kv_heads, ceil_div(d.tokens / d.sequences, 32) * (d.heads / d.kv_heads), 8);
+        p.key_part = p.keys.parts > 1 ? (int64_t)p.keys.items() * kPackedRows * 2 * cls : 0;
+        p.stats = 2 * (int64_t)d.heads * d.tokens;
+    }
+    return p;
+}
+
+PackedArgs args_of(const pam_attn_desc_t &d, const void *q, const void *k, const void *v, const int32_t *q_start,
+                   const int32_t *k_start)
+{
+    PackedArgs a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_start = q_start;
+    a.k_start = k_start;
+    for (int i = 0; i < 2; ++i) {
+        a.qs[i] = d.q_stride[i];
+        a.ks[i] = d.k_stride[i];
+        a.vs[i] = d.v_stride[i];
+    }
+    a.sequences = d.sequences;
+    a.heads = d.heads;
+    a.kv_heads = d.kv_heads;
+    a.group = d.heads / d.kv_heads;
+    a.dim = d.dim;
+    a.dim_v = d.dim_v;
+    a.tokens = (int32_t)d.tokens;
+    a.keys = (int32_t)d.keys;
+    a.causal = (d.flags & PAM_ATTN_CAUSAL) != 0;
+    a.scale = d.scale;
+    return a;
+}
+
+// Whether every row may be read 16 bytes at a time, with the offsets of a tile of
+// 64 rows, in bytes, in 32 bits.
+bool wide_rows(const pam_attn_desc_t &d, const void *p, const int64_t *stride, int dim)
+{
+    const int per = d.dtype == PAM_F32 ? 4 : 8;
+    return (uintptr_t)p % 16 == 0 && stride[0] % per == 0 && stride[1] % per == 0 && dim % per == 0 && stride[0] >= 0 &&
+           stride[0] <= 1 << 23;
+}
+bool wide_of(const pam_attn_desc_t &d, const void *q, const void *k, const void *v)
+{
+    return wide_rows(d, q, d.q_stride, d.dim) && wide_rows(d, k, d.k_stride, d.dim) && wide_rows(d, v, d.v_stride, d.dim_v);
+}
+bool at16(const void *p) { return (uintptr_t)p % 16 == 0; }
+
+}  // namespace
+
+size_t packed_fwd_workspace(const pam_attn_desc_t &d)
+{
+    return d.tokens ? (size_t)plans_of(d, false).row_part * sizeof(float) : 0;
+}
+
+size_t packed_bwd_workspace(const pam_attn_desc_t &d)
+{
+    const Plans p = plans_of(d, true);
+    return (size_t)(p.row_part + p.key_part + p.stats) * sizeof(float);
+}
+
+hipError_t launch_packed_fwd(const pam_attn_desc_t &d, const void *q, const void *k, const void *v,
+                             const int32_t *q_start, const int32_t *k_start, void *out, float *so, float *lse,
+                             void *workspace, hipStream_t s)
+{
+    PackedArgs a = args_of(d, q, k, v, q_start, k_start);
+    a.plan = plans_of(d, false).rows;
+    a.part = (float *)workspace;
+    a.out = out;
+    a.so = so;
+    a.lse = lse;
+    a.wide = wide_of(d, q, k, v) && at16(out) && at16(so);
+    if (d.dtype == PAM_F32)
+        return packed_fwd_f32(a, s);
+    return d.dtype == PAM_F16 ? packed_fwd_f16(a, s) : packed_fwd_bf16(a, s);
+}
+
+hipError_t launch_packed_bwd(const pam_attn_desc_t &d, const void *q, const void *k, const void *v,
+                             const int32_t *q_start, const int32_t *k_start, const float *so, const float *lse,
+                             const void *dout, const int64_t *dos, void *gq, void *gk, void *gv, void *workspace,
+                             hipStream_t s)
+{
+    PackedArgs a = args_of(d, q, k, v, q_start, k_start);
+    const Plans p = plans_of(d, true);
+    a.plan = p.rows;
+    a.key_plan = p.keys;
+    a.part = (float *)workspace;
+    a.key_part = a.part + p.row_part;
+    a.stats = a.key_part + p.key_part;
+    a.so = const_cast<float *>(so);
+    a.lse = const_cast<float *>(lse);
+    a.dout = dout;
+    a.dos[0] = dos[0];
+    a.dos[1] = dos[1];
+    a.gq = gq;
+    a.gk = gk;
+    a.gv = gv;
+    a.wide = wide_of(d, q, k, v) && wide_rows(d, dout, dos, d.dim_v) && at16(so) && at16(gq) && at16(gk) && at16(gv);
+    if (d.dtype == PAM_F32)
+        return packed_bwd_f32(a, s);
+    return d.dtype == PAM_F16 ? packed_bwd_f16(a, s) : packed_bwd_bf16(a, s);
+}
+
+}  // namespace pam

@@ -1,0 +1,8 @@
+// Attention over a paged cache (gfx950) for f16 queries.
+#include "pam_paged_kernels.h"
+
+namespace pam {
+
+hipError_t paged_f16(const PagedArgs &a, int store, bool wide, hipStream_t s) { return paged_type<f16>(a, store, wide, s); }
+
+}  // namespace pam

@@ -1,0 +1,460 @@
+// Kernels of attention over a paged cache for one element type of queries
+// (included by one source file per type, so that they compile side by side).
+//
+// The queries of all heads of a key head, and both maps of differential
+// attention, are the rows of one tile of 32: a row of map m is padded with zeros to
+// the channels of both maps' keys, so that one product forms every row's scores
+// with its own map, and both maps meet the values in one product.
+//   s_rj = scale <q_r, number_j> kscale_j,   p_rj = softmax over the keys that r sees,
+//   o_r = sum_j p_rj vscale_j number_j,      out = o, or o^0 - lambda o^1.
+// Scores are formed transposed, as in pam_attn_kernels.h: a lane holds one row.
+#pragma once
+
+#include "pam_attn_common.h"
+#include "pam_paged.h"
+#include "pam_store.h"
+
+namespace pam {
+
+namespace {
+
+constexpr int kPagedWaves = 4;
+
+template <class T, int C>
+struct PagedSizes {
+    using R = Rows<T, C>;
+    static constexpr int CK = C / kChunk<T>, TV = C / 32, CP = 32 / kChunk<T>;
+    static constexpr int kPieces = C / 16;       // pieces of eight elements of a tile of 32 rows that a lane brings
+    static constexpr int kTile = R::size(32);
+    static constexpr int kScales = 3 * 32 * 4;   // of a tile: both maps' keys, values
+    // waves per SIMD that the registers are for
+    static constexpr int kWavesPerSimd = C == 256 || (sizeof(T) == 4 && C == 128) ? 1 : 2;
+    // LDS of a wave: its tile, or its sums of `live` rows; its scales, or tops and sums
+    static constexpr int wave_bytes(int live) { return std::max(kTile, live * C * 4); }
+    static constexpr int bytes(int live) { return kPagedWaves * (wave_bytes(live) + kScales); }
+};
+
+// A tile's rows on their way from the pool: pieces of eight elements, in registers.
+template <class T, class S, int C, bool WIDE>
+struct Staged {
+    using Z = PagedSizes<T, C>;
+    static constexpr int kPer = C / 8;  // pieces of a row
+    Stored8<S> x[Z::kPieces];
+    __device__ __forceinline__ static int row_of(int n) { return n * (64 / kPer) + lane_id() / kPer; }
+    __device__ __forceinline__ static int channel() { return lane_id() % kPer * 8; }
+    // rows of `dim` elements from `pool`; lane j has the number of row j of the tile,
+    // negative: 0
+    __device__ __forceinline__ void load(const S *pool, int rid, int dim)
+    {
+        const int c = channel(), m = max(min(dim - c, 8), 0);
+#pragma unroll
+        for (int n = 0; n < Z::kPieces; ++n) {
+            const int r = __shfl(rid, row_of(n));
+            const S *p = pool + (int64_t)r * dim + c;
+            x[n] = Stored8<S>{};
+            if constexpr (WIDE) {
+                if (r >= 0 && m > 0)
+                    x[n] = load_stored(p);
+            } else {
+                x[n] = load_stored_some(p, r >= 0 ? m : 0);
+            }
+        }
+    }
+    // to the tile, as T; SCALED: times the row's factor, which lane j has of row j
+    template <bool SCALED>
+    __device__ __forceinline__ void put(char *tile, float scale) const
+    {
+        using R = typename Z::R;
+        const int c = channel();
+#pragma unroll
+        for (int n = 0; n < Z::kPieces; ++n) {
+            const int row = row_of(n);
+            if constexpr (std::is_same<T, S>::value) {
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                    store16(tile + R::at(row, c * (int)sizeof(T) / 16 + i),
+                            uint4v{x[n].w[4 * i], x[n].w[4 * i + 1], x[n].w[4 * i + 2], x[n].w[4 * i + 3]});
+            } else {
+                float y[8];
+                unpack<S>(x[n], y);
+                if constexpr (SCALED) {
+                    const float f = __shfl(scale, row);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        y[j] *= f;
+                }
+                const Stored8<T> t = pack<T>(y);
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                    store16(tile + R::at(row, c * (int)sizeof(T) / 16 + i),
+                            uint4v{t.w[4 * i], t.w[4 * i + 1], t.w[4 * i + 2], t.w[4 * i + 3]});
+            }
+        }
+    }
+};
+
+// Sums of waves or parts p < n of one row, relative to the largest top: a part that
+// saw nothing has the sum 0; one whose top is -inf and whose sum is not 0 has a NaN.
+struct Joined {
+    float top, sum;
+    float4v o;
+};
+template <class GetStats, class GetSums>
+__device__ __forceinline__ Joined joined(int n, const GetStats &stats, const GetSums &sums)
+{
+    Joined r = {-INFINITY, 0.0f, {}};
+    for (int p = 0; p < n; ++p) {
+        const float2 st = stats(p);
+        r.top = st.y != 0.0f ? __builtin_fmaxf(r.top, st.x) : r.top;
+    }
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+        const float2 st = stats(p);
+        const float4v x = sums(p);
+        const float f = st.y == 0.0f ? 0.0f : (st.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.x - r.top));
+        r.sum += f * st.y;
+        r.o += f * x;
+    }
+    return r;
+}
+
+// Four channels of an output row from its maps' rows.
+template <class T, class GetRow>
+__device__ __forceinline__ void paged_out(const PagedArgs &a, int b, int hk, int x, int ch, const GetRow &row)
+{
+    const int g = x / a.len_q, i = x - g * a.len_q, h = hk * a.group + g;
+    float y[4];
+    const Joined r0 = row(x * a.pool.maps);
+    const float i0 = r0.sum != 0.0f ? 1.0f / r0.sum : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        y[j] = r0.o[j] * i0;
+    if (a.pool.maps == 2) {
+        const Joined r1 = row(x * 2 + 1);
+        const float i1 = r1.sum != 0.0f ? 1.0f / r1.sum : 0.0f, lam = (float)((const T *)a.lam)[h];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            y[j] -= lam * (r1.o[j] * i1);
+    }
+    T *out = (T *)a.out + (((int64_t)b * a.len_q + i) * a.heads + h) * a.pool.dim_v;
+    if (a.pool.dim_v % 4 == 0 && (uintptr_t)a.out % 16 == 0)
+        store4<T, true>(out, ch, a.pool.dim_v, y);
+    else
+        store4<T, false>(out, ch, a.pool.dim_v, y);
+}
+
+// A block takes a part of a unit's keys (a unit: 32 rows of one key head of one
+// sequence), and every wave a run of tiles of 32 keys of it.  A tile is brought from
+// its pages to registers while the one before is worked on, turned into the
+// queries' type on its way to LDS (e4m3 and int8 numbers are exact there), and
+// read as operands from there: the values straight after the keys, in the same
+// place.  The waves meet in LDS at the end.
+template <class T, class S, int C, bool WIDE>
+__global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)) void k_paged(PagedArgs a)
+{
+    using Z = PagedSizes<T, C>;
+    using R = typename Z::R;
+    // fp16 has no range for a probability times a scale: its values are scaled before
+    // they are rounded (by a relative 2^-11 at most), others by way of the probabilities
+    constexpr bool kValues = kScaled<S> && std::is_same<T, f16>::value, kProbs = kScaled<S> && !kValues;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const int l = lane_id(), w = wave_id();
+    const float c = a.scale * kLog2e;
+    const int stride = Z::wave_bytes(a.live);
+    char *tile = lds + w * stride;
+    float *scales = reinterpret_cast<float *>(lds + kPagedWaves * stride + w * Z::kScales);
+    const uint32_t kr = lds_address(tile) + R::row_lane(), vc = lds_address(tile) + R::col_lane();
+    const uint32_t items = (uint32_t)a.units * a.parts;
+    for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
+        const uint32_t unit = uniform(n / a.parts);
+        const int part = n - unit * a.parts;
+        const uint32_t head = uniform(unit / a.tiles);
+        const int rt = unit - head * a.tiles, b = uniform(head / a.pool.kv_heads), hk = head - b * a.pool.kv_heads;
+        const int nk = uniform(cached(a.pool, b));
+        const int nq = uniform(a.q_len ? min(max(a.q_len[b], 0), a.len_q) : a.len_q);
+        // this lane's row
+        const int r = rt * 32 + (l & 31), x = r / a.pool.maps, m = r - x * a.pool.maps;
+        const int g = x / a.len_q, i = x - g * a.len_q, h = hk * a.group + g;
+        const bool in = r < a.rows && i < nq;
+        const int limit = in ? max(min(nk, i + nk - nq + 1), 0) : 0;
+        int wend = limit, wall = r < a.rows ? limit : nk;
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            wend = max(wend, __shfl_xor(wend, s));
+            wall = min(wall, __shfl_xor(wall, s));
+        }
+        wend = uniform(wend);
+        wall = uniform(wall);
+        int from, to;
+        {
+            const int trips = (wend + 31) / 32, runs = a.parts * kPagedWaves, per = trips / runs, more = trips - per * runs;
+            const int run = part * kPagedWaves + w;  // runs differ by a tile at the most
+            from = uniform(run * per + min(run, more));
+            to = uniform(from + per + (run < more));
+        }
+
+        Staged<T, S, C, WIDE> ks, vs;
+        int rid = -1, next = -1;          // rows of the tile under way, and of the one after
+        float sk0 = 0.0f, sk1 = 0.0f, sv = 0.0f;
+        auto find = [&](int t) {          // lane j: row of key j of tile t
+            const int j = t * 32 + (l & 31);
+            return j < wend ? cache_row(a.pool, b, hk, j) : -1;
+        };
+        auto fetch_keys = [&]() {
+            ks.load((const S *)a.pool.k, rid, a.pool.maps * a.pool.dim);
+            if constexpr (kScaled<S>) {
+                const int64_t at = max(rid, 0);
+                sk0 = rid < 0 ? 0.0f : a.pool.ks[at * a.pool.maps];
+                sk1 = rid < 0 || a.pool.maps == 1 ? 0.0f : a.pool.ks[at * 2 + 1];
+                sv = rid < 0 ? 0.0f : a.pool.vs[at];
+            }
+        };
+        if (from < to) {
+            rid = find(from);
+            fetch_keys();
+            if (from + 1 < to)
+                next = find(from + 1);
+            vs.load((const S *)a.pool.v, rid, a.pool.dim_v);
+        }
+        // the row as an operand, 0 outside its map's channels
+        uint4v q[Z::CK];
+        {
+            constexpr int per = 16 / sizeof(T);
+            const T *row = (const T *)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2] + m * a.qs[3];
+#pragma unroll
+            for (int s = 0; s < Z::CK; ++s) {
+                const int ch = s * kChunk<T> + (l >> 5) * per - m * a.pool.dim;
+                q[s] = uint4v{0, 0, 0, 0};
+                if (a.q_wide) {
+                    if (in && ch >= 0 && ch < a.pool.dim)
+                        q[s] = load16(row + ch);
+                } else {
+                    T y[per];
+#pragma unroll
+                    for (int j = 0; j < per; ++j)
+                        y[j] = in && ch + j >= 0 && ch + j < a.pool.dim ? row[ch + j] : (T)0.0f;
+                    __builtin_memcpy(&q[s], y, 16);
+                }
+            }
+        }
+        f32x16 o[Z::TV] = {};
+        float top = -INFINITY, sum = 0.0f;
+        for (int t = from; t < to; ++t) {
+            const uint32_t seen = (uint32_t)__ballot(rid >= 0);
+            ks.template put<false>(tile, 0.0f);
+            if constexpr (kScaled<S>) {
+                if (l < 32) {
+                    scales[l] = sk0;
+                    scales[32 + l] = sk1;
+                    scales[64 + l] = sv;
+                }
+            }
+            const float sv_here = sv;
+            wave_fence();
+            const int after = rid = next;
+            if (t + 1 < to) {
+                fetch_keys();
+                next = t + 2 < to ? find(t + 2) : -1;
+            }
+            f32x16 s = {};
+#pragma unroll
+            for (int k = 0; k < Z::CK; ++k)
+                mma<T>(s, R::row_chunk(kr, 0, k), q[k]);
+            if constexpr (kScaled<S>) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const float4v f = *reinterpret_cast<const float4v *>(scales + m * 32 + 8 * y + 4 * (l >> 5));
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        s[4 * y + z] *= f[z];
+                }
+            }
+            if (seen != ~0u || t * 32 + 32 > wall) {
+                const uint32_t bits = (seen & low_bits(limit - t * 32)) >> (4 * (l >> 5));
+#pragma unroll
+                for (int y = 0; y < 16; ++y)
+                    s[y] = bits >> (8 * (y >> 2) + (y & 3)) & 1 ? s[y] : -INFINITY;
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int y = 1; y < 16; ++y)
+                mx = __builtin_fmaxf(mx, s[y]);
+            mx *= c;
+            if (__any(mx > top + 8.0f)) {  // the maximum is followed only when it grew by more than 2^8
+                const float up = __builtin_fmaxf(top, xor32_max(mx));
+                const float f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - up);
+                top = up;
+                sum *= f;
+#pragma unroll
+                for (int v = 0; v < Z::TV; ++v)
+                    o[v] *= f;
+            }
+            const float base = top == -INFINITY ? 0.0f : top - kLift<T>;
+            float add = 0.0f;
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+                s[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y], c, -base));
+                add += s[y];
+            }
+            sum += add;
+            if constexpr (kProbs) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const float4v f = *reinterpret_cast<const float4v *>(scales + 64 + 8 * y + 4 * (l >> 5));
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        s[4 * y + z] *= f[z];
+                }
+            }
+            uint4v p[Z::CP];
+#pragma unroll
+            for (int k = 0; k < Z::CP; ++k)
+                p[k] = operand<T>(s, k);
+            wave_fence();  // the keys are read
+            vs.template put<kValues>(tile, sv_here);
+            wave_fence();
+            if (t + 1 < to)
+                vs.load((const S *)a.pool.v, after, a.pool.dim_v);
+#pragma unroll
+            for (int k = 0; k < Z::CP; ++k)
+#pragma unroll
+                for (int v = 0; v < Z::TV; ++v)
+                    mma<T>(o[v], R::col_chunk(vc, 0, k, 32 * v), p[k]);
+            wave_fence();  // the values are read
+        }
+        sum = xor32_add(sum);
+        // [row][channel] of this wave where its tile was, tops and sums where its scales were
+        float *mine = reinterpret_cast<float *>(tile);
+        if ((l & 31) < a.live) {
+#pragma unroll
+            for (int v = 0; v < Z::TV; ++v)
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    *reinterpret_cast<float4v *>(mine + (l & 31) * C + 32 * v + 8 * y + 4 * (l >> 5)) =
+                        sum != 0.0f ? float4v{o[v][4 * y], o[v][4 * y + 1], o[v][4 * y + 2], o[v][4 * y + 3]} : float4v{};
+            if (l < 32)
+                *reinterpret_cast<float2 *>(scales + 2 * l) = make_float2(top, sum);
+        }
+        __syncthreads();
+        auto row_at = [&](int row, int ch) {
+            return joined(
+                kPagedWaves,
+                [&](int p) {
+                    return *reinterpret_cast<const float2 *>(lds + kPagedWaves * stride + p * Z::kScales + row * 8);
+                },
+                [&](int p) {
+                    return *reinterpret_cast<const float4v *>(reinterpret_cast<const float *>(lds + p * stride) + row * C + ch);
+                });
+        };
+        const int rows = min(a.rows - rt * 32, 32);
+        if (a.parts == 1) {
+            const int outs = rows / a.pool.maps;
+            for (int e = threadIdx.x; e < outs * (C / 4); e += 64 * kPagedWaves) {
+                const int ch = e % (C / 4) * 4;
+                if (ch < a.pool.dim_v)
+                    paged_out<T>(a, b, hk, rt * 32 / a.pool.maps + e / (C / 4), ch,
+                                 [&](int row) { return row_at(row - rt * 32, ch); });
+            }
+        } else {
+            const int64_t at = (int64_t)n * a.live;
+            for (int e = threadIdx.x; e < rows * (C / 4); e += 64 * kPagedWaves) {
+                const int row = e / (C / 4), ch = e % (C / 4) * 4;
+                const Joined j = row_at(row, ch);
+                *reinterpret_cast<float4v *>(a.part + (at + row) * C + ch) = j.o;
+                if (ch == 0)
+                    *reinterpret_cast<float2 *>(a.part + (int64_t)items * a.live * C + (at + row) * 2) =
+                        make_float2(j.top, j.sum);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins the parts of every unit: a block per output row, its threads in teams that
+// take every so-manieth part of four channels each.
+constexpr int kJoinThreads = 256;
+
+template <class T, int C>
+__global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a)
+{
+    constexpr int QUADS = C / 4, TEAMS = kJoinThreads / QUADS;
+    __shared__ Joined s[TEAMS][QUADS];
+    const int team = threadIdx.x / QUADS, quad = threadIdx.x % QUADS, ch = quad * 4;
+    const int64_t items = (int64_t)a.units * a.parts;
+    const uint32_t per = a.live / a.pool.maps;  // output rows of a unit
+    const uint32_t rows = (uint32_t)a.units * per;
+    for (uint32_t e = blockIdx.x; e < rows; e += gridDim.x) {
+        const uint32_t unit = e / per, head = unit / a.tiles;
+        const int rt = unit - head * a.tiles, b = head / a.pool.kv_heads, hk = head - b * a.pool.kv_heads;
+        const int x = rt * 32 / a.pool.maps + (e - unit * per);
+        if (x * a.pool.maps >= a.rows)  // the same in every thread
+            continue;
+        Joined mine[2] = {};
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            if (m == a.pool.maps)
+                break;
+            const int row = x * a.pool.maps + m - rt * 32;
+            auto at = [&](int p) { return ((int64_t)unit * a.parts + min(team + p * TEAMS, a.parts - 1)) * a.live + row; };
+            const int n = team < a.parts ? (a.parts - team + TEAMS - 1) / TEAMS : 0;
+            mine[m] = joined(
+                n, [&](int p) { return *reinterpret_cast<const float2 *>(a.part + items * a.live * C + at(p) * 2); },
+                [&](int p) { return *reinterpret_cast<const float4v *>(a.part + at(p) * C + ch); });
+        }
+        Joined r[2] = {};
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            if (m == a.pool.maps)
+                break;
+            __syncthreads();
+            s[team][quad] = mine[m];
+            __syncthreads();
+            r[m] = joined(
+                TEAMS, [&](int p) { return make_float2(s[p][quad].top, s[p][quad].sum); },
+                [&](int p) { return s[p][quad].o; });
+        }
+        if (team == 0 && ch < a.pool.dim_v)
+            paged_out<T>(a, b, hk, x, ch, [&](int row) { return row == x * a.pool.maps ? r[0] : r[1]; });
+    }
+}
+
+template <class T, class S, int C, bool WIDE>
+hipError_t paged_class_launch(const PagedArgs &a, hipStream_t s)
+{
+    using Z = PagedSizes<T, C>;
+    hipError_t e = launch_lds<k_paged<T, S, C, WIDE>>(item_blocks((int64_t)a.units * a.parts), 64 * kPagedWaves,
+                                                      Z::bytes(a.live), a, s);
+    if (e != hipSuccess || a.parts == 1)
+        return e;
+    const unsigned rows = (unsigned)std::min<int64_t>((int64_t)a.units * (a.live / a.pool.maps), 1 << 23);
+    hipLaunchKernelGGL((k_paged_join<T, C>), dim3(rows), dim3(kJoinThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <class T, class S, bool WIDE>
+hipError_t paged_wide(const PagedArgs &a, hipStream_t s)
+{
+    switch (paged_class(a.pool.maps * a.pool.dim, a.pool.dim_v)) {
+    case 64: return paged_class_launch<T, S, 64, WIDE>(a, s);
+    case 128: return paged_class_launch<T, S, 128, WIDE>(a, s);
+    default: return paged_class_launch<T, S, 256, WIDE>(a, s);
+    }
+}
+
+template <class T, class S>
+hipError_t paged_store(const PagedArgs &a, bool wide, hipStream_t s)
+{
+    return wide ? paged_wide<T, S, true>(a, s) : paged_wide<T, S, false>(a, s);
+}
+
+template <class T>
+hipError_t paged_type(const PagedArgs &a, int store, bool wide, hipStream_t s)
+{
+    if (store == PAM_STORE_E4M3)
+        return paged_store<T, e4m3>(a, wide, s);
+    return store == PAM_STORE_INT8 ? paged_store<T, int8>(a, wide, s) : paged_store<T, T>(a, wide, s);
+}
+
+}  // namespace
+
+}  // namespace pam
