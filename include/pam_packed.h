@@ -202,8 +202,8 @@ typedef struct {
  *   k : element (b, i, head, map, x) at strides k_stride (sequence, token, head,
  *       map) and v without the map axis; with starts the sequence axis is not
  *       there, its stride not looked at.
- * Without starts `rows` is not looked at, with them `length` is not.  rows (sequences
- * length) less than 2^31.  Asynchronous.
+ * Without starts `rows` is not looked at, with them `length` is not.  (rows + 16)
+ * kv_heads maps less than 2^31 (rows: sequences length).  Asynchronous.
  */
 typedef struct {
     int64_t rows;
@@ -220,7 +220,7 @@ pam_status_t pam_cache_write(const pam_cache_desc_t *desc, const pam_cache_rows_
  * length x kv_heads x maps x dim, v sequences x length x kv_heads x dim_v,
  * contiguous, of type dtype; 0 from k_len[b] on.  Values of 8 bits are the
  * fp32 products of number and scale, rounded to dtype.  k or v may be NULL: not
- * asked for.  Asynchronous.
+ * asked for.  (sequences length + 16) kv_heads maps less than 2^31.  Asynchronous.
  */
 pam_status_t pam_cache_read(const pam_cache_desc_t *desc, int32_t length, const int32_t *table, const int32_t *k_len,
                             const void *k_pages, const void *v_pages, const float *k_scale, const float *v_scale,

@@ -568,6 +568,11 @@ def _new(stream, make):
         return make()
 
 
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A new contiguous tensor of ``t``'s shape and type."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 _SIZE_MAX = ctypes.c_size_t(-1).value
 
 
@@ -810,27 +815,28 @@ def pam_norm_gate_bwd(x: torch.Tensor, *, grad_r: torch.Tensor | None, grad_h: t
 
 def _attn_desc(q, k, v, q_start, k_start, scale, causal):
     """Descriptor of a call and the pointers that both directions take."""
-    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+    qs, ks, vs = q.shape, k.shape, v.shape
+    if len(qs) != 3 or len(ks) != 3 or len(vs) != 3:
         raise ValueError("q must be T x H x d, k S x Hk x d, v S x Hk x dv")
-    (t, H, d), (n, hk, dv) = q.shape, v.shape
-    if k.shape != (n, hk, d):
+    (t, H, d), (n, hk, dv) = qs, vs
+    if ks != (n, hk, d):
         raise ValueError("q, k and v do not agree in keys, key heads or head size")
     if (q_start is None) != (k_start is None):
         raise ValueError("q_start and k_start go together")
-    B = 1
+    B, pqs, pks = 1, None, None
+    dt = q.dtype
     if q_start is not None:
         if q_start.dim() != 1 or q_start.shape[0] < 2:
             raise ValueError("q_start must hold one more than the sequences")
         B = q_start.shape[0] - 1
     _counts(t, n, H, hk, d, dv, B)
-    dt = q.dtype
     code, dev = _dtype_of(q, "q"), _device_of(q, "q")
-    ptrs = [_rows_ptr(q, dt, dev, "q"), _rows_ptr(k, dt, dev, "k"), _rows_ptr(v, dt, dev, "v"),
-            _shaped_ptr(q_start, (B + 1,), torch.int32, dev, "q_start"),
-            _shaped_ptr(k_start, (B + 1,), torch.int32, dev, "k_start")]
+    if q_start is not None:
+        pqs = _shaped_ptr(q_start, (B + 1,), torch.int32, dev, "q_start")
+        pks = _shaped_ptr(k_start, (B + 1,), torch.int32, dev, "k_start")
     desc = AttnDesc(code, B, H, hk, d, dv, PAM_ATTN_CAUSAL if causal else 0, d ** -0.5 if scale is None else scale,
                     t, n, q.stride()[:2], k.stride()[:2], v.stride()[:2])
-    return desc, ptrs, dev
+    return desc, (_rows_ptr(q, dt, dev, "q"), _rows_ptr(k, dt, dev, "k"), _rows_ptr(v, dt, dev, "v"), pqs, pks), dev
 
 
 def pam_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_start: torch.Tensor | None = None,
@@ -883,33 +889,34 @@ def pam_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, saved, grad_
 
 
 def _head_norm_desc(q, k, table, w_q, w_k, norm, eps, pos, start, interleaved):
-    if q.dim() != 4 or (k is not None and (k.dim() != 4 or k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3])):
+    shape, kshape, tshape = q.shape, None if k is None else k.shape, table.shape
+    if len(shape) != 4 or (k is not None and (len(kshape) != 4 or kshape[:2] != shape[:2] or kshape[3] != shape[3])):
         raise ValueError("q must be B x L x H x d and k B x L x Hk x d")
-    if table.dim() != 3 or table.shape[2] != 2:
+    if len(tshape) != 3 or tshape[2] != 2:
         raise ValueError("table must be entries x pairs x 2")
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {sorted(NORMS)}")
     if k is None and w_k is not None:
         raise ValueError("w_k goes with k")
-    B, n, H, d = q.shape
-    hk = 0 if k is None else k.shape[2]
-    _counts(B, n, H, hk, d, table.shape[1])
+    B, n, H, d = shape
+    hk = 0 if k is None else kshape[2]
+    _counts(B, n, H, hk, d, tshape[1])
     if not -(1 << 62) < start < 1 << 62:
         raise ValueError("start must be less than 2^62 in size")
     # weights of every head, or of all
-    given = [w.dim() for w in (w_q, w_k) if w is not None]
-    per_head = 2 in given
-    if per_head and given != [2] * len(given):
+    first = w_q if w_q is not None else w_k
+    per_head = first is not None and first.dim() == 2
+    if w_q is not None and w_k is not None and w_q.dim() != w_k.dim():
         raise ValueError("w_q and w_k must both have a row per head, or neither")
-    dt, dev = q.dtype, _device_of(q, "q")
-    desc = HeadNormDesc(_dtype_of(q, "q"), NORMS[norm], B, n, H, hk, d, table.shape[1],
-                        PAM_ROTARY_INTERLEAVED if interleaved else 0, per_head, eps, start, table.shape[0],
+    dt, dev, f32 = q.dtype, _device_of(q, "q"), torch.float32
+    desc = HeadNormDesc(_dtype_of(q, "q"), NORMS[norm], B, n, H, hk, d, tshape[1],
+                        PAM_ROTARY_INTERLEAVED if interleaved else 0, per_head, eps, start, tshape[0],
                         q.stride()[:3], (0, 0, 0) if k is None else k.stride()[:3])
-    f32 = torch.float32
-    ptrs = [_rows_ptr(q, dt, dev, "q"), None if k is None else _rows_ptr(k, dt, dev, "k"),
-            _shaped_ptr(w_q, (H, d) if per_head else (d,), f32, dev, "w_q"),
-            _shaped_ptr(w_k, (hk, d) if per_head else (d,), f32, dev, "w_k"),
-            _shaped_ptr(table, table.shape, f32, dev, "table"), _shaped_ptr(pos, (B, n), torch.int32, dev, "pos")]
+    ptrs = (_rows_ptr(q, dt, dev, "q"), None if k is None else _rows_ptr(k, dt, dev, "k"),
+            None if w_q is None else _shaped_ptr(w_q, (H, d) if per_head else (d,), f32, dev, "w_q"),
+            None if w_k is None else _shaped_ptr(w_k, (hk, d) if per_head else (d,), f32, dev, "w_k"),
+            _shaped_ptr(table, tshape, f32, dev, "table"),
+            None if pos is None else _shaped_ptr(pos, (B, n), torch.int32, dev, "pos"))
     return desc, ptrs, dev
 
 
@@ -923,7 +930,7 @@ def pam_head_norm_rotary_fwd(q: torch.Tensor, k: torch.Tensor | None, table: tor
     own outputs.  Returns (q', k')."""
     desc, ptrs, dev = _head_norm_desc(q, k, table, w_q, w_k, norm, eps, pos, start, interleaved)
     if out is None:
-        qo, ko = _new(stream, lambda: (q.new_empty(q.shape), None if k is None else q.new_empty(k.shape)))
+        qo, ko = _new(stream, lambda: (_like(q), None if k is None else _like(k)))
         pqo, pko = qo.data_ptr(), None if k is None else ko.data_ptr()
     else:
         qo, ko = out
@@ -948,7 +955,7 @@ def pam_head_norm_rotary_bwd(q: torch.Tensor, k: torch.Tensor | None, table: tor
     pgq = _shaped_ptr(grad_q, q.shape, q.dtype, dev, "grad_q")
     pgk = None if k is None else _shaped_ptr(grad_k, k.shape, q.dtype, dev, "grad_k")
     ws_bytes = _workspace_bytes(L.pam_head_norm_rotary_bwd_workspace(d), "pam_head_norm_rotary_bwd")
-    *grads, ws = _new(stream, lambda: [None if t is None else t.new_empty(t.shape) for t in (q, k, w_q, w_k)] + [
+    *grads, ws = _new(stream, lambda: [None if t is None else _like(t) for t in (q, k, w_q, w_k)] + [
         q.new_empty(max(ws_bytes, 16), dtype=torch.uint8)])
     _check(L.pam_head_norm_rotary_bwd(d, *ptrs, pgq, pgk, *(None if t is None else t.data_ptr() for t in grads),
                                       ws.data_ptr(), _stream_ptr(stream)), "pam_head_norm_rotary_bwd")
@@ -998,22 +1005,23 @@ class PagedCache:
 
     def _call(self, dtype, table, k_len):
         """Descriptor and the pointers of table, lengths and pool of a call with activations of ``dtype``."""
-        if self.device != torch._C._cuda_getDevice():
+        dev = self.device
+        if dev != torch._C._cuda_getDevice():
             raise ValueError("the cache must be on the current device")
-        store = _STORES.get(self.k.dtype)
+        code, store = _DTYPES.get(dtype), _STORES.get(self.k.dtype)
+        if code is None:
+            raise ValueError("activations are float32, float16 or bfloat16")
         if store is None:
             if dtype is not self.k.dtype:
                 raise ValueError(f"a cache of {self.k.dtype} goes with activations of that type, not {dtype}")
-            store = _DTYPES[dtype]
-        elif dtype not in _DTYPES:
-            raise ValueError("activations are float32, float16 or bfloat16")
-        if table.dim() != 2:
+            store = code
+        shape = table.shape
+        if len(shape) != 2:
             raise ValueError("table must be B x pages of a sequence")
-        B, width = table.shape
+        B, width = shape
         _counts(B, width)
-        pt = _shaped_ptr(table, (B, width), torch.int32, self.device, "table")
-        pn = _shaped_ptr(k_len, (B,), torch.int32, self.device, "k_len")
-        return CacheDesc(_DTYPES[dtype], store, *self._sizes, B, width), pt, pn
+        return (CacheDesc(code, store, *self._sizes, B, width), _shaped_ptr(table, shape, torch.int32, dev, "table"),
+                _shaped_ptr(k_len, (B,), torch.int32, dev, "k_len"))
 
 
 def pam_cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, k_len: torch.Tensor, *,
@@ -1058,8 +1066,9 @@ def pam_cache_read(cache: PagedCache, table: torch.Tensor, k_len: torch.Tensor, 
         raise ValueError("length must not be negative")
     pages, page, hk, d, dv, maps = cache._sizes
     lead = (desc.sequences, length, hk)
-    k, v = _new(stream, lambda: (cache.k.new_empty((*lead, 2, d) if maps == 2 else (*lead, d), dtype=dtype),
-                                 cache.v.new_empty((*lead, dv), dtype=dtype)))
+    kshape, where = (*lead, 2, d) if maps == 2 else (*lead, d), cache.k.device
+    k, v = _new(stream, lambda: (torch.empty(kshape, dtype=dtype, device=where),
+                                 torch.empty((*lead, dv), dtype=dtype, device=where)))
     _check(lib().pam_cache_read(ctypes.byref(desc), length, pt, pn, *cache._pool, k.data_ptr(), v.data_ptr(),
                                 _stream_ptr(stream)), "pam_cache_read")
     return k, v

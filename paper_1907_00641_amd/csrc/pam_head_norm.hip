@@ -34,7 +34,8 @@ struct HeadNormArgs {
     int64_t start, entries;
     int32_t batch, length, heads, kv_heads, dim, pairs;
     int32_t group;               // lanes per row, a power of two
-    int32_t chunks_q, chunks_k;  // backward: blocks per vector of weights of q, of k
+    int32_t chunks_q, chunks_k;  // blocks per vector of weights of q, of k
+    Divisor by_length, by_heads, by_kv_heads;
     bool layer, per_head;
     float eps;
 };
@@ -88,16 +89,21 @@ struct Lane {
             pair0 = turns = 0;
         }
     }
+    // V elements in accesses of up to 16 bytes
+    template <class X>
+    struct Wide {
+        typedef X Vec __attribute__((ext_vector_type(V), aligned(sizeof(X) * V > 16 ? 16 : sizeof(X) * V)));
+    };
     template <class X>
     __device__ __forceinline__ static void get(const X *p, int n, bool ok, float (&x)[V])
     {
-        X y[V];
         if constexpr (WIDE) {
+            typename Wide<X>::Vec y = {};
             if (ok && n > 0)
-                __builtin_memcpy(y, __builtin_assume_aligned(p, sizeof(X) * V > 16 ? 16 : sizeof(X) * V), sizeof(y));
+                y = *reinterpret_cast<const typename Wide<X>::Vec *>(p);
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                x[j] = ok && n > 0 ? (float)y[j] : 0.0f;
+                x[j] = (float)y[j];
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j)
@@ -118,12 +124,12 @@ struct Lane {
             T *p = row + (i ? c1 : c0);
             const int n = i ? n1 : n0;
             if constexpr (WIDE) {
-                T y[V];
+                typename Wide<T>::Vec y;
 #pragma unroll
                 for (int j = 0; j < V; ++j)
                     y[j] = rounded<T>(x[i][j]);
                 if (n > 0)
-                    __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T) * V > 16 ? 16 : sizeof(T) * V), y, sizeof(y));
+                    *reinterpret_cast<typename Wide<T>::Vec *>(p) = y;
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j)
@@ -149,20 +155,26 @@ struct Lane {
         const int64_t at = a.pos ? (int64_t)a.pos[tok] : a.start + l;
         const bool in = at >= 0 && at < a.entries;
         const float2 *row = a.table + (in ? at : 0) * a.pairs + pair0;
-        float2 cs[V] = {};
+        const float *p = reinterpret_cast<const float *>(row);
+        const float nan = __builtin_nanf("");
         if constexpr (WIDE) {
-            if (turns > 0)
-                __builtin_memcpy(cs, __builtin_assume_aligned(row, 16), sizeof(cs));
+            float4v y[V / 2] = {};
+            if (turns > 0) {
+#pragma unroll
+                for (int j = 0; j < V / 2; ++j)
+                    y[j] = *reinterpret_cast<const float4v *>(p + 4 * j);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                c[j] = in ? y[j / 2][2 * (j % 2)] : nan;
+                s[j] = in ? y[j / 2][2 * (j % 2) + 1] : nan;
+            }
         } else {
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (j < turns)
-                    cs[j] = row[j];
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            c[j] = in ? cs[j].x : __builtin_nanf("");
-            s[j] = in ? cs[j].y : __builtin_nanf("");
+            for (int j = 0; j < V; ++j) {
+                c[j] = j >= turns ? 1.0f : (in ? p[2 * j] : nan);
+                s[j] = j >= turns ? 0.0f : (in ? p[2 * j + 1] : nan);
+            }
         }
     }
     // the rotation by the angle, or (sign -1) back; one rounding per product and
@@ -209,43 +221,6 @@ struct Lane {
     }
 };
 
-// Forward: a group of lanes per row, all heads of a token behind each other, so
-// that a wave reads and writes whole rows.
-template <class T, int V, bool INTERLEAVED, bool WIDE>
-__global__ __launch_bounds__(kThreads) void k_head_norm_fwd(HeadNormArgs a)
-{
-    using L = Lane<T, V, INTERLEAVED, WIDE>;
-    const int per = kThreads / a.group, j = threadIdx.x & (a.group - 1), all = a.heads + a.kv_heads;
-    const L lane(a, j);
-    const uint32_t rows = (uint32_t)a.batch * a.length * all;
-    // the same turns for every lane of a wave: sums are over lanes
-    for (uint32_t e0 = blockIdx.x * per; e0 < rows; e0 += gridDim.x * per) {
-        const uint32_t e = min(e0 + threadIdx.x / a.group, rows - 1);
-        const bool live = e0 + threadIdx.x / a.group < rows;
-        const uint32_t tok = e / all, h = e - tok * all, b = tok / a.length, l = tok - b * a.length;
-        const bool key = h >= (uint32_t)a.heads;
-        const uint32_t hh = key ? h - a.heads : h;
-        const T *from = key ? (const T *)a.k + b * a.ks[0] + l * a.ks[1] + hh * a.ks[2]
-                            : (const T *)a.q + b * a.qs[0] + l * a.qs[1] + hh * a.qs[2];
-        T *to = key ? (T *)a.k_out + ((int64_t)tok * a.kv_heads + hh) * a.dim
-                    : (T *)a.q_out + ((int64_t)tok * a.heads + hh) * a.dim;
-        float x[2][V], w[2][V], c[V], s[V];
-        lane.load(from, live, x);
-        const float *wv = key ? a.w_k : a.w_q;
-        lane.weights(wv && a.per_head ? wv + (int64_t)hh * a.dim : wv, w);
-        lane.angles(a, tok, l, c, s);
-        lane.normalise(a, x);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            x[0][i] *= w[0][i];
-            x[1][i] *= w[1][i];
-        }
-        lane.turn(x, c, s, 1.0f);
-        if (live)
-            lane.store(to, x);
-    }
-}
-
 // The vectors of weights: one of q and one of k, or one per head; a vector's
 // rows are dealt to its blocks in turn.  Blocks of q's vectors come first.
 struct Vector {
@@ -263,6 +238,89 @@ struct Vector {
     }
 };
 
+// Rows of a block's vector: which token and head, and where the row lies.
+template <class T>
+struct VectorRows {
+    const T *base;
+    int64_t st[3];
+    int of;            // heads of a token among the rows
+    int head, heads;
+    uint32_t rows;
+    Divisor by_of, by_length;
+    int length;
+    __device__ __forceinline__ VectorRows(const HeadNormArgs &a, const Vector &vec)
+        : base(vec.key ? (const T *)a.k : (const T *)a.q), head(vec.head), heads(vec.key ? a.kv_heads : a.heads),
+          by_length(a.by_length), length(a.length)
+    {
+        by_of.m = vec.key ? a.by_kv_heads.m : a.by_heads.m;
+        by_of.s = vec.key ? a.by_kv_heads.s : a.by_heads.s;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            st[i] = vec.key ? a.ks[i] : a.qs[i];
+        of = head < 0 ? heads : 1;
+        rows = (uint32_t)a.batch * a.length * of;
+    }
+    // row e: its token, its place in its sequence, its elements, and where it is in contiguous arrays
+    __device__ __forceinline__ const T *at(uint32_t e, uint32_t &tok, uint32_t &l, int64_t &dense) const
+    {
+        tok = head < 0 ? by_of(e) : e;
+        const uint32_t h = head < 0 ? e - tok * of : (uint32_t)head, b = by_length(tok);
+        l = tok - b * length;
+        dense = (int64_t)tok * heads + h;
+        return base + b * st[0] + l * st[1] + h * st[2];
+    }
+};
+
+// Forward.  A block's rows share a vector of weights, which its lanes keep; the next
+// row's loads are under way while a row is worked on.
+template <class T, int V, bool INTERLEAVED, bool WIDE>
+__global__ __launch_bounds__(kThreads) void k_head_norm_fwd(HeadNormArgs a)
+{
+    using L = Lane<T, V, INTERLEAVED, WIDE>;
+    const int per = kThreads / a.group, j = threadIdx.x & (a.group - 1), g = threadIdx.x / a.group;
+    const L lane(a, j);
+    const Vector vec(a, blockIdx.x);
+    const VectorRows<T> in(a, vec);
+    const uint32_t step = vec.chunks * per;
+    T *to = vec.key ? (T *)a.k_out : (T *)a.q_out;
+    const float *wv = vec.key ? a.w_k : a.w_q;
+    struct Row {
+        float x[2][V], c[V], s[V];
+        int64_t at;
+        bool live;
+    };
+    auto fetch = [&](uint32_t e) {
+        Row r;
+        uint32_t tok, l;
+        r.live = e < in.rows;
+        const T *from = in.at(min(e, in.rows - 1), tok, l, r.at);
+        lane.load(from, r.live, r.x);
+        lane.angles(a, tok, l, r.c, r.s);
+        return r;
+    };
+    float w[2][V];
+    uint32_t e0 = (blockIdx.x - vec.first) * per;
+    if (e0 >= in.rows)
+        return;
+    Row row = fetch(e0 + g);
+    lane.weights(wv && vec.head >= 0 ? wv + (int64_t)vec.head * a.dim : wv, w);
+    for (; e0 < in.rows; e0 += step) {
+        Row next = row;
+        if (e0 + step < in.rows)
+            next = fetch(e0 + step + g);
+        lane.normalise(a, row.x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            row.x[0][i] *= w[0][i];
+            row.x[1][i] *= w[1][i];
+        }
+        lane.turn(row.x, row.c, row.s, 1.0f);
+        if (row.live)
+            lane.store(to + row.at * a.dim, row.x);
+        row = next;
+    }
+}
+
 // Backward.  A block's rows share a vector of weights, whose gradient its lanes
 // sum over them; the block's groups are added in LDS, the blocks by a second
 // kernel, both in a fixed order.
@@ -274,19 +332,17 @@ __global__ __launch_bounds__(kThreads) void k_head_norm_bwd(HeadNormArgs a)
     const int per = kThreads / a.group, j = threadIdx.x & (a.group - 1), g = threadIdx.x / a.group;
     const L lane(a, j);
     const Vector vec(a, blockIdx.x);
-    const int chunk = blockIdx.x - vec.first, heads = vec.key ? a.kv_heads : a.heads, of = vec.head < 0 ? heads : 1;
-    const uint32_t rows = (uint32_t)a.batch * a.length * of;
+    const VectorRows<T> in(a, vec);
     const float *wv = vec.key ? a.w_k : a.w_q;
     float w[2][V], dw[2][V] = {};
     lane.weights(wv && vec.head >= 0 ? wv + (int64_t)vec.head * a.dim : wv, w);
     const float inv = 1.0f / (float)a.dim;
-    for (uint32_t e0 = chunk * per; e0 < rows; e0 += vec.chunks * per) {
-        const uint32_t e = min(e0 + g, rows - 1);
-        const bool live = e0 + g < rows;
-        const uint32_t tok = e / of, h = vec.head < 0 ? e - tok * of : vec.head, b = tok / a.length, l = tok - b * a.length;
-        const T *from = vec.key ? (const T *)a.k + b * a.ks[0] + l * a.ks[1] + h * a.ks[2]
-                                : (const T *)a.q + b * a.qs[0] + l * a.qs[1] + h * a.qs[2];
-        const int64_t at = ((int64_t)tok * heads + h) * a.dim;
+    for (uint32_t e0 = (blockIdx.x - vec.first) * per; e0 < in.rows; e0 += vec.chunks * per) {
+        const bool live = e0 + g < in.rows;
+        uint32_t tok, l;
+        int64_t at;
+        const T *from = in.at(min(e0 + g, in.rows - 1), tok, l, at);
+        at *= a.dim;
         float x[2][V], y[2][V], c[V], s[V];
         lane.load(from, live, x);
         lane.load((const T *)(vec.key ? a.gk : a.gq) + at, live, y);
@@ -386,30 +442,37 @@ int lanes_of(const pam_head_norm_desc_t &d, int v)
     return g;
 }
 
-// The backward pass's blocks: four per CU where there are rows for that, at
-// least eight turns of the block's rows each.
-constexpr int kBwdBlocks = 1024;
+// Blocks of a pass where there are rows for that, and the turns of its rows that a block
+// takes at least.
+constexpr int kFwdBlocks = 2048, kFwdTurns = 2, kBwdBlocks = 1024, kBwdTurns = 8;
 
-Shape shape_of(const pam_head_norm_desc_t &d, int v, bool wide)
+Shape shape_of(const pam_head_norm_desc_t &d, bool backward, int v, bool wide)
 {
     Shape s{v, lanes_of(d, v), 1, 1, wide};
     const int64_t tokens = (int64_t)d.batch * d.length, per = kThreads / s.group;
+    const int64_t blocks = backward ? kBwdBlocks : kFwdBlocks, turns = backward ? kBwdTurns : kFwdTurns;
     auto chunks = [&](int64_t rows, int64_t share) {
-        return (int)std::max<int64_t>(1, std::min<int64_t>(share, rows / (per * 8)));
+        return (int)std::max<int64_t>({1, std::min<int64_t>(share, rows / (per * turns))});
     };
     const int64_t all = d.heads + d.kv_heads;
     if (d.w_per_head) {
-        s.chunks_q = s.chunks_k = chunks(tokens, std::max<int64_t>(1, kBwdBlocks / all));
+        s.chunks_q = s.chunks_k = chunks(tokens, std::max<int64_t>(1, blocks / all));
     } else {
-        s.chunks_q = chunks(tokens * d.heads, std::max<int64_t>(1, kBwdBlocks * (int64_t)d.heads / all));
-        s.chunks_k = chunks(tokens * d.kv_heads, std::max<int64_t>(1, kBwdBlocks * (int64_t)d.kv_heads / all));
+        s.chunks_q = chunks(tokens * d.heads, std::max<int64_t>(1, blocks * (int64_t)d.heads / all));
+        s.chunks_k = chunks(tokens * d.kv_heads, std::max<int64_t>(1, blocks * (int64_t)d.kv_heads / all));
+    }
+    if (!backward && (tokens * all) / per < blocks) {  // few rows: a turn each, in blocks of their own
+        auto turn = [&](int64_t rows) { return (int)std::max<int64_t>(1, (rows + per - 1) / per); };
+        s.chunks_q = turn(d.w_per_head ? tokens : tokens * d.heads);
+        s.chunks_k = turn(d.w_per_head ? tokens : tokens * d.kv_heads);
     }
     return s;
 }
 
 // The widest groups of channels, of 8 or 4, that divide a row's parts and the
 // place of every row; else 8, one by one.
-Shape shape_of(const pam_head_norm_desc_t &d, uint64_t places, const float *w_q, const float *w_k, const float *table)
+Shape shape_of(const pam_head_norm_desc_t &d, bool backward, uint64_t places, const float *w_q, const float *w_k,
+               const float *table)
 {
     const int es = d.dtype == PAM_F32 ? 4 : 2;
     uint64_t all = (uint64_t)(d.pairs | d.dim) | places / es;
@@ -419,11 +482,11 @@ Shape shape_of(const pam_head_norm_desc_t &d, uint64_t places, const float *w_q,
     if (vectors % 16 == 0 && places % es == 0) {
         // f32: eight are two accesses of 16 bytes, which every place has to be a multiple of
         if (all % 8 == 0)
-            return shape_of(d, 8, true);
+            return shape_of(d, backward, 8, true);
         if (all % 4 == 0 && lanes_of(d, 4) <= 64)
-            return shape_of(d, 4, true);
+            return shape_of(d, backward, 4, true);
     }
-    return shape_of(d, 8, false);
+    return shape_of(d, backward, 8, false);
 }
 
 HeadNormArgs args_of(const pam_head_norm_desc_t &d, const Shape &s, const void *q, const void *k, const float *w_q,
@@ -454,19 +517,20 @@ HeadNormArgs args_of(const pam_head_norm_desc_t &d, const Shape &s, const void *
     a.layer = d.norm == PAM_NORM_LAYER;
     a.per_head = d.w_per_head != 0;
     a.eps = d.eps;
+    a.by_length = Divisor::of(std::max(d.length, 1));
+    a.by_heads = Divisor::of(d.heads);
+    a.by_kv_heads = Divisor::of(std::max(d.kv_heads, 1));
     return a;
 }
 
 template <class T, int V, bool INTERLEAVED, bool WIDE>
-hipError_t launch_as(const HeadNormArgs &a, const Shape &sh, int64_t bwd_blocks, hipStream_t s)
+hipError_t launch_as(const HeadNormArgs &a, const Shape &sh, unsigned blocks, bool backward, hipStream_t s)
 {
-    if (bwd_blocks < 0) {
-        const int64_t per = kThreads / sh.group, rows = (int64_t)a.batch * a.length * (a.heads + a.kv_heads);
-        hipLaunchKernelGGL((k_head_norm_fwd<T, V, INTERLEAVED, WIDE>),
-                           dim3((unsigned)std::min<int64_t>((rows + per - 1) / per, 1 << 20)), dim3(kThreads), 0, s, a);
+    if (!backward) {
+        hipLaunchKernelGGL((k_head_norm_fwd<T, V, INTERLEAVED, WIDE>), dim3(blocks), dim3(kThreads), 0, s, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((k_head_norm_bwd<T, V, INTERLEAVED, WIDE>), dim3((unsigned)bwd_blocks), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_head_norm_bwd<T, V, INTERLEAVED, WIDE>), dim3(blocks), dim3(kThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !(a.gw_q || a.gw_k))
         return e;
@@ -478,25 +542,26 @@ hipError_t launch_as(const HeadNormArgs &a, const Shape &sh, int64_t bwd_blocks,
 }
 
 template <class T>
-hipError_t launch_type(const HeadNormArgs &a, const Shape &sh, bool interleaved, int64_t bwd_blocks, hipStream_t s)
+hipError_t launch_type(const HeadNormArgs &a, const Shape &sh, bool interleaved, unsigned blocks, bool backward,
+                       hipStream_t s)
 {
     if (!sh.wide)
-        return interleaved ? launch_as<T, 8, true, false>(a, sh, bwd_blocks, s)
-                           : launch_as<T, 8, false, false>(a, sh, bwd_blocks, s);
+        return interleaved ? launch_as<T, 8, true, false>(a, sh, blocks, backward, s)
+                           : launch_as<T, 8, false, false>(a, sh, blocks, backward, s);
     if (sh.v == 8)
-        return interleaved ? launch_as<T, 8, true, true>(a, sh, bwd_blocks, s)
-                           : launch_as<T, 8, false, true>(a, sh, bwd_blocks, s);
-    return interleaved ? launch_as<T, 4, true, true>(a, sh, bwd_blocks, s)
-                       : launch_as<T, 4, false, true>(a, sh, bwd_blocks, s);
+        return interleaved ? launch_as<T, 8, true, true>(a, sh, blocks, backward, s)
+                           : launch_as<T, 8, false, true>(a, sh, blocks, backward, s);
+    return interleaved ? launch_as<T, 4, true, true>(a, sh, blocks, backward, s)
+                       : launch_as<T, 4, false, true>(a, sh, blocks, backward, s);
 }
 
-hipError_t launch_any(int32_t dtype, const HeadNormArgs &a, const Shape &sh, bool interleaved, int64_t bwd_blocks,
+hipError_t launch_any(int32_t dtype, const HeadNormArgs &a, const Shape &sh, bool interleaved, unsigned blocks, bool backward,
                       hipStream_t s)
 {
     if (dtype == PAM_F32)
-        return launch_type<float>(a, sh, interleaved, bwd_blocks, s);
-    return dtype == PAM_F16 ? launch_type<f16>(a, sh, interleaved, bwd_blocks, s)
-                            : launch_type<bf16>(a, sh, interleaved, bwd_blocks, s);
+        return launch_type<float>(a, sh, interleaved, blocks, backward, s);
+    return dtype == PAM_F16 ? launch_type<f16>(a, sh, interleaved, blocks, backward, s)
+                            : launch_type<bf16>(a, sh, interleaved, blocks, backward, s);
 }
 
 }  // namespace
@@ -505,11 +570,11 @@ hipError_t launch_head_norm_fwd(const pam_head_norm_desc_t &d, const void *q, co
                                 const float *w_k, const float *table, const int32_t *pos, void *q_out, void *k_out,
                                 hipStream_t s)
 {
-    const Shape sh = shape_of(d, (uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out, w_q, w_k, table);
+    const Shape sh = shape_of(d, false, (uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out, w_q, w_k, table);
     HeadNormArgs a = args_of(d, sh, q, k, w_q, w_k, table, pos);
     a.q_out = q_out;
     a.k_out = k_out;
-    return launch_any(d.dtype, a, sh, d.flags & PAM_ROTARY_INTERLEAVED, -1, s);
+    return launch_any(d.dtype, a, sh, d.flags & PAM_ROTARY_INTERLEAVED, (unsigned)sh.blocks(d), false, s);
 }
 
 // by the descriptor alone: the largest of what the widths take
@@ -519,7 +584,7 @@ size_t head_norm_bwd_workspace(const pam_head_norm_desc_t &d)
     for (int v = 4; v <= 8; v += 4) {
         if (lanes_of(d, v) > 64)
             continue;
-        const Shape s = shape_of(d, v, true);
+        const Shape s = shape_of(d, true, v, true);
         most = std::max(most, s.blocks(d) * s.group * 2 * v);
     }
     return (size_t)most * sizeof(float);
@@ -530,7 +595,7 @@ hipError_t launch_head_norm_bwd(const pam_head_norm_desc_t &d, const void *q, co
                                 const void *gk_out, void *gq, void *gk, float *gw_q, float *gw_k, void *workspace,
                                 hipStream_t s)
 {
-    const Shape sh = shape_of(d, (uintptr_t)q | (uintptr_t)k | (uintptr_t)gq_out | (uintptr_t)gk_out | (uintptr_t)gq |
+    const Shape sh = shape_of(d, true, (uintptr_t)q | (uintptr_t)k | (uintptr_t)gq_out | (uintptr_t)gk_out | (uintptr_t)gq |
                                      (uintptr_t)gk,
                               w_q, w_k, table);
     HeadNormArgs a = args_of(d, sh, q, k, w_q, w_k, table, pos);
@@ -541,7 +606,7 @@ hipError_t launch_head_norm_bwd(const pam_head_norm_desc_t &d, const void *q, co
     a.gw_q = gw_q;
     a.gw_k = gw_k;
     a.part = (float *)workspace;
-    return launch_any(d.dtype, a, sh, d.flags & PAM_ROTARY_INTERLEAVED, sh.blocks(d), s);
+    return launch_any(d.dtype, a, sh, d.flags & PAM_ROTARY_INTERLEAVED, (unsigned)sh.blocks(d), true, s);
 }
 
 }  // namespace pam

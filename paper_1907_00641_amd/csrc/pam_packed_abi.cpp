@@ -322,7 +322,9 @@ pam_status_t pam_cache_write(const pam_cache_desc_t *desc, const pam_cache_rows_
     } else {
         r.rows = (int64_t)d.sequences * r.length;
     }
-    REQUIRE(r.rows >= 0 && r.rows <= kMost31, "rows must be less than 2^31");
+    // tokens are taken in whole blocks of 16
+    REQUIRE(r.rows >= 0 && ((__int128)r.rows + 16) * d.kv_heads * d.maps <= kMost31,
+            "(rows + 16) kv_heads maps must be less than 2^31");
     if (r.rows == 0 || d.sequences == 0 || d.table_width == 0)
         return PAM_OK;
     REQUIRE(k && v, "a pointer is NULL");
@@ -348,7 +350,8 @@ pam_status_t pam_cache_read(const pam_cache_desc_t *desc, int32_t length, const 
     CHECK(check_cache(desc));
     const pam_cache_desc_t &d = *desc;
     REQUIRE(length >= 0, "length must not be negative");
-    REQUIRE((__int128)d.sequences * length * d.kv_heads < (__int128)1 << 40, "sequences length kv_heads must be less than 2^40");
+    REQUIRE(((__int128)d.sequences * length + 16) * d.kv_heads * d.maps <= kMost31,
+            "(sequences length + 16) kv_heads maps must be less than 2^31");
     if (length == 0 || d.sequences == 0 || (!k && !v))
         return PAM_OK;
     Pool p;

@@ -23,8 +23,9 @@ struct PagedPlan {
     int64_t units, floats;
 };
 
-// The keys are split so that the units fill the card, with two tiles of 32 keys or
-// more for every wave of a part.
+// The keys are split so that the units fill the card once, unless a wave of a part had fewer
+// than two tiles of 32 keys then.  (16 sequences of up to 16384, 8 key heads: twice or four times
+// as many parts 103 and 116 us for 100, before shares went by lengths.)
 PagedPlan plan_of(const pam_cache_desc_t &c, const pam_paged_attn_desc_t &d)
 {
     PagedPlan p;
@@ -34,10 +35,11 @@ PagedPlan plan_of(const pam_cache_desc_t &c, const pam_paged_attn_desc_t &d)
     p.units = (int64_t)c.sequences * c.kv_heads * p.tiles;
     const int64_t table = (int64_t)c.table_width * c.page_size;
     const int64_t bound = d.key_bound ? std::min<int64_t>(d.key_bound, table) : table;
-    const int64_t most = ceil_div(bound, 32 * 4 * 2), fill = p.units ? at_once(c) / p.units : 1;
+    const int64_t most = bound / (32 * 4 * 2), fill = p.units ? at_once(c) / p.units : 1;
     p.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({most, fill, 256}));
     const int64_t width = paged_class(c.maps * c.dim, c.dim_v);
-    p.floats = p.parts > 1 ? p.units * p.parts * p.live * (width + 2) : 0;
+    // the blocks' sums, and two numbers for every unit
+    p.floats = p.parts > 1 ? p.units * (p.parts * p.live * (width + 2) + 2) : 0;
     return p;
 }
 
@@ -59,6 +61,7 @@ hipError_t launch_paged(const pam_cache_desc_t &c, const pam_paged_attn_desc_t &
     a.q_len = q_len;
     a.out = out;
     a.part = (float *)workspace;
+    a.cuts = (int2 *)(a.part + p.floats - 2 * p.units);
     a.heads = d.heads;
     a.group = d.heads / c.kv_heads;
     a.len_q = d.len_q;
@@ -74,11 +77,13 @@ hipError_t launch_paged(const pam_cache_desc_t &c, const pam_paged_attn_desc_t &
         a.qs[i] = i == 3 && c.maps == 1 ? 0 : d.q_stride[i];
         a.q_wide = a.q_wide && a.qs[i] % per == 0;
     }
-    // rows of whole eights, which begin at multiples of eight elements
-    const bool wide = c.maps * c.dim % 8 == 0 && c.dim_v % 8 == 0;
+    a.by_page = Divisor::of(c.page_size);
+    // rows of whole pieces, which begin at multiples of them
+    const int both = c.maps * c.dim | c.dim_v;
+    const int piece = both % 16 == 0 && (c.store == PAM_STORE_E4M3 || c.store == PAM_STORE_INT8) ? 16 : (both % 8 ? 0 : 8);
     if (c.dtype == PAM_F32)
-        return paged_f32(a, c.store, wide, s);
-    return c.dtype == PAM_F16 ? paged_f16(a, c.store, wide, s) : paged_bf16(a, c.store, wide, s);
+        return paged_f32(a, c.store, piece, s);
+    return c.dtype == PAM_F16 ? paged_f16(a, c.store, piece, s) : paged_bf16(a, c.store, piece, s);
 }
 
 }  // namespace pam

@@ -3,6 +3,9 @@
 
 namespace pam {
 
-hipError_t paged_bf16(const PagedArgs &a, int store, bool wide, hipStream_t s) { return paged_type<bf16>(a, store, wide, s); }
+hipError_t paged_bf16(const PagedArgs &a, int store, int piece, hipStream_t s)
+{
+    return paged_type<bf16>(a, store, piece, s);
+}
 
 }  // namespace pam

@@ -3,6 +3,9 @@
 
 namespace pam {
 
-hipError_t paged_f32(const PagedArgs &a, int store, bool wide, hipStream_t s) { return paged_type<float>(a, store, wide, s); }
+hipError_t paged_f32(const PagedArgs &a, int store, int piece, hipStream_t s)
+{
+    return paged_type<float>(a, store, piece, s);
+}
 
 }  // namespace pam

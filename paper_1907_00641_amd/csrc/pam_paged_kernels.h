@@ -19,12 +19,12 @@ namespace pam {
 namespace {
 
 constexpr int kPagedWaves = 4;
+constexpr int kPagedLeast = 2;  // tiles of 32 keys that a wave of a part has at the least
 
 template <class T, int C>
 struct PagedSizes {
     using R = Rows<T, C>;
     static constexpr int CK = C / kChunk<T>, TV = C / 32, CP = 32 / kChunk<T>;
-    static constexpr int kPieces = C / 16;       // pieces of eight elements of a tile of 32 rows that a lane brings
     static constexpr int kTile = R::size(32);
     static constexpr int kScales = 3 * 32 * 4;   // of a tile: both maps' keys, values
     // waves per SIMD that the registers are for
@@ -34,61 +34,83 @@ struct PagedSizes {
     static constexpr int bytes(int live) { return kPagedWaves * (wave_bytes(live) + kScales); }
 };
 
-// A tile's rows on their way from the pool: pieces of eight elements, in registers.
-template <class T, class S, int C, bool WIDE>
+// A tile's rows on their way from the pool, in registers: pieces of PE elements, read in
+// accesses of up to 16 bytes from wherever there is a row (rows that there are not, and channels
+// past a row's, repeat others and are cleared on their way to LDS); PE 0: pieces of
+// eight, element by element.
+template <class T, class S, int C, int PE>
 struct Staged {
-    using Z = PagedSizes<T, C>;
-    static constexpr int kPer = C / 8;  // pieces of a row
-    Stored8<S> x[Z::kPieces];
+    static constexpr int E = PE ? PE : 8, kPer = C / E, N = C / (2 * E);  // pieces of a row, of a lane
+    static constexpr int kWords = E * sizeof(S) / 4;
+    uint32_t x[N][kWords], live;  // live: bit n: piece n is a row's
     __device__ __forceinline__ static int row_of(int n) { return n * (64 / kPer) + lane_id() / kPer; }
-    __device__ __forceinline__ static int channel() { return lane_id() % kPer * 8; }
+    __device__ __forceinline__ static int channel() { return lane_id() % kPer * E; }
     // rows of `dim` elements from `pool`; lane j has the number of row j of the tile,
-    // negative: 0
+    // negative: there is none
     __device__ __forceinline__ void load(const S *pool, int rid, int dim)
     {
-        const int c = channel(), m = max(min(dim - c, 8), 0);
+        const int c = channel();
+        live = 0;
 #pragma unroll
-        for (int n = 0; n < Z::kPieces; ++n) {
+        for (int n = 0; n < N; ++n) {
             const int r = __shfl(rid, row_of(n));
-            const S *p = pool + (int64_t)r * dim + c;
-            x[n] = Stored8<S>{};
-            if constexpr (WIDE) {
-                if (r >= 0 && m > 0)
-                    x[n] = load_stored(p);
+            live |= (r >= 0 && c < dim ? 1u : 0u) << n;
+            if constexpr (PE != 0) {
+                const S *p = pool + (int64_t)max(r, 0) * dim + min(c, dim - E);
+                __builtin_memcpy(x[n], __builtin_assume_aligned(p, sizeof(x[n]) > 16 ? 16 : sizeof(x[n])), sizeof(x[n]));
             } else {
-                x[n] = load_stored_some(p, r >= 0 ? m : 0);
+                const Stored8<S> y = load_stored_some(pool + (int64_t)r * dim + c, r >= 0 ? max(min(dim - c, 8), 0) : 0);
+#pragma unroll
+                for (int i = 0; i < kWords; ++i)
+                    x[n][i] = y.w[i];
             }
         }
     }
     // to the tile, as T; SCALED: times the row's factor, which lane j has of row j
     template <bool SCALED>
-    __device__ __forceinline__ void put(char *tile, float scale) const
+    __device__ __forceinline__ void put(char *tile, float scale)
     {
-        using R = typename Z::R;
+        using R = typename PagedSizes<T, C>::R;
+        if (__any(live != (1u << N) - 1)) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int i = 0; i < kWords; ++i)
+                    x[n][i] = live >> n & 1 ? x[n][i] : 0;
+        }
         const int c = channel();
 #pragma unroll
-        for (int n = 0; n < Z::kPieces; ++n) {
+        for (int n = 0; n < N; ++n) {
             const int row = row_of(n);
-            if constexpr (std::is_same<T, S>::value) {
+            uint32_t y[E * sizeof(T) / 4];
+            if constexpr (!kScaled<S>) {
 #pragma unroll
-                for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-                    store16(tile + R::at(row, c * (int)sizeof(T) / 16 + i),
-                            uint4v{x[n].w[4 * i], x[n].w[4 * i + 1], x[n].w[4 * i + 2], x[n].w[4 * i + 3]});
-            } else {
-                float y[8];
-                unpack<S>(x[n], y);
-                if constexpr (SCALED) {
-                    const float f = __shfl(scale, row);
+                for (int i = 0; i < kWords; ++i)
+                    y[i] = x[n][i];
+            } else if constexpr (!SCALED) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        y[j] *= f;
+                for (int i = 0; i < kWords; ++i) {
+                    uint32_t z[sizeof(T)];
+                    widen<T, S>(x[n][i], z);
+#pragma unroll
+                    for (int k = 0; k < (int)sizeof(T); ++k)
+                        y[i * sizeof(T) + k] = z[k];
                 }
-                const Stored8<T> t = pack<T>(y);
+            } else {
+                const float f = __shfl(scale, row);
 #pragma unroll
-                for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-                    store16(tile + R::at(row, c * (int)sizeof(T) / 16 + i),
-                            uint4v{t.w[4 * i], t.w[4 * i + 1], t.w[4 * i + 2], t.w[4 * i + 3]});
+                for (int i = 0; i < kWords; ++i) {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    uint32_t z[4];
+                    widen<float, S>(x[n][i], z);
+                    const T4 t = {(T)(__uint_as_float(z[0]) * f), (T)(__uint_as_float(z[1]) * f),
+                                  (T)(__uint_as_float(z[2]) * f), (T)(__uint_as_float(z[3]) * f)};
+                    __builtin_memcpy(y + i * sizeof(T), &t, sizeof(t));
+                }
             }
+#pragma unroll
+            for (int i = 0; i < E * (int)sizeof(T) / 16; ++i)
+                store16(tile + R::at(row, c * (int)sizeof(T) / 16 + i), uint4v{y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]});
         }
     }
 };
@@ -143,13 +165,81 @@ __device__ __forceinline__ void paged_out(const PagedArgs &a, int b, int hk, int
         store4<T, false>(out, ch, a.pool.dim_v, y);
 }
 
-// A block takes a part of a unit's keys (a unit: 32 rows of one key head of one
+// How the blocks of a head's tile of rows are shared among the sequences: `shares` blocks,
+// so many to a sequence as its keys take in runs of one length, the shortest that the blocks
+// suffice for; a sequence to a lane.  More than 64 sequences: as many to each.  (16 sequences of
+// half to all of 16384 keys: 94 us for 97 with as many to each.)
+struct Shares {
+    int n, first;  // of this lane's sequence (up to 64 sequences): blocks, and the first of them
+    bool equal;
+    int each;
+    __device__ __forceinline__ explicit Shares(const PagedArgs &a)
+    {
+        const int B = a.pool.sequences, shares = B * a.parts;
+        equal = B > 64 || a.parts == 1;
+        each = a.parts;
+        n = first = 0;
+        if (equal)
+            return;
+        const int l = lane_id(), t = l < B ? (cached(a.pool, l) + 31) / 32 : 0;
+        // blocks at runs of s tiles: the quotient rounded up, exactly
+        auto blocks = [&](int s) {
+            int k = (int)((float)t * (1.0f / (float)s));
+            k += (int64_t)k * s < t;
+            k += (int64_t)k * s < t;
+            k -= (int64_t)(k - 1) * s >= t;
+            k -= (int64_t)(k - 1) * s >= t;
+            return l < B ? max(k, 1) : 0;
+        };
+        // Runs of all / (shares - B) tiles always suffice: each sequence has less than a block
+        // more than its tiles over that.  Shorter ones than all / shares do not.  (Sums in 32
+        // bits are off by a relative 2^-21 at the most.)
+        const float all = lanes_sum<64>((float)t);
+        const int least = kPagedLeast * kPagedWaves;
+        int lo = max((int)uniform_float(all / (float)shares), least) - 1;
+        int hi = max((int)uniform_float(__builtin_ceilf(all / (float)(shares - B) * (1.0f + 0x1p-20f))) + 1, lo + 1);
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (uniform_float(lanes_sum<64>((float)blocks(mid))) <= (float)shares)
+                hi = mid;
+            else
+                lo = mid;
+        }
+        n = blocks(hi);
+        int upto = n;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const int x = __shfl_up(upto, s);
+            upto += l >= s ? x : 0;
+        }
+        first = upto - n;
+    }
+    // the sequence of block r, its part and their number; -1: none
+    __device__ __forceinline__ int find(int r, int &part, int &parts) const
+    {
+        if (equal) {
+            const int b = r / each;
+            part = r - b * each;
+            parts = each;
+            return b;
+        }
+        const uint64_t one = __ballot(r >= first && r < first + n);
+        if (!one)
+            return -1;
+        const int b = __builtin_ctzll(one);
+        part = r - uniform(__shfl(first, b));
+        parts = uniform(__shfl(n, b));
+        return b;
+    }
+};
+
+// A block takes a part of the keys of a unit (32 rows of one key head of one
 // sequence), and every wave a run of tiles of 32 keys of it.  A tile is brought from
 // its pages to registers while the one before is worked on, turned into the
 // queries' type on its way to LDS (e4m3 and int8 numbers are exact there), and
 // read as operands from there: the values straight after the keys, in the same
 // place.  The waves meet in LDS at the end.
-template <class T, class S, int C, bool WIDE>
+template <class T, class S, int C, int PE>
 __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)) void k_paged(PagedArgs a)
 {
     using Z = PagedSizes<T, C>;
@@ -164,13 +254,16 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
     char *tile = lds + w * stride;
     float *scales = reinterpret_cast<float *>(lds + kPagedWaves * stride + w * Z::kScales);
     const uint32_t kr = lds_address(tile) + R::row_lane(), vc = lds_address(tile) + R::col_lane();
-    const uint32_t items = (uint32_t)a.units * a.parts;
+    const uint32_t items = (uint32_t)a.units * a.parts, heads = a.pool.kv_heads * a.tiles;
+    const Shares shares(a);
     for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
-        const uint32_t unit = uniform(n / a.parts);
-        const int part = n - unit * a.parts;
-        const uint32_t head = uniform(unit / a.tiles);
-        const int rt = unit - head * a.tiles, b = uniform(head / a.pool.kv_heads), hk = head - b * a.pool.kv_heads;
-        const int nk = uniform(cached(a.pool, b));
+        const uint32_t share = uniform(n / heads), head = n - share * heads;
+        int part, parts;
+        const int b = uniform(shares.find(share, part, parts));
+        if (b < 0)  // the same in the whole block
+            continue;
+        const int hk = uniform(head / a.tiles), rt = head - hk * a.tiles;
+        const int nk = a.pool.pages ? uniform(cached(a.pool, b)) : 0;
         const int nq = uniform(a.q_len ? min(max(a.q_len[b], 0), a.len_q) : a.len_q);
         // this lane's row
         const int r = rt * 32 + (l & 31), x = r / a.pool.maps, m = r - x * a.pool.maps;
@@ -187,18 +280,18 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
         wall = uniform(wall);
         int from, to;
         {
-            const int trips = (wend + 31) / 32, runs = a.parts * kPagedWaves, per = trips / runs, more = trips - per * runs;
+            const int trips = (wend + 31) / 32, runs = parts * kPagedWaves, per = trips / runs, more = trips - per * runs;
             const int run = part * kPagedWaves + w;  // runs differ by a tile at the most
             from = uniform(run * per + min(run, more));
             to = uniform(from + per + (run < more));
         }
 
-        Staged<T, S, C, WIDE> ks, vs;
+        Staged<T, S, C, PE> ks, vs;
         int rid = -1, next = -1;          // rows of the tile under way, and of the one after
         float sk0 = 0.0f, sk1 = 0.0f, sv = 0.0f;
         auto find = [&](int t) {          // lane j: row of key j of tile t
             const int j = t * 32 + (l & 31);
-            return j < wend ? cache_row(a.pool, b, hk, j) : -1;
+            return j < wend ? cache_row(a.pool, a.by_page, b, hk, j) : -1;
         };
         auto fetch_keys = [&]() {
             ks.load((const S *)a.pool.k, rid, a.pool.maps * a.pool.dim);
@@ -347,7 +440,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
                 });
         };
         const int rows = min(a.rows - rt * 32, 32);
-        if (a.parts == 1) {
+        if (parts == 1) {
             const int outs = rows / a.pool.maps;
             for (int e = threadIdx.x; e < outs * (C / 4); e += 64 * kPagedWaves) {
                 const int ch = e % (C / 4) * 4;
@@ -366,93 +459,127 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
                         make_float2(j.top, j.sum);
             }
         }
+        // for the join: the unit's first block and their number
+        if (a.parts > 1 && part == 0 && threadIdx.x == 0)
+            a.cuts[(uint32_t)b * heads + head] = make_int2(share, parts);
         __syncthreads();
     }
 }
 
-// Joins the parts of every unit: a block per output row, its threads in teams that
-// take every so-manieth part of four channels each.
-constexpr int kJoinThreads = 256;
+// Joins the parts of the units that have several: a block per output row, its threads in
+// teams that take every so-manieth part of four channels each.  What bounds it is the loads'
+// latency: four parts of both maps are under way together.
+constexpr int kJoinThreads = 1024;  // the most
 
 template <class T, int C>
 __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a)
 {
-    constexpr int QUADS = C / 4, TEAMS = kJoinThreads / QUADS;
-    __shared__ Joined s[TEAMS][QUADS];
-    const int team = threadIdx.x / QUADS, quad = threadIdx.x % QUADS, ch = quad * 4;
-    const int64_t items = (int64_t)a.units * a.parts;
-    const uint32_t per = a.live / a.pool.maps;  // output rows of a unit
+    constexpr int QUADS = C / 4, MOST = kJoinThreads / QUADS, AHEAD = 4;
+    __shared__ float2 s[2][MOST];
+    __shared__ float4v so[2][MOST][QUADS];
+    const int teams = blockDim.x / QUADS, team = threadIdx.x / QUADS, quad = threadIdx.x % QUADS, ch = quad * 4;
+    const int maps = a.pool.maps;
+    const float2 *stats = reinterpret_cast<const float2 *>(a.part + (int64_t)a.units * a.parts * a.live * C);
+    const uint32_t per = a.live / maps, heads = a.pool.kv_heads * a.tiles;  // per: output rows of a unit
     const uint32_t rows = (uint32_t)a.units * per;
     for (uint32_t e = blockIdx.x; e < rows; e += gridDim.x) {
-        const uint32_t unit = e / per, head = unit / a.tiles;
-        const int rt = unit - head * a.tiles, b = head / a.pool.kv_heads, hk = head - b * a.pool.kv_heads;
-        const int x = rt * 32 / a.pool.maps + (e - unit * per);
-        if (x * a.pool.maps >= a.rows)  // the same in every thread
+        const uint32_t unit = e / per, b = unit / heads, head = unit - b * heads;
+        const int hk = head / a.tiles, rt = head - hk * a.tiles;
+        const int x = rt * 32 / maps + (e - unit * per);
+        const int2 cut = a.cuts[unit];
+        const int from = cut.x, parts = cut.y;
+        if (x * maps >= a.rows || parts == 1)  // the same in every thread
             continue;
-        Joined mine[2] = {};
+        float top[2] = {-INFINITY, -INFINITY}, sum[2] = {};
+        float4v o[2] = {};
+        for (int p0 = team; p0 < parts; p0 += AHEAD * teams) {
+            float2 st[AHEAD][2];
+            float4v y[AHEAD][2];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int p = min(p0 + k * teams, parts - 1);
+                const int64_t at = ((int64_t)(from + p) * heads + head) * a.live + x * maps - rt * 32;
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const int64_t row = at + (m < maps ? m : 0);
+                    st[k][m] = stats[row];
+                    y[k][m] = *reinterpret_cast<const float4v *>(a.part + row * C + ch);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    if (p0 + k * teams >= parts || st[k][m].y == 0.0f)  // saw nothing
+                        continue;
+                    // a top of -inf beside a sum that is not 0: a NaN
+                    const float to = __builtin_fmaxf(top[m], st[k][m].x);
+                    const float f0 = top[m] == -INFINITY ? (sum[m] == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(top[m] - to);
+                    const float f1 = st[k][m].x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st[k][m].x - to);
+                    o[m] = o[m] * f0 + y[k][m] * f1;
+                    sum[m] = sum[m] * f0 + st[k][m].y * f1;
+                    top[m] = to;
+                }
+        }
+        __syncthreads();
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            if (m == a.pool.maps)
-                break;
-            const int row = x * a.pool.maps + m - rt * 32;
-            auto at = [&](int p) { return ((int64_t)unit * a.parts + min(team + p * TEAMS, a.parts - 1)) * a.live + row; };
-            const int n = team < a.parts ? (a.parts - team + TEAMS - 1) / TEAMS : 0;
-            mine[m] = joined(
-                n, [&](int p) { return *reinterpret_cast<const float2 *>(a.part + items * a.live * C + at(p) * 2); },
-                [&](int p) { return *reinterpret_cast<const float4v *>(a.part + at(p) * C + ch); });
+            if (quad == 0)
+                s[m][team] = make_float2(top[m], sum[m]);
+            so[m][team][quad] = o[m];
         }
-        Joined r[2] = {};
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            if (m == a.pool.maps)
-                break;
-            __syncthreads();
-            s[team][quad] = mine[m];
-            __syncthreads();
-            r[m] = joined(
-                TEAMS, [&](int p) { return make_float2(s[p][quad].top, s[p][quad].sum); },
-                [&](int p) { return s[p][quad].o; });
-        }
+        __syncthreads();
         if (team == 0 && ch < a.pool.dim_v)
-            paged_out<T>(a, b, hk, x, ch, [&](int row) { return row == x * a.pool.maps ? r[0] : r[1]; });
+            paged_out<T>(a, b, hk, x, ch, [&](int row) {
+                const int m = row - x * maps;
+                return joined(
+                    min(teams, parts), [&](int p) { return s[m][p]; }, [&](int p) { return so[m][p][quad]; });
+            });
     }
 }
 
-template <class T, class S, int C, bool WIDE>
-hipError_t paged_class_launch(const PagedArgs &a, hipStream_t s)
+template <class T, class S, int C, int PE>
+hipError_t paged_launch(const PagedArgs &a, hipStream_t s)
 {
     using Z = PagedSizes<T, C>;
-    hipError_t e = launch_lds<k_paged<T, S, C, WIDE>>(item_blocks((int64_t)a.units * a.parts), 64 * kPagedWaves,
-                                                      Z::bytes(a.live), a, s);
+    hipError_t e = launch_lds<k_paged<T, S, C, PE>>(item_blocks((int64_t)a.units * a.parts), 64 * kPagedWaves,
+                                                    Z::bytes(a.live), a, s);
     if (e != hipSuccess || a.parts == 1)
         return e;
     const unsigned rows = (unsigned)std::min<int64_t>((int64_t)a.units * (a.live / a.pool.maps), 1 << 23);
-    hipLaunchKernelGGL((k_paged_join<T, C>), dim3(rows), dim3(kJoinThreads), 0, s, a);
+    // enough teams for a round or two of the loads
+    const int64_t threads = (int64_t)C / 4 * std::max(a.parts / 4, 4);
+    hipLaunchKernelGGL((k_paged_join<T, C>), dim3(rows), dim3(threads <= 256 ? 256 : kJoinThreads), 0, s, a);
     return hipGetLastError();
 }
 
-template <class T, class S, bool WIDE>
-hipError_t paged_wide(const PagedArgs &a, hipStream_t s)
+template <class T, class S, int PE>
+hipError_t paged_class_launch(const PagedArgs &a, hipStream_t s)
 {
     switch (paged_class(a.pool.maps * a.pool.dim, a.pool.dim_v)) {
-    case 64: return paged_class_launch<T, S, 64, WIDE>(a, s);
-    case 128: return paged_class_launch<T, S, 128, WIDE>(a, s);
-    default: return paged_class_launch<T, S, 256, WIDE>(a, s);
+    case 64: return paged_launch<T, S, 64, PE>(a, s);
+    case 128: return paged_launch<T, S, 128, PE>(a, s);
+    default: return paged_launch<T, S, 256, PE>(a, s);
     }
 }
 
+// piece: the elements that every row is whole pieces of: 16 (types of 8 bits), 8, or 0
 template <class T, class S>
-hipError_t paged_store(const PagedArgs &a, bool wide, hipStream_t s)
+hipError_t paged_store(const PagedArgs &a, int piece, hipStream_t s)
 {
-    return wide ? paged_wide<T, S, true>(a, s) : paged_wide<T, S, false>(a, s);
+    if constexpr (kScaled<S>) {
+        if (piece == 16)
+            return paged_class_launch<T, S, 16>(a, s);
+    }
+    return piece ? paged_class_launch<T, S, 8>(a, s) : paged_class_launch<T, S, 0>(a, s);
 }
 
 template <class T>
-hipError_t paged_type(const PagedArgs &a, int store, bool wide, hipStream_t s)
+hipError_t paged_type(const PagedArgs &a, int store, int piece, hipStream_t s)
 {
     if (store == PAM_STORE_E4M3)
-        return paged_store<T, e4m3>(a, wide, s);
-    return store == PAM_STORE_INT8 ? paged_store<T, int8>(a, wide, s) : paged_store<T, T>(a, wide, s);
+        return paged_store<T, e4m3>(a, piece, s);
+    return store == PAM_STORE_INT8 ? paged_store<T, int8>(a, piece, s) : paged_store<T, T>(a, piece, s);
 }
 
 }  // namespace

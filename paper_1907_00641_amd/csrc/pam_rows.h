@@ -113,6 +113,21 @@ __device__ __forceinline__ T rounded(float x)
     return (T)x;
 }
 
+// Division of numbers below 2^31 by one that the host knows, 1 <= d < 2^31, as a product (the
+// round-up method of Granlund and Montgomery 1994): with s = ceil(log2 d) and
+// m = floor(2^32 (2^s - d) / d) + 1, n / d = (n + floor(n m / 2^32)) / 2^s.
+struct Divisor {
+    uint32_t m, s;
+    __host__ static Divisor of(int64_t d)
+    {
+        uint32_t s = 0;
+        while (((int64_t)1 << s) < d)
+            ++s;
+        return {(uint32_t)(((((uint64_t)1 << s) - (uint64_t)d) << 32) / (uint64_t)d + 1), s};
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (__umulhi(n, m) + n) >> s; }
+};
+
 // a / b of numbers that are not negative, in 32 bits where they fit
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)
 {

@@ -83,6 +83,35 @@ __device__ __forceinline__ void unpack(const Stored8<S> &r, float (&x)[8])
     }
 }
 
+// Four stored numbers of 8 bits, which lie in a word, as T: exact.
+template <class T, class S>
+__device__ __forceinline__ void widen(uint32_t w, uint32_t (&to)[sizeof(T)])
+{
+    if constexpr (std::is_same<S, e4m3>::value && std::is_same<T, bf16>::value) {
+        to[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+        to[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+    } else if constexpr (std::is_same<S, e4m3>::value && std::is_same<T, f16>::value) {
+        to[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+        to[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
+    } else {
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        float x[4];
+        if constexpr (std::is_same<S, e4m3>::value) {
+            const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+            x[0] = a[0];
+            x[1] = a[1];
+            x[2] = b[0];
+            x[3] = b[1];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                x[j] = (float)(int8)(w >> (8 * j));
+        }
+        const T4 y = {(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
+        __builtin_memcpy(to, &y, sizeof(y));
+    }
+}
+
 // Numbers as stored: to nearest, ties to even.  Those of 8 bits are in
 // [-kTop, kTop].
 template <class S>
@@ -119,9 +148,10 @@ __device__ __forceinline__ int cached(const Pool &c, int b)
 
 // Number of the row of head h of the token at position p (in [0, width page)) of
 // sequence b, counted in tokens of a head; negative: there is no such page.
-__device__ __forceinline__ int cache_row(const Pool &c, int b, int h, int p)
+// by_page: of the page's size.
+__device__ __forceinline__ int cache_row(const Pool &c, const Divisor &by_page, int b, int h, int p)
 {
-    const int w = (int)((uint32_t)p / (uint32_t)c.page), at = c.table[(int64_t)b * c.width + w];
+    const int w = (int)by_page((uint32_t)p), at = c.table[(int64_t)b * c.width + w];
     return at >= 0 && at < c.pages ? (at * c.kv_heads + h) * c.page + (p - w * c.page) : -1;
 }
 
