@@ -21,19 +21,30 @@ int64_t at_once(const pam_attn_desc_t &d)
 
 // rows: of all sequences, on the axis that is dealt out; walked: tiles of the other
 // axis that a unit of an average sequence walks over; least: tiles of a part.
-PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_t walked, int64_t least)
+// Units beyond whole rounds of the blocks that the card holds are cut, to fill one more
+// round; of causal units, which are of unequal lengths, all or none, longest first, and
+// `rounds` rounds of them.
+PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_t walked, int64_t least, int64_t rounds)
 {
     PackedPlan p{};
+    if (rows == 0)
+        return p;
+    const bool causal = d.flags & PAM_ATTN_CAUSAL;
     p.slots = (uint32_t)(rows / kPackedRows + d.sequences);
     p.heads = (uint32_t)heads;
+    p.full = p.units();
     p.parts = 1;
     // units of sequences of the average length
     const int64_t units = ceil_div(std::max<int64_t>(rows / d.sequences, 1), kPackedRows) * d.sequences * heads;
-    const int64_t room = at_once(d);
-    if (units < room)
-        p.parts = (uint32_t)std::max<int64_t>(1, std::min(walked / least, room / units));
-    if ((d.flags & PAM_ATTN_CAUSAL) && p.parts == 1 && room == 2 * kCUs && p.units() >= 2 * kCUs)
+    const int64_t room = at_once(d), full = causal ? 0 : units / room * room, rest = units - full;
+    const int64_t fill = causal ? (units < room ? rounds * room / units : 1) : (rest ? room / rest : 1);
+    const int64_t parts = std::min(walked / least, fill);
+    if (parts > 1) {
+        p.full = (uint32_t)full;
+        p.parts = (uint32_t)parts;
+    } else if (causal && room == 2 * kCUs && units >= 2 * kCUs) {
         p.fold = (uint32_t)kCUs;
+    }
     return p;
 }
 
@@ -46,11 +57,11 @@ Plans plans_of(const pam_attn_desc_t &d, bool backward)
 {
     Plans p{};
     const int64_t cls = packed_class(d.dim, d.dim_v);
-    p.rows = plan_of(d, d.tokens, d.heads, ceil_div(d.keys / d.sequences, 64), 4);
-    p.row_part = p.rows.parts > 1 ? (int64_t)p.rows.items() * kPackedRows * (cls + (backward ? 0 : 2)) : 0;
+    p.rows = plan_of(d, d.tokens, d.heads, ceil_div(d.keys / d.sequences, 64), 4, 1);
+    p.row_part = (int64_t)p.rows.cut() * p.rows.parts * kPackedRows * (cls + (backward ? 0 : 2));
     if (backward) {
-        p.keys = plan_of(d, d.keys, d.kv_heads, ceil_div(d.tokens / d.sequences, 32) * (d.heads / d.kv_heads), 8);
-        p.key_part = p.keys.parts > 1 ? (int64_t)p.keys.items() * kPackedRows * 2 * cls : 0;
+        p.keys = plan_of(d, d.keys, d.kv_heads, ceil_div(d.tokens / d.sequences, 32) * (d.heads / d.kv_heads), 8, 2);
+        p.key_part = (int64_t)p.keys.cut() * p.keys.parts * kPackedRows * 2 * cls;
         p.stats = 2 * (int64_t)d.heads * d.tokens;
     }
     return p;

@@ -7,14 +7,16 @@ namespace pam {
 
 constexpr int kPackedRows = 128;  // rows (queries, or keys) of a block
 
-// How a launch's work is dealt out: `slots` places for tiles of 128 rows, as many as
-// the sequences' tiles at the most (which sequence's tile a place has is known on the
-// device alone), times heads, times parts along the walked axis.
+// How a launch's work is dealt out.  A unit is a place for a tile of 128 rows, of one head:
+// there are as many places as the sequences' tiles at the most (which sequence's tile a place
+// has is known on the device alone).  The first `full` units are an item each, the others
+// `parts` items along the walked axis, whose sums a second kernel joins.
 struct PackedPlan {
-    uint32_t slots, heads, parts;
-    uint32_t fold;  // units [fold, 2 fold) are taken in reverse; 0: none
+    uint32_t slots, heads, full, parts;
+    uint32_t fold;  // items [fold, 2 fold) are taken in reverse; 0: none
     __host__ __device__ uint32_t units() const { return slots * heads; }
-    __host__ __device__ uint32_t items() const { return slots * heads * parts; }
+    __host__ __device__ uint32_t cut() const { return slots * heads - full; }
+    __host__ __device__ uint32_t items() const { return full + cut() * parts; }
 };
 
 struct PackedArgs {

@@ -124,20 +124,22 @@ struct Place {
 // their die's L2.  Where two blocks share a CU, the second ones of the first round are
 // taken in reverse: the longest unit is paired with the shortest of the round.
 struct PackedItem {
+    uint32_t unit, slot;  // slot: of the parts' sums, the number of the part
+    int part, parts, h;
     Place place;
-    int h, part, parts;
-    uint32_t slot;  // of the parts' sums: the item
     __device__ __forceinline__ static uint32_t order(const PackedPlan &p, uint32_t n)
     {
         return n >= p.fold && n < 2 * p.fold ? 3 * p.fold - 1 - n : n;
     }
     __device__ __forceinline__ PackedItem(const PackedPlan &p, const int32_t *start, int sequences, int total, uint32_t n)
-        : place(start, sequences, total, uniform(order(p, n) / p.parts / p.heads))
+        : PackedItem(p, start, sequences, total, order(p, n), uniform((order(p, n) - p.full) / p.parts))
     {
-        const uint32_t m = order(p, n), unit = uniform(m / p.parts);
-        slot = m;
-        parts = p.parts;
-        part = m - unit * p.parts;
+    }
+    __device__ __forceinline__ PackedItem(const PackedPlan &p, const int32_t *start, int sequences, int total, uint32_t m,
+                                          uint32_t cut)
+        : unit(m < p.full ? m : p.full + cut), slot(m - p.full), part(m < p.full ? 0 : m - p.full - cut * p.parts),
+          parts(m < p.full ? 1 : p.parts), h(0), place(start, sequences, total, uniform(unit / p.heads))
+    {
         h = uniform(unit - unit / p.heads * p.heads);
     }
     // the walked tiles of this item, of `trips` of its unit
@@ -310,7 +312,8 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
                     *reinterpret_cast<float4v *>(a.part + at * C + 32 * v + 8 * g + 4 * (l >> 5)) =
                         sum != 0.0f ? float4v{o[v][4 * g], o[v][4 * g + 1], o[v][4 * g + 2], o[v][4 * g + 3]} : float4v{};
             if (l < 32)
-                *reinterpret_cast<float2 *>(a.part + (int64_t)items * kPackedRows * C + at * 2) = make_float2(top, sum);
+                *reinterpret_cast<float2 *>(a.part + (int64_t)a.plan.cut() * a.plan.parts * kPackedRows * C + at * 2) =
+                    make_float2(top, sum);
             continue;
         }
         if (!in)
@@ -341,21 +344,21 @@ template <class T, int C, bool WIDE>
 __global__ __launch_bounds__(kAttnThreads) void k_packed_join(PackedArgs a)
 {
     constexpr int QUADS = C / 4, ROWS = kAttnThreads / QUADS, STEPS = kPackedRows / ROWS;
-    const float *stats = a.part + (int64_t)a.plan.items() * kPackedRows * C;
-    const uint32_t blocks = a.plan.units() * STEPS;
+    const float *stats = a.part + (int64_t)a.plan.cut() * a.plan.parts * kPackedRows * C;
+    const uint32_t blocks = a.plan.cut() * STEPS;
     for (uint32_t n = blockIdx.x; n < blocks; n += gridDim.x) {
-        const uint32_t unit = n / STEPS, slot = unit / a.plan.heads;
+        const uint32_t u = n / STEPS, unit = a.plan.full + u, slot = unit / a.plan.heads;
         const int h = unit - slot * a.plan.heads;
         const Place place(a.q_start, a.sequences, a.tokens, uniform(slot));
         if (place.b < 0)
             continue;
         int qb, nq;
         rows_of(a.q_start, a.tokens, place.b, qb, nq);
-        const int row = (n - unit * STEPS) * ROWS + threadIdx.x / QUADS, ch = threadIdx.x % QUADS * 4;
+        const int row = (n - u * STEPS) * ROWS + threadIdx.x / QUADS, ch = threadIdx.x % QUADS * 4;
         const int i = place.rank * kPackedRows + row;
         if (i >= nq || ch >= a.dim_v)
             continue;
-        auto at = [&](uint32_t p) { return ((int64_t)unit * a.plan.parts + p) * kPackedRows + row; };
+        auto at = [&](uint32_t p) { return ((int64_t)u * a.plan.parts + p) * kPackedRows + row; };
         float top = -INFINITY, sum = 0.0f;
         float4v o = {};
         for (uint32_t p = 0; p < a.plan.parts; ++p) {
@@ -727,12 +730,12 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_finish(PackedArgs a)
 {
     // blocks of a unit: of queries, C channels a row; of keys, 2 C
     constexpr int SQ = kPackedRows * (C / 4) / kAttnThreads, SK = 2 * SQ;
-    const uint32_t nq = a.plan.parts > 1 ? a.plan.units() * SQ : 0, nk = a.key_plan.parts > 1 ? a.key_plan.units() * SK : 0;
+    const uint32_t nq = a.plan.cut() * SQ, nk = a.key_plan.cut() * SK;
     for (uint32_t n = blockIdx.x; n < nq + nk; n += gridDim.x) {
         const bool key = n >= nq;
         const PackedPlan &p = key ? a.key_plan : a.plan;
         const uint32_t m = key ? n - nq : n, steps = key ? SK : SQ, width = key ? 2 * C : C;
-        const uint32_t unit = m / steps, slot = unit / p.heads;
+        const uint32_t u = m / steps, unit = p.full + u, slot = unit / p.heads;
         const int h = unit - slot * p.heads;
         const int32_t *start = key ? a.k_start : a.q_start;
         const int total = key ? a.keys : a.tokens;
@@ -741,13 +744,13 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_finish(PackedArgs a)
             continue;
         int base, len;
         rows_of(start, total, place.b, base, len);
-        const uint32_t e = (m - unit * steps) * kAttnThreads + threadIdx.x, row = e / (width / 4), ch = e % (width / 4) * 4;
+        const uint32_t e = (m - u * steps) * kAttnThreads + threadIdx.x, row = e / (width / 4), ch = e % (width / 4) * 4;
         const int i = (key ? place.tiles - 1 - place.rank : place.rank) * kPackedRows + row;
         const bool value = ch >= C;
         const int cc = value ? ch - C : ch, dim = value ? a.dim_v : a.dim;
         if (i >= len || cc >= dim)
             continue;
-        const float *from = (key ? a.key_part : a.part) + ((int64_t)unit * p.parts * kPackedRows + row) * width + ch;
+        const float *from = (key ? a.key_part : a.part) + ((int64_t)u * p.parts * kPackedRows + row) * width + ch;
         float4v s = {};
 #pragma unroll 4
         for (uint32_t q = 0; q < p.parts; ++q)
@@ -763,9 +766,9 @@ hipError_t packed_fwd_launch(const PackedArgs &a, hipStream_t s)
 {
     using S = PackedSizes<T, C>;
     hipError_t e = launch_lds<k_packed_fwd<T, C, WIDE>>(item_blocks(a.plan.items()), kAttnThreads, 2 * S::kKeyTile, a, s);
-    if (e != hipSuccess || a.plan.parts == 1)
+    if (e != hipSuccess || a.plan.cut() == 0)
         return e;
-    const int64_t blocks = (int64_t)a.plan.units() * (kPackedRows * (C / 4) / kAttnThreads);
+    const int64_t blocks = (int64_t)a.plan.cut() * (kPackedRows * (C / 4) / kAttnThreads);
     hipLaunchKernelGGL((k_packed_join<T, C, WIDE>), dim3(item_blocks(blocks)), dim3(kAttnThreads), 0, s, a);
     return hipGetLastError();
 }
@@ -775,14 +778,13 @@ hipError_t packed_bwd_launch(const PackedArgs &a, hipStream_t s)
 {
     using S = PackedSizes<T, C>;
     hipError_t e = hipSuccess;
-    if (a.tokens)
+    if (a.plan.units())
         e = launch_lds<k_packed_dq<T, C, WIDE>>(item_blocks(a.plan.items()), kAttnThreads, 2 * S::kKeyTile, a, s);
-    if (e == hipSuccess && a.keys)
+    if (e == hipSuccess && a.key_plan.units())
         e = launch_lds<k_packed_dkv<T, C, WIDE>>(item_blocks(a.key_plan.items()), kAttnThreads,
                                                 2 * S::kQueryTile + S::kValues, a, s);
     constexpr int SQ = kPackedRows * (C / 4) / kAttnThreads;
-    const int64_t blocks = (a.tokens && a.plan.parts > 1 ? (int64_t)a.plan.units() * SQ : 0) +
-                           (a.keys && a.key_plan.parts > 1 ? (int64_t)a.key_plan.units() * 2 * SQ : 0);
+    const int64_t blocks = (int64_t)a.plan.cut() * SQ + (int64_t)a.key_plan.cut() * 2 * SQ;
     if (e != hipSuccess || blocks == 0)
         return e;
     hipLaunchKernelGGL((k_packed_finish<T, C, WIDE>), dim3(item_blocks(blocks)), dim3(kAttnThreads), 0, s, a);
