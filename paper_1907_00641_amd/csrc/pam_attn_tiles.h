@@ -190,16 +190,17 @@ __device__ __forceinline__ void load_lds4(const void *base, uint32_t off, uint32
 //   parts start at multiples of 16 bytes, dim is whole pieces, no stride is
 //   negative, and a tile's offsets in bytes fit 32 bits.
 //   else: element by element through registers.
+//   Blocks whose waves work in teams of WAVES give the wave's number in its team.
 template <class T, int NC, int PARTS, int ROWS, int WAVES, bool WIDE>
 __device__ __forceinline__ void load_rows(char *lds, const T *from, int64_t row_stride, int64_t part_stride, int last,
-                                          int dim)
+                                          int dim, int wave)
 {
     using R = Rows<T, NC>;
     constexpr int per = 16 / sizeof(T), kPart = R::kPieces / PARTS;
     if constexpr (WIDE) {
         constexpr int kLoads = ROWS * R::kBytes / 1024, kStep = WAVES * 64 / R::kPieces;  // rows between a wave's loads
         static_assert(kLoads % WAVES == 0, "whole loads per wave");
-        const int w = WAVES == 1 ? 0 : wave_id();
+        const int w = WAVES == 1 ? 0 : wave;
         const uint32_t at = w * 64 + again(lane_id());
         const int row0 = at / R::kPieces;
 #pragma unroll
@@ -213,7 +214,7 @@ __device__ __forceinline__ void load_rows(char *lds, const T *from, int64_t row_
                            lds_address(lds) + R::at((n * WAVES + w) * 64 / R::kPieces));
         }
     } else {
-        for (int e = again(WAVES == 1 ? lane_id() : (int)threadIdx.x); e < ROWS * PARTS * dim; e += 64 * WAVES) {
+        for (int e = again((WAVES == 1 ? 0 : wave * 64) + lane_id()); e < ROWS * PARTS * dim; e += 64 * WAVES) {
             const int c = e % dim, part = e / dim % PARTS, row = e / dim / PARTS;
             const int ch = part * (NC / PARTS) + c;
             *reinterpret_cast<T *>(lds + R::at(row, ch / per) + (ch % per) * sizeof(T)) =
@@ -222,14 +223,26 @@ __device__ __forceinline__ void load_rows(char *lds, const T *from, int64_t row_
     }
 }
 
+template <class T, int NC, int PARTS, int ROWS, int WAVES, bool WIDE>
+__device__ __forceinline__ void load_rows(char *lds, const T *from, int64_t row_stride, int64_t part_stride, int last,
+                                          int dim)
+{
+    load_rows<T, NC, PARTS, ROWS, WAVES, WIDE>(lds, from, row_stride, part_stride, last, dim, wave_id());
+}
+
 // Clears the rows whose bit is 0 in `seen` (row r: bit r).
+template <class T, int NC, int ROWS, int WAVES>
+__device__ __forceinline__ void clear_rows(char *lds, uint64_t seen, int wave)
+{
+    using R = Rows<T, NC>;
+    for (int e = again((WAVES == 1 ? 0 : wave * 64) + lane_id()); e < ROWS * R::kPieces; e += 64 * WAVES)
+        if (!(seen >> (e / R::kPieces) & 1))
+            store16(lds + e * 16, uint4v{0, 0, 0, 0});
+}
 template <class T, int NC, int ROWS, int WAVES>
 __device__ __forceinline__ void clear_rows(char *lds, uint64_t seen)
 {
-    using R = Rows<T, NC>;
-    for (int e = again(WAVES == 1 ? lane_id() : (int)threadIdx.x); e < ROWS * R::kPieces; e += 64 * WAVES)
-        if (!(seen >> (e / R::kPieces) & 1))
-            store16(lds + e * 16, uint4v{0, 0, 0, 0});
+    clear_rows<T, NC, ROWS, WAVES>(lds, seen, wave_id());
 }
 
 // A row as an operand, straight from memory: chunk s of channels of `row` for

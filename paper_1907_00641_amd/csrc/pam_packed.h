@@ -12,7 +12,7 @@ constexpr int kPackedRows = 128;  // rows (queries, or keys) of a block
 // has is known on the device alone).  The first `full` units are an item each, the others
 // `parts` items along the walked axis, whose sums a second kernel joins.
 struct PackedPlan {
-    uint32_t slots, heads, full, parts;
+    uint32_t slots, heads, full, parts, teams;  // teams: of four waves, in a block
     uint32_t fold;  // items [fold, 2 fold) are taken in reverse; 0: none
     __host__ __device__ uint32_t units() const { return slots * heads; }
     __host__ __device__ uint32_t cut() const { return slots * heads - full; }

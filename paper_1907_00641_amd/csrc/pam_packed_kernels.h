@@ -10,6 +10,10 @@
 // rows' operands stay in registers, and so do the probabilities: scores are formed
 // transposed, which makes a lane hold one row, and their layout, rounded, is an
 // operand of the next product (pam_attn_tiles.h).
+// KS: teams of four waves in a block, which take every KS-th tile of the walk for the same
+// rows and meet in LDS.  Two where the card has room for them: a wave alone on its SIMD
+// computes its products and its softmax one after the other, two overlap, and the walk is
+// half as long.
 #pragma once
 
 #include "pam_attn_common.h"
@@ -32,7 +36,40 @@ struct PackedSizes {
     static constexpr int kKeyTile = 2 * R::size(kKeys);
     static constexpr int kQueryTile = 2 * R::size(kQueries) + 2 * kQueries * 4;  // queries, dout, two statistics
     static constexpr int kValues = R::size(kPackedRows);                         // the keys' pass: the block's values
+    // LDS of a block of KS teams of four waves: two tiles for each; at the end, the sums of all
+    // teams but the first
+    static constexpr int rows_lds(int ks) { return std::max(2 * ks * kKeyTile, (ks - 1) * kPackedRows * (C * 4 + 8)); }
+    static constexpr int keys_lds(int ks)
+    {
+        return std::max(2 * ks * kQueryTile + kValues, (ks - 1) * kPackedRows * 2 * C * 4);
+    }
 };
+
+// Sums that two teams of waves hold, a register at a time through LDS: [wave][register / 4][lane].
+template <int N>
+__device__ __forceinline__ void leave_sums(char *lds, int wave, const f32x16 (&x)[N])
+{
+#pragma unroll
+    for (int v = 0; v < N; ++v)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4v *>(lds + (((wave * N + v) * 4 + g) * 64 + lane_id()) * 16) =
+                float4v{x[v][4 * g], x[v][4 * g + 1], x[v][4 * g + 2], x[v][4 * g + 3]};
+}
+// x = x f + theirs f2
+template <int N>
+__device__ __forceinline__ void take_sums(const char *lds, int wave, f32x16 (&x)[N], float f, float f2)
+{
+#pragma unroll
+    for (int v = 0; v < N; ++v)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4v y = *reinterpret_cast<const float4v *>(lds + (((wave * N + v) * 4 + g) * 64 + lane_id()) * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                x[v][4 * g + j] = x[v][4 * g + j] * f + y[j] * f2;
+        }
+}
 
 // A sequence's rows.
 struct Sequence {
@@ -152,7 +189,7 @@ struct PackedItem {
 };
 
 // Clears the rows of no sequence: those before the first, and from the last's end on.
-template <class T>
+template <int KS, class T>
 __device__ __forceinline__ void clear_outside(T *rows, const int32_t *start, int sequences, int total, int64_t width)
 {
     if (!start)
@@ -162,7 +199,8 @@ __device__ __forceinline__ void clear_outside(T *rows, const int32_t *start, int
     rows_of(start, total, sequences - 1, last, n);
     last += n;
     const int64_t head = first * width, all = head + (int64_t)(total - last) * width;
-    for (int64_t e = (int64_t)blockIdx.x * kAttnThreads + threadIdx.x; e < all; e += (int64_t)gridDim.x * kAttnThreads)
+    for (int64_t e = (int64_t)blockIdx.x * (KS * kAttnThreads) + threadIdx.x; e < all;
+         e += (int64_t)gridDim.x * (KS * kAttnThreads))
         rows[e < head ? e : e - head + last * width] = (T)0.0f;
 }
 
@@ -183,18 +221,18 @@ __device__ __forceinline__ void hide_rows(f32x16 &s, uint32_t bits)
 // scaled): the probabilities are at most 2^8 then, and nothing is lost, since both
 // sums carry the same factor.  Probabilities are rounded to the activations' type for
 // their product; their sum is of the 32-bit values.
-template <class T, int C, bool WIDE>
-__global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) void k_packed_fwd(PackedArgs a)
+template <class T, int C, bool WIDE, int KS>
+__global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) void k_packed_fwd(PackedArgs a)
 {
     using S = PackedSizes<T, C>;
     using R = typename S::R;
     constexpr int KT = S::kKeys, N = KT / 32;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int l = lane_id(), w = wave_id();
+    const int l = lane_id(), w = wave_id() % kAttnWaves, ks = wave_id() / kAttnWaves;
     const float c = a.scale * kLog2e;
-    clear_outside((T *)a.out, a.q_start, a.sequences, a.tokens, (int64_t)a.heads * a.dim_v);
+    clear_outside<KS>((T *)a.out, a.q_start, a.sequences, a.tokens, (int64_t)a.heads * a.dim_v);
     if (a.dim < C || a.dim_v < C) {  // the channels that no load writes
-        for (int e = threadIdx.x; e < 2 * S::kKeyTile / 16; e += kAttnThreads)
+        for (int e = threadIdx.x; e < 2 * KS * S::kKeyTile / 16; e += KS * kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
@@ -219,17 +257,18 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
         const int wall = q0 + 32 * w + 31 < nq ? (a.causal ? min(nk, q0 + 32 * w + nk - nq + 1) : nk) : 0;
         int from, to;
         item.range(max(end + KT - 1, 0) / KT, from, to);
-        const T *kp = uniform_ptr((const T *)a.k + (kb0 + (int64_t)from * KT) * a.ks[0] + hk * a.ks[1]);
-        const T *vp = uniform_ptr((const T *)a.v + (kb0 + (int64_t)from * KT) * a.vs[0] + hk * a.vs[1]);
-        auto issue = [&](int t) {  // tiles in order
-            char *at = lds + (t & 1) * S::kKeyTile;
-            load_rows<T, C, 1, KT, kAttnWaves, WIDE>(at, kp, a.ks[0], 0, nk - 1 - t * KT, a.dim);
-            load_rows<T, C, 1, KT, kAttnWaves, WIDE>(at + R::size(KT), vp, a.vs[0], 0, nk - 1 - t * KT, a.dim_v);
-            kp = uniform_ptr(kp + KT * a.ks[0]);
-            vp = uniform_ptr(vp + KT * a.vs[0]);
+        const T *kp = uniform_ptr((const T *)a.k + (kb0 + (int64_t)(from + ks) * KT) * a.ks[0] + hk * a.ks[1]);
+        const T *vp = uniform_ptr((const T *)a.v + (kb0 + (int64_t)(from + ks) * KT) * a.vs[0] + hk * a.vs[1]);
+        char *mine = lds + ks * 2 * S::kKeyTile;  // this team's two tiles
+        auto issue = [&](int t, int place) {      // tiles in order
+            char *at = mine + place * S::kKeyTile;
+            load_rows<T, C, 1, KT, kAttnWaves, WIDE>(at, kp, a.ks[0], 0, nk - 1 - t * KT, a.dim, w);
+            load_rows<T, C, 1, KT, kAttnWaves, WIDE>(at + R::size(KT), vp, a.vs[0], 0, nk - 1 - t * KT, a.dim_v, w);
+            kp = uniform_ptr(kp + KS * KT * a.ks[0]);
+            vp = uniform_ptr(vp + KS * KT * a.vs[0]);
         };
-        if (from < to)
-            issue(from);
+        if (from + ks < to)
+            issue(from + ks, 0);
         uint4v q[S::CK];
         const T *qrow = (const T *)a.q + (qb + (int64_t)i) * a.qs[0] + h * a.qs[1];
 #pragma unroll
@@ -237,18 +276,19 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
             q[x] = memory_chunk<T, WIDE>(qrow, x, a.dim, in);
         f32x16 o[S::TV] = {};
         float top = -INFINITY, sum = 0.0f;
-        for (int t = from; t < to; ++t) {
-            const int k0 = t * KT;
-            char *kb = lds + (t & 1) * S::kKeyTile, *vb = kb + R::size(KT);
+        for (int t0 = from, place = 0; t0 < to; t0 += KS, place ^= 1) {  // the teams' tiles of a turn
+            const int t = t0 + ks, k0 = t * KT;
+            char *kb = mine + place * S::kKeyTile, *vb = kb + R::size(KT);
             wait_loads();
-            __syncthreads();  // tile t is there for every wave, and tile t - 1 done with
-            if (t + 1 < to)
-                issue(t + 1);
-            if (k0 + KT > nk) {  // rows past the sequence: of keys, the scores are hidden
-                clear_rows<T, C, KT, kAttnWaves>(vb, (1ull << (nk - k0)) - 1);
+            __syncthreads();  // the tiles are there for every wave, and those before done with
+            if (t + KS < to)
+                issue(t + KS, place ^ 1);
+            if (min(t0 + KS, to) * KT > nk) {  // rows past the sequence: of keys, the scores are hidden
+                if (t < to && k0 + KT > nk)
+                    clear_rows<T, C, KT, kAttnWaves>(vb, (1ull << (nk - k0)) - 1, w);
                 __syncthreads();
             }
-            if (k0 >= wend)
+            if (t >= to || k0 >= wend)
                 continue;
             const uint32_t kr = lds_address(kb) + R::row_lane(), vc = lds_address(vb) + R::col_lane();
             f32x16 s[N] = {};
@@ -303,6 +343,39 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
         }
         __syncthreads();  // the next item's loads write where this one's were read
         sum = xor32_add(sum);
+        if constexpr (KS == 2) {
+            float2 *stats = reinterpret_cast<float2 *>(lds + kPackedRows * C * 4);
+            if (ks == 1) {
+                if (__any(sum == 0.0f)) {
+#pragma unroll
+                    for (int v = 0; v < S::TV; ++v)
+                        o[v] = sum == 0.0f ? f32x16{} : o[v];
+                }
+                leave_sums(lds, w, o);
+                if (l < 32)
+                    stats[w * 32 + l] = make_float2(top, sum);
+            }
+            __syncthreads();
+            if (ks == 0) {
+                const float2 st = stats[w * 32 + (l & 31)];
+                const float up = __builtin_fmaxf(sum != 0.0f ? top : -INFINITY, st.y != 0.0f ? st.x : -INFINITY);
+                // a team whose top is -inf and whose sum is not 0 has a NaN in it; one whose sum is
+                // 0 saw nothing, and what it holds need not be finite
+                const float f = sum == 0.0f ? 0.0f : (top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - up));
+                const float f2 = st.y == 0.0f ? 0.0f : (st.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.x - up));
+                if (__any(sum == 0.0f)) {
+#pragma unroll
+                    for (int v = 0; v < S::TV; ++v)
+                        o[v] = sum == 0.0f ? f32x16{} : o[v];
+                }
+                take_sums(lds, w, o, f, f2);
+                sum = sum * f + st.y * f2;
+                top = up;
+            }
+            __syncthreads();
+            if (ks == 1)
+                continue;
+        }
         if (item.parts > 1) {  // unnormalised sums, tops and sums, for k_packed_join
             const int64_t at = ((int64_t)item.slot * kAttnWaves + w) * 32 + (l & 31);
 #pragma unroll
@@ -392,18 +465,18 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_join(PackedArgs a)
 // D and dq.  D is taken from out in 32 bits: it is the difference of dp and D that
 // counts, which may be far smaller than either.  Score gradients are rounded to the
 // activations' type for their product.
-template <class T, int C, bool WIDE>
-__global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) void k_packed_dq(PackedArgs a)
+template <class T, int C, bool WIDE, int KS>
+__global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) void k_packed_dq(PackedArgs a)
 {
     using S = PackedSizes<T, C>;
     using R = typename S::R;
     constexpr int KT = S::kKeys;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int l = lane_id(), w = wave_id();
+    const int l = lane_id(), w = wave_id() % kAttnWaves, ks = wave_id() / kAttnWaves;
     const float c = a.scale * kLog2e;
-    clear_outside((T *)a.gq, a.q_start, a.sequences, a.tokens, (int64_t)a.heads * a.dim);
+    clear_outside<KS>((T *)a.gq, a.q_start, a.sequences, a.tokens, (int64_t)a.heads * a.dim);
     if (a.dim < C || a.dim_v < C) {
-        for (int e = threadIdx.x; e < 2 * S::kKeyTile / 16; e += kAttnThreads)
+        for (int e = threadIdx.x; e < 2 * KS * S::kKeyTile / 16; e += KS * kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
@@ -426,17 +499,18 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
         const int wall = q0 + 32 * w + 31 < nq ? (a.causal ? min(nk, q0 + 32 * w + nk - nq + 1) : nk) : 0;
         int from, to;
         item.range(max(end + KT - 1, 0) / KT, from, to);
-        const T *kp = uniform_ptr((const T *)a.k + (kb0 + (int64_t)from * KT) * a.ks[0] + hk * a.ks[1]);
-        const T *vp = uniform_ptr((const T *)a.v + (kb0 + (int64_t)from * KT) * a.vs[0] + hk * a.vs[1]);
-        auto issue = [&](int t) {
-            char *at = lds + (t & 1) * S::kKeyTile;
-            load_rows<T, C, 1, KT, kAttnWaves, WIDE>(at, kp, a.ks[0], 0, nk - 1 - t * KT, a.dim);
-            load_rows<T, C, 1, KT, kAttnWaves, WIDE>(at + R::size(KT), vp, a.vs[0], 0, nk - 1 - t * KT, a.dim_v);
-            kp = uniform_ptr(kp + KT * a.ks[0]);
-            vp = uniform_ptr(vp + KT * a.vs[0]);
+        const T *kp = uniform_ptr((const T *)a.k + (kb0 + (int64_t)(from + ks) * KT) * a.ks[0] + hk * a.ks[1]);
+        const T *vp = uniform_ptr((const T *)a.v + (kb0 + (int64_t)(from + ks) * KT) * a.vs[0] + hk * a.vs[1]);
+        char *mine = lds + ks * 2 * S::kKeyTile;
+        auto issue = [&](int t, int place) {
+            char *at = mine + place * S::kKeyTile;
+            load_rows<T, C, 1, KT, kAttnWaves, WIDE>(at, kp, a.ks[0], 0, nk - 1 - t * KT, a.dim, w);
+            load_rows<T, C, 1, KT, kAttnWaves, WIDE>(at + R::size(KT), vp, a.vs[0], 0, nk - 1 - t * KT, a.dim_v, w);
+            kp = uniform_ptr(kp + KS * KT * a.ks[0]);
+            vp = uniform_ptr(vp + KS * KT * a.vs[0]);
         };
-        if (from < to)
-            issue(from);
+        if (from + ks < to)
+            issue(from + ks, 0);
         const int64_t row = (int64_t)(qb + i) * a.heads + h;
         uint4v q[S::CK], g[S::CK];
         const T *qrow = (const T *)a.q + (qb + (int64_t)i) * a.qs[0] + h * a.qs[1];
@@ -456,26 +530,30 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
             lse = x == -INFINITY ? INFINITY : x * kLog2e;
         }
         D = lse == INFINITY ? 0.0f : D;
-        if (l < 32 && in && item.part == 0) {
+        if (l < 32 && in && item.part == 0 && ks == 0) {
             float *st = a.stats + (int64_t)h * 2 * a.tokens + qb + i;
             st[0] = lse;
             st[a.tokens] = D;
         }
         f32x16 acc[S::TV] = {};
         Range range;
-        for (int t = from; t < to; ++t) {
-            const int k0 = t * KT;
-            char *kb = lds + (t & 1) * S::kKeyTile, *vb = kb + R::size(KT);
+        for (int t0 = from, place = 0; t0 < to; t0 += KS, place ^= 1) {
+            const int t = t0 + ks, k0 = t * KT;
+            char *kb = mine + place * S::kKeyTile, *vb = kb + R::size(KT);
             wait_loads();
             __syncthreads();
-            if (t + 1 < to)
-                issue(t + 1);
-            if (k0 + KT > nk) {
-                const uint64_t seen = (1ull << (nk - k0)) - 1;
-                clear_rows<T, C, KT, kAttnWaves>(kb, seen);
-                clear_rows<T, C, KT, kAttnWaves>(vb, seen);
+            if (t + KS < to)
+                issue(t + KS, place ^ 1);
+            if (min(t0 + KS, to) * KT > nk) {
+                if (t < to && k0 + KT > nk) {
+                    const uint64_t seen = (1ull << (nk - k0)) - 1;
+                    clear_rows<T, C, KT, kAttnWaves>(kb, seen, w);
+                    clear_rows<T, C, KT, kAttnWaves>(vb, seen, w);
+                }
                 __syncthreads();
             }
+            if (t >= to)
+                continue;
             const uint32_t kr = lds_address(kb) + R::row_lane(), kc = lds_address(kb) + R::col_lane();
             const uint32_t vr = lds_address(vb) + R::row_lane();
 #pragma unroll
@@ -510,8 +588,23 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
             }
         }
         __syncthreads();
+        float f = a.scale * range.down();
+        if constexpr (KS == 2) {
+            if (ks == 1) {
+#pragma unroll
+                for (int v = 0; v < S::TV; ++v)
+                    acc[v] *= f;
+                leave_sums(lds, w, acc);
+            }
+            __syncthreads();
+            if (ks == 0)
+                take_sums(lds, w, acc, f, 1.0f);
+            f = 1.0f;
+            __syncthreads();
+            if (ks == 1)
+                continue;
+        }
         float *part = a.part + (((int64_t)item.slot * kAttnWaves + w) * 32 + (l & 31)) * C;
-        const float f = a.scale * range.down();
 #pragma unroll
         for (int v = 0; v < S::TV; ++v)
 #pragma unroll
@@ -538,19 +631,19 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
 // apart from dq's: one pass would save two of the seven products, but either dq or
 // dk and dv would have to be summed over blocks, by atomics in an order that changes
 // from run to run, or by parts of 32 bits as large as the scores' rows over 128.
-template <class T, int C, bool WIDE>
-__global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) void k_packed_dkv(PackedArgs a)
+template <class T, int C, bool WIDE, int KS>
+__global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) void k_packed_dkv(PackedArgs a)
 {
     using S = PackedSizes<T, C>;
     using R = typename S::R;
     constexpr int QT = S::kQueries;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int l = lane_id(), w = wave_id();
+    const int l = lane_id(), w = wave_id() % kAttnWaves, ks = wave_id() / kAttnWaves;
     const float c = a.scale * kLog2e;
-    clear_outside((T *)a.gk, a.k_start, a.sequences, a.keys, (int64_t)a.kv_heads * a.dim);
-    clear_outside((T *)a.gv, a.k_start, a.sequences, a.keys, (int64_t)a.kv_heads * a.dim_v);
+    clear_outside<KS>((T *)a.gk, a.k_start, a.sequences, a.keys, (int64_t)a.kv_heads * a.dim);
+    clear_outside<KS>((T *)a.gv, a.k_start, a.sequences, a.keys, (int64_t)a.kv_heads * a.dim_v);
     if (a.dim < C || a.dim_v < C) {
-        for (int e = threadIdx.x; e < (2 * S::kQueryTile + S::kValues) / 16; e += kAttnThreads)
+        for (int e = threadIdx.x; e < (2 * KS * S::kQueryTile + S::kValues) / 16; e += KS * kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
     }
@@ -576,7 +669,7 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
         uint4v kf[S::CK];
         const T *krow = (const T *)a.k + (kb0 + (int64_t)j) * a.ks[0] + hk * a.ks[1];
         // the wave's 32 rows of values stay in LDS: in registers too they did not fit 256
-        char *vrows = lds + 2 * S::kQueryTile + R::size(32) * w;
+        char *vrows = lds + 2 * KS * S::kQueryTile + R::size(32) * w;  // (the teams write the same)
         const T *vrow = (const T *)a.v + (kb0 + (int64_t)j) * a.vs[0] + hk * a.vs[1];
 #pragma unroll
         for (int x = 0; x < S::CK; ++x) {
@@ -596,7 +689,7 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
         int t0, t1;
         item.range(per * a.group, t0, t1);
         // head and first query of the next tile to load
-        int nh = h0 + (per ? t0 / per : 0), ni = first + (per ? t0 % per : 0) * QT;
+        int nh = h0 + (per ? (t0 + ks) / per : 0), ni = first + (per ? (t0 + ks) % per : 0) * QT;
         nh = uniform(nh);
         ni = uniform(ni);
         const T *qp, *gp;
@@ -606,48 +699,72 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
             gp = uniform_ptr((const T *)a.dout + (qb + (int64_t)ni) * a.dos[0] + h * a.dos[1]);
             sp = uniform_ptr(a.stats + (int64_t)h * 2 * a.tokens + qb + ni);
         };
+        // the first query of the tile KS tiles on, and its head: a step may pass several heads
+        auto step = [&](int &i, int &h) {
+            i += KS * QT;
+            while (i >= nq && h < h1) {  // nq > first: every head has a tile
+                i -= per * QT;
+                ++h;
+            }
+        };
+        char *mine = lds + ks * 2 * S::kQueryTile;
         auto issue = [&](int buf) {
-            char *to = lds + buf * S::kQueryTile;
-            load_rows<T, C, 1, QT, kAttnWaves, WIDE>(to, qp, a.qs[0], 0, nq - 1 - ni, a.dim);
-            load_rows<T, C, 1, QT, kAttnWaves, WIDE>(to + R::size(QT), gp, a.dos[0], 0, nq - 1 - ni, a.dim_v);
+            char *to = mine + buf * S::kQueryTile;
+            load_rows<T, C, 1, QT, kAttnWaves, WIDE>(to, qp, a.qs[0], 0, nq - 1 - ni, a.dim, w);
+            load_rows<T, C, 1, QT, kAttnWaves, WIDE>(to + R::size(QT), gp, a.dos[0], 0, nq - 1 - ni, a.dim_v, w);
             // 2 statistics of 32 queries, one by half of each of two waves
             const int y = again(l);
             if (w < 2 && y < 32)
                 load_lds4(uniform_ptr(sp + w * (int64_t)a.tokens), 4u * (uint32_t)min(y, nq - 1 - ni),
                           lds_address(to + 2 * R::size(QT)) + w * 128);
-            ni += QT;
-            qp = uniform_ptr(qp + QT * a.qs[0]);
-            gp = uniform_ptr(gp + QT * a.dos[0]);
-            sp += QT;
-            if (ni >= nq && ++nh < h1) {
-                ni = first;
-                head(nh);
+            const int was = nh;
+            step(ni, nh);
+            if (nh != was) {
+                if (nh < h1)
+                    head(nh);
+            } else {
+                qp = uniform_ptr(qp + KS * QT * a.qs[0]);
+                gp = uniform_ptr(gp + KS * QT * a.dos[0]);
+                sp += KS * QT;
             }
         };
-        int i0 = ni - QT;  // of the tile at hand
-        if (t0 < t1) {
-            head(nh);
-            issue(t0 & 1);
+        int i0s[KS], ihs[KS];  // of every team's tile at hand
+#pragma unroll
+        for (int x = 0; x < KS; ++x) {
+            ihs[x] = uniform(h0 + (per ? (t0 + x) / per : 0));
+            i0s[x] = uniform(first + (per ? (t0 + x) % per : 0) * QT);
         }
-        for (int t = t0; t < t1; ++t) {
-            const int buf = t & 1;
-            char *qb_ = lds + buf * S::kQueryTile, *gb = qb_ + R::size(QT);
+        if (t0 + ks < t1) {
+            head(nh);
+            issue(0);
+        }
+        for (int tt = t0, buf = 0; tt < t1; tt += KS, buf ^= 1) {
+            const int t = tt + ks;
+            char *qb_ = mine + buf * S::kQueryTile, *gb = qb_ + R::size(QT);
             const float *st = reinterpret_cast<const float *>(gb + R::size(QT));
-            i0 += QT;
-            if (i0 >= nq)
-                i0 = first;
             wait_loads();
             __syncthreads();
-            if (t + 1 < t1)
+            if (t + KS < t1)
                 issue(buf ^ 1);
+            // rows past the sequence, or before the first that sees a key of the block
+            bool clear = false;
+#pragma unroll
+            for (int x = 0; x < KS; ++x)
+                clear = clear || (tt + x < t1 && (i0s[x] + QT > nq || i0s[x] < lowest));
+            const int i0 = KS == 2 && ks ? i0s[KS - 1] : i0s[0];
             const bool tail = i0 + QT > nq;
-            if (tail || i0 < lowest) {  // rows past the sequence, or before the first that sees a key of the block
-                const uint32_t live = low_bits(nq - i0) & ~low_bits(lowest - i0);
-                clear_rows<T, C, QT, kAttnWaves>(qb_, live);
-                clear_rows<T, C, QT, kAttnWaves>(gb, live);
+            if (clear) {  // the same in the whole block
+                if (t < t1 && (tail || i0 < lowest)) {
+                    const uint32_t live = low_bits(nq - i0) & ~low_bits(lowest - i0);
+                    clear_rows<T, C, QT, kAttnWaves>(qb_, live, w);
+                    clear_rows<T, C, QT, kAttnWaves>(gb, live, w);
+                }
                 __syncthreads();
             }
-            if (!wany || i0 + QT <= wfirst)
+#pragma unroll
+            for (int x = 0; x < KS; ++x)
+                step(i0s[x], ihs[x]);
+            if (t >= t1 || !wany || i0 + QT <= wfirst)
                 continue;
             const uint32_t qr = lds_address(qb_) + R::row_lane(), qc = lds_address(qb_) + R::col_lane();
             const uint32_t gr = lds_address(gb) + R::row_lane(), gc = lds_address(gb) + R::col_lane();
@@ -697,6 +814,27 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
                 }
         }
         __syncthreads();
+        const float fv = __builtin_amdgcn_exp2f(-lift);
+        float fk = a.scale * range.down() * fv;
+        if constexpr (KS == 2) {
+            char *lds_v = lds + kPackedRows * C * 4;
+            if (ks == 1) {
+#pragma unroll
+                for (int v = 0; v < S::TV; ++v)
+                    gk[v] *= fk;
+                leave_sums(lds, w, gk);
+                leave_sums(lds_v, w, gv);
+            }
+            __syncthreads();
+            if (ks == 0) {
+                take_sums(lds, w, gk, fk, 1.0f);
+                take_sums(lds_v, w, gv, 1.0f, 1.0f);
+            }
+            fk = 1.0f;
+            __syncthreads();
+            if (ks == 1)
+                continue;
+        }
         if (!seen && item.parts == 1)
             continue;
         const int64_t row = (int64_t)(kb0 + j) * a.kv_heads + hk;
@@ -715,7 +853,6 @@ __global__ __launch_bounds__(kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) v
                     store4<T, WIDE>(to, at, dim, y);
             }
         };
-        const float fv = __builtin_amdgcn_exp2f(-lift), fk = a.scale * range.down() * fv;
 #pragma unroll
         for (int v = 0; v < S::TV; ++v) {
             put((T *)a.gk + row * a.dim, part, gk[v], v, a.dim, fk);
@@ -761,11 +898,35 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_finish(PackedArgs a)
     }
 }
 
+template <class T, int C, bool WIDE, int KS>
+hipError_t packed_fwd_teams(const PackedArgs &a, hipStream_t s)
+{
+    return launch_lds<k_packed_fwd<T, C, WIDE, KS>>(item_blocks(a.plan.items()), KS * kAttnThreads,
+                                                   PackedSizes<T, C>::rows_lds(KS), a, s);
+}
+template <class T, int C, bool WIDE, int KS>
+hipError_t packed_dq_teams(const PackedArgs &a, hipStream_t s)
+{
+    return launch_lds<k_packed_dq<T, C, WIDE, KS>>(item_blocks(a.plan.items()), KS * kAttnThreads,
+                                                  PackedSizes<T, C>::rows_lds(KS), a, s);
+}
+template <class T, int C, bool WIDE, int KS>
+hipError_t packed_dkv_teams(const PackedArgs &a, hipStream_t s)
+{
+    return launch_lds<k_packed_dkv<T, C, WIDE, KS>>(item_blocks(a.key_plan.items()), KS * kAttnThreads,
+                                                   PackedSizes<T, C>::keys_lds(KS), a, s);
+}
+
+// two teams where the plan says so, and the registers are for two waves per SIMD
 template <class T, int C, bool WIDE>
 hipError_t packed_fwd_launch(const PackedArgs &a, hipStream_t s)
 {
-    using S = PackedSizes<T, C>;
-    hipError_t e = launch_lds<k_packed_fwd<T, C, WIDE>>(item_blocks(a.plan.items()), kAttnThreads, 2 * S::kKeyTile, a, s);
+    hipError_t e = hipErrorInvalidValue;
+    if constexpr (PackedSizes<T, C>::kSmall) {
+        e = a.plan.teams == 2 ? packed_fwd_teams<T, C, WIDE, 2>(a, s) : packed_fwd_teams<T, C, WIDE, 1>(a, s);
+    } else {
+        e = packed_fwd_teams<T, C, WIDE, 1>(a, s);
+    }
     if (e != hipSuccess || a.plan.cut() == 0)
         return e;
     const int64_t blocks = (int64_t)a.plan.cut() * (kPackedRows * (C / 4) / kAttnThreads);
@@ -776,13 +937,18 @@ hipError_t packed_fwd_launch(const PackedArgs &a, hipStream_t s)
 template <class T, int C, bool WIDE>
 hipError_t packed_bwd_launch(const PackedArgs &a, hipStream_t s)
 {
-    using S = PackedSizes<T, C>;
     hipError_t e = hipSuccess;
-    if (a.plan.units())
-        e = launch_lds<k_packed_dq<T, C, WIDE>>(item_blocks(a.plan.items()), kAttnThreads, 2 * S::kKeyTile, a, s);
-    if (e == hipSuccess && a.key_plan.units())
-        e = launch_lds<k_packed_dkv<T, C, WIDE>>(item_blocks(a.key_plan.items()), kAttnThreads,
-                                                2 * S::kQueryTile + S::kValues, a, s);
+    if constexpr (PackedSizes<T, C>::kSmall) {
+        if (a.plan.units())
+            e = a.plan.teams == 2 ? packed_dq_teams<T, C, WIDE, 2>(a, s) : packed_dq_teams<T, C, WIDE, 1>(a, s);
+        if (e == hipSuccess && a.key_plan.units())
+            e = a.key_plan.teams == 2 ? packed_dkv_teams<T, C, WIDE, 2>(a, s) : packed_dkv_teams<T, C, WIDE, 1>(a, s);
+    } else {
+        if (a.plan.units())
+            e = packed_dq_teams<T, C, WIDE, 1>(a, s);
+        if (e == hipSuccess && a.key_plan.units())
+            e = packed_dkv_teams<T, C, WIDE, 1>(a, s);
+    }
     constexpr int SQ = kPackedRows * (C / 4) / kAttnThreads;
     const int64_t blocks = (int64_t)a.plan.cut() * SQ + (int64_t)a.key_plan.cut() * 2 * SQ;
     if (e != hipSuccess || blocks == 0)

@@ -149,8 +149,22 @@ def test_attention_in_parts(shape, t, causal):
 
 
 @pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape,causal", [(([700, 650], 0, 44, 44, 16, 16), False), (([700, 650], 0, 44, 44, 16, 16), True),
+                                          (([130] * 20, 0, 14, 7, 72, 72), False), (([130] * 20, 0, 14, 7, 72, 72), True),
+                                          (([300] * 9, 7, 16, 4, 32, 32), True), (([300] * 9, 7, 16, 4, 32, 32), False),
+                                          (([3100], 0, 8, 8, 16, 16), True), (([1500, 1300], 0, 8, 8, 72, 72), True),
+                                          (([900, 40, 900], 0, 16, 8, 64, 64), False)], ids=str)
+def test_attention_many_units(shape, causal, t):
+    """About as many units as the card holds blocks, and more: whole rounds and a cut rest, one team of waves or two,
+    the second blocks of the CUs in reverse, long causal walks in parts."""
+    log(f"[packed units] {shape} {t} causal={causal}")
+    c = Packed(22, *shape, t, causal)
+    c.compare(*c.run())
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("d", [40, 64, 100])
-@pytest.mark.parametrize("lens", [[70, 0, 129], [500]], ids=str)
+@pytest.mark.parametrize("lens", [[70, 0, 129], [500], [140] * 40], ids=str)
 def test_attention_rows_of_no_sequence(lens, d, t):
     """Before the first sequence and behind the last one: no part of anything, whatever they hold; their results 0."""
     import torch
@@ -264,12 +278,13 @@ def test_attention_common_part_of_values():
 
 
 @pytest.mark.parametrize("t", ["f16", "bf16"])
-def test_attention_small_and_large_gradients(t):
+@pytest.mark.parametrize("lens", [[130], [130] * 70], ids=["few units", "many units"])
+def test_attention_small_and_large_gradients(t, lens):
     """Upstream gradients of 1e-6 and, in bf16, 1e20."""
     import torch
 
     for size in (1e-6, 1e3) + ((1e20,) if t == "bf16" else ()):
-        c = Packed(17, [130], 20, 2, 1, 64, 64, t)
+        c = Packed(17, lens, 20, 2, 1, 64, 64, t)
         want, saved = c.run()
         g = (c.g.float() * size).to(c.g.dtype)
         c.g, c.gh = g, host(g)
@@ -319,7 +334,7 @@ def test_attention_repeats_and_streams():
         assert same(c.run(), want)
 
 
-@pytest.mark.parametrize("lens", [[700, 50], [64, 64, 64]], ids=str)
+@pytest.mark.parametrize("lens", [[700, 50], [64, 64, 64], [400] * 60], ids=str)
 def test_attention_in_a_graph(lens):
     """Forward and backward captured, replayed with eager calls between, and with other lengths in the same starts."""
     import torch
@@ -852,6 +867,20 @@ def test_paged_attention_in_parts(store, t, maps):
     c.compare(want)
     for bound in (1, 600, 100000):
         c.compare(c.run(key_bound=bound))
+
+
+@pytest.mark.parametrize("lens", [[4000, 1, 0, 17, 900, 2300], [1] * 5 + [6000], [1500] * 6, [300 + 61 * b for b in range(64)],
+                                  [700 - 7 * b for b in range(70)], [0, 0, 0]], ids=["mixed", "one long", "equal", "64", "70", "none"])
+@pytest.mark.parametrize("maps", [1, 2])
+def test_paged_attention_shares(lens, maps):
+    """The blocks are shared out by the sequences' lengths, which the host does not know; the bits do not depend on how
+    much longer the table is, but for the split."""
+    total = max(max(lens), 1) + 900
+    c = Paged(59, len(lens), 1, total, 16, 4, 2, 32, 32, "bf16", "int8", maps, k_len=lens)
+    want = c.run()
+    c.compare(want)
+    assert same(c.run(), want)
+    c.compare(c.run(key_bound=max(max(lens), 1)))
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
