@@ -90,6 +90,24 @@ __device__ __forceinline__ uint4v operand(const f32x16 &p, int s)
     }
 }
 
+// The same in two operands, the rounded value and what the rounding left, rounded: together
+// off by u^2, which is no more than the 32-bit sums are.
+template <class T>
+__device__ __forceinline__ void operands(const f32x16 &p, int s, uint4v &high, uint4v &low)
+{
+    static_assert(sizeof(T) == 2, "fp32 is exact");
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    T8 h, l;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        h[j] = (T)p[8 * s + j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        l[j] = (T)(p[8 * s + j] - (float)h[j]);
+    high = __builtin_bit_cast(uint4v, h);
+    low = __builtin_bit_cast(uint4v, l);
+}
+
 // Rows of NC channels in LDS.  The loads that write LDS directly fill 1024
 // bytes in order, so rows cannot be padded: the 16-byte pieces of a row are
 // permuted by an exclusive or with a number that depends on the row.  LDS serves

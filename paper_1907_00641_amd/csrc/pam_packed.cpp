@@ -21,7 +21,8 @@ int64_t at_once(const pam_attn_desc_t &d)
 
 // rows: of all sequences, on the axis that is dealt out; walked: tiles of the other
 // axis that a unit of an average sequence walks over, `many` of which are a long walk; least:
-// tiles of a part.
+// tiles of a part, of one team, of two, and of two with so few units that the card is mostly idle
+// (keys, 3 x 1000, 2 key heads, 36 units, 8 tiles 26 us for 32; 4 x 500, 8 heads, 128 units, 42 for 37).
 //
 // Teams (bf16, forward and backward, one team or two): 1 x 500, 8 heads of 64, causal 17 and 34 us
 // for 13 and 36; 4 x 500 20 and 44 for 13 and 38; 2 x 1000, 16 of 128, 39 and 122 for 28 and 84; 3 x 2000, 8
@@ -33,8 +34,8 @@ int64_t at_once(const pam_attn_desc_t &d)
 // Parts: units beyond whole rounds of the blocks that the card holds are cut, to fill one more
 // round; of causal units, which are of unequal lengths, all or none, longest first, and
 // `rounds` rounds of them (keys, 16384 tokens, 2 key heads of 128: one round 1774 us, two 1132).
-PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_t walked, int64_t many, int64_t least,
-                   int64_t rounds)
+PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_t walked, int64_t many,
+                   const int64_t (&least)[3], int64_t rounds)
 {
     PackedPlan p{};
     if (rows == 0)
@@ -51,7 +52,7 @@ PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_
     p.teams = two ? 2 : 1;
     const int64_t room = at_once(d) / p.teams, full = causal ? 0 : units / room * room, rest = units - full;
     const int64_t fill = causal ? (units < room ? rounds * room / units : 1) : (rest ? room / rest : 1);
-    const int64_t parts = std::min(walked / (least * p.teams), fill);
+    const int64_t parts = std::min(walked / least[two ? (units <= kCUs / 4 ? 2 : 1) : 0], fill);
     if (parts > 1) {
         p.full = (uint32_t)full;
         p.parts = (uint32_t)parts;
@@ -70,10 +71,11 @@ Plans plans_of(const pam_attn_desc_t &d, bool backward)
 {
     Plans p{};
     const int64_t cls = packed_class(d.dim, d.dim_v);
-    p.rows = plan_of(d, d.tokens, d.heads, ceil_div(d.keys / d.sequences, 64), 48, 4, 1);
+    p.rows = plan_of(d, d.tokens, d.heads, ceil_div(d.keys / d.sequences, 64), 48, {4, 8, 8}, 1);
     p.row_part = (int64_t)p.rows.cut() * p.rows.parts * kPackedRows * (cls + (backward ? 0 : 2));
     if (backward) {
-        p.keys = plan_of(d, d.keys, d.kv_heads, ceil_div(d.tokens / d.sequences, 32) * (d.heads / d.kv_heads), 96, 8, 2);
+        p.keys = plan_of(d, d.keys, d.kv_heads, ceil_div(d.tokens / d.sequences, 32) * (d.heads / d.kv_heads), 96,
+                         {8, 16, 8}, 2);
         p.key_part = (int64_t)p.keys.cut() * p.keys.parts * kPackedRows * 2 * cls;
         p.stats = 2 * (int64_t)d.heads * d.tokens;
     }

@@ -28,11 +28,12 @@ template <class T, int C>
 struct PackedSizes {
     using R = Rows<T, C>;
     static constexpr int kKeys = R::kBytes <= 256 ? 64 : 32;  // keys per tile
-    static constexpr int kQueries = 32;                       // queries per tile of the keys' pass
+    static constexpr int kQueries = R::kBytes <= 128 ? 64 : 32;  // queries per tile of the keys' pass
     static constexpr int CK = C / kChunk<T>, TV = C / 32, CP = 32 / kChunk<T>;
     // waves per SIMD that the registers are for
     static constexpr bool kSmall = sizeof(T) == 2 || C == 64;
     static constexpr int kWavesPerSimd = kSmall ? 2 : 1;
+    static constexpr bool kTwoOperands = sizeof(T) == 2 && C == 64;  // dq's score gradients
     static constexpr int kKeyTile = 2 * R::size(kKeys);
     static constexpr int kQueryTile = 2 * R::size(kQueries) + 2 * kQueries * 4;  // queries, dout, two statistics
     static constexpr int kValues = R::size(kPackedRows);                         // the keys' pass: the block's values
@@ -203,6 +204,9 @@ __device__ __forceinline__ void clear_outside(T *rows, const int32_t *start, int
          e += (int64_t)gridDim.x * (KS * kAttnThreads))
         rows[e < head ? e : e - head + last * width] = (T)0.0f;
 }
+
+// The lowest n of 64 bits.
+__device__ __forceinline__ uint64_t low_bits64(int n) { return n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1; }
 
 // Scores of this lane's row to -inf where a bit is 0.  bits: of the tile's 32 rows.
 __device__ __forceinline__ void hide_rows(f32x16 &s, uint32_t bits)
@@ -463,8 +467,11 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_join(PackedArgs a)
 // ---------------------------------------------------------------------------
 
 // D and dq.  D is taken from out in 32 bits: it is the difference of dp and D that
-// counts, which may be far smaller than either.  Score gradients are rounded to the
-// activations' type for their product.
+// counts, which may be far smaller than either.  A row's score gradients add up to 0, so that
+// what their rounding leaves counts for more than in the other products, the more the fewer
+// channels there are: with one operand dq was off by 1.45 (heads of 128) to 1.56 times (of 16) as
+// much as by being rounded alone, with two by 1.0.  Heads of up to 64 take two (bf16, 8 of 64, 2 x
+// 4800: 212 us for 165), larger ones one (16384 causal, of 128: 768 us; with two 988).
 template <class T, int C, bool WIDE, int KS>
 __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) void k_packed_dq(PackedArgs a)
 {
@@ -580,10 +587,21 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
                     });
 #pragma unroll
                 for (int x = 0; x < S::CP; ++x) {
-                    const uint4v ds = operand<T>(s[0], x);
+                    if constexpr (S::kTwoOperands) {
+                        uint4v ds, low;
+                        operands<T>(s[0], x, ds, low);
 #pragma unroll
-                    for (int v = 0; v < S::TV; ++v)
-                        mma<T>(acc[v], R::col_chunk(kc, 32 * kt, x, 32 * v), ds);
+                        for (int v = 0; v < S::TV; ++v) {
+                            const uint4v kf = R::col_chunk(kc, 32 * kt, x, 32 * v);
+                            mma<T>(acc[v], kf, ds);
+                            mma<T>(acc[v], kf, low);
+                        }
+                    } else {
+                        const uint4v ds = operand<T>(s[0], x);
+#pragma unroll
+                        for (int v = 0; v < S::TV; ++v)
+                            mma<T>(acc[v], R::col_chunk(kc, 32 * kt, x, 32 * v), ds);
+                    }
                 }
             }
         }
@@ -712,11 +730,11 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
             char *to = mine + buf * S::kQueryTile;
             load_rows<T, C, 1, QT, kAttnWaves, WIDE>(to, qp, a.qs[0], 0, nq - 1 - ni, a.dim, w);
             load_rows<T, C, 1, QT, kAttnWaves, WIDE>(to + R::size(QT), gp, a.dos[0], 0, nq - 1 - ni, a.dim_v, w);
-            // 2 statistics of 32 queries, one by half of each of two waves
+            // 2 statistics of a tile's queries, one by each of two waves
             const int y = again(l);
-            if (w < 2 && y < 32)
+            if (w < 2 && y < QT)
                 load_lds4(uniform_ptr(sp + w * (int64_t)a.tokens), 4u * (uint32_t)min(y, nq - 1 - ni),
-                          lds_address(to + 2 * R::size(QT)) + w * 128);
+                          lds_address(to + 2 * R::size(QT)) + w * (4 * QT));
             const int was = nh;
             step(ni, nh);
             if (nh != was) {
@@ -752,10 +770,9 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
             for (int x = 0; x < KS; ++x)
                 clear = clear || (tt + x < t1 && (i0s[x] + QT > nq || i0s[x] < lowest));
             const int i0 = KS == 2 && ks ? i0s[KS - 1] : i0s[0];
-            const bool tail = i0 + QT > nq;
             if (clear) {  // the same in the whole block
-                if (t < t1 && (tail || i0 < lowest)) {
-                    const uint32_t live = low_bits(nq - i0) & ~low_bits(lowest - i0);
+                if (t < t1 && (i0 + QT > nq || i0 < lowest)) {
+                    const uint64_t live = low_bits64(nq - i0) & ~low_bits64(lowest - i0);
                     clear_rows<T, C, QT, kAttnWaves>(qb_, live, w);
                     clear_rows<T, C, QT, kAttnWaves>(gb, live, w);
                 }
@@ -769,49 +786,55 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
             const uint32_t qr = lds_address(qb_) + R::row_lane(), qc = lds_address(qb_) + R::col_lane();
             const uint32_t gr = lds_address(gb) + R::row_lane(), gc = lds_address(gb) + R::col_lane();
             const uint32_t vr = lds_address(vrows) + R::row_lane();
-            f32x16 s[1], dp = {};
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[0][r] = std::is_same<T, f16>::value ? lifted : 0.0f;
+            for (int qt = 0; qt < QT / 32; ++qt) {
+                const int i1 = i0 + 32 * qt;
+                if (i1 >= nq || i1 + 32 <= wfirst)
+                    continue;
+                f32x16 s[1], dp = {};
 #pragma unroll
-            for (int x = 0; x < S::CK; ++x) {
-                mma<T>(s[0], R::row_chunk(qr, 0, x), kf[x]);
-                mma<T>(dp, R::row_chunk(gr, 0, x), R::row_chunk(vr, 0, x));
-            }
-            if (k0 + 32 * w + 32 > nk || i0 < wfirst + 31 || tail)
-                hide_rows(s[0], low_bits(nq - i0) & ~low_bits(from > i0 ? from - i0 : 0));
-            uint4v pf[S::CP], ds[S::CP];
-            f32x16 p;
+                for (int r = 0; r < 16; ++r)
+                    s[0][r] = std::is_same<T, f16>::value ? lifted : 0.0f;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int at = 8 * g + 4 * (l >> 5);
-                const float4v ls = *reinterpret_cast<const float4v *>(st + at);
-                const float4v d = *reinterpret_cast<const float4v *>(st + QT + at);
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int r = 4 * g + y;
-                    p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, -ls[y]));
-                    s[0][r] = p[r] * (dp[r] - d[y]);
+                for (int x = 0; x < S::CK; ++x) {
+                    mma<T>(s[0], R::row_chunk(qr, 32 * qt, x), kf[x]);
+                    mma<T>(dp, R::row_chunk(gr, 32 * qt, x), R::row_chunk(vr, 0, x));
                 }
-            }
-            if constexpr (std::is_same<T, f16>::value)
-                range.fit(s, [&](float f) {
+                if (k0 + 32 * w + 32 > nk || i1 < wfirst + 31 || i1 + 32 > nq)
+                    hide_rows(s[0], low_bits(nq - i1) & ~low_bits(from > i1 ? from - i1 : 0));
+                uint4v pf[S::CP], ds[S::CP];
+                f32x16 p;
 #pragma unroll
-                    for (int v = 0; v < S::TV; ++v)
-                        gk[v] *= f;
-                });
+                for (int g = 0; g < 4; ++g) {
+                    const int at = 32 * qt + 8 * g + 4 * (l >> 5);
+                    const float4v ls = *reinterpret_cast<const float4v *>(st + at);
+                    const float4v d = *reinterpret_cast<const float4v *>(st + QT + at);
 #pragma unroll
-            for (int x = 0; x < S::CP; ++x) {
-                pf[x] = operand<T>(p, x);
-                ds[x] = operand<T>(s[0], x);
-            }
-#pragma unroll
-            for (int x = 0; x < S::CP; ++x)
-#pragma unroll
-                for (int v = 0; v < S::TV; ++v) {
-                    mma<T>(gv[v], R::col_chunk(gc, 0, x, 32 * v), pf[x]);
-                    mma<T>(gk[v], R::col_chunk(qc, 0, x, 32 * v), ds[x]);
+                    for (int y = 0; y < 4; ++y) {
+                        const int r = 4 * g + y;
+                        p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][r], c, -ls[y]));
+                        s[0][r] = p[r] * (dp[r] - d[y]);
+                    }
                 }
+                if constexpr (std::is_same<T, f16>::value)
+                    range.fit(s, [&](float f) {
+#pragma unroll
+                        for (int v = 0; v < S::TV; ++v)
+                            gk[v] *= f;
+                    });
+#pragma unroll
+                for (int x = 0; x < S::CP; ++x) {
+                    pf[x] = operand<T>(p, x);
+                    ds[x] = operand<T>(s[0], x);
+                }
+#pragma unroll
+                for (int x = 0; x < S::CP; ++x)
+#pragma unroll
+                    for (int v = 0; v < S::TV; ++v) {
+                        mma<T>(gv[v], R::col_chunk(gc, 32 * qt, x, 32 * v), pf[x]);
+                        mma<T>(gk[v], R::col_chunk(qc, 32 * qt, x, 32 * v), ds[x]);
+                    }
+            }
         }
         __syncthreads();
         const float fv = __builtin_amdgcn_exp2f(-lift);

@@ -66,9 +66,8 @@ struct Staged {
             }
         }
     }
-    // to the tile, as T; SCALED: times the row's factor, which lane j has of row j
-    template <bool SCALED>
-    __device__ __forceinline__ void put(char *tile, float scale)
+    // to the tile, as T
+    __device__ __forceinline__ void put(char *tile)
     {
         using R = typename PagedSizes<T, C>::R;
         if (__any(live != (1u << N) - 1)) {
@@ -83,29 +82,16 @@ struct Staged {
         for (int n = 0; n < N; ++n) {
             const int row = row_of(n);
             uint32_t y[E * sizeof(T) / 4];
-            if constexpr (!kScaled<S>) {
 #pragma unroll
-                for (int i = 0; i < kWords; ++i)
-                    y[i] = x[n][i];
-            } else if constexpr (!SCALED) {
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) {
+            for (int i = 0; i < kWords; ++i) {
+                if constexpr (kScaled<S>) {
                     uint32_t z[sizeof(T)];
                     widen<T, S>(x[n][i], z);
 #pragma unroll
                     for (int k = 0; k < (int)sizeof(T); ++k)
                         y[i * sizeof(T) + k] = z[k];
-                }
-            } else {
-                const float f = __shfl(scale, row);
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) {
-                    typedef T T4 __attribute__((ext_vector_type(4)));
-                    uint32_t z[4];
-                    widen<float, S>(x[n][i], z);
-                    const T4 t = {(T)(__uint_as_float(z[0]) * f), (T)(__uint_as_float(z[1]) * f),
-                                  (T)(__uint_as_float(z[2]) * f), (T)(__uint_as_float(z[3]) * f)};
-                    __builtin_memcpy(y + i * sizeof(T), &t, sizeof(t));
+                } else {
+                    y[i] = x[n][i];
                 }
             }
 #pragma unroll
@@ -244,9 +230,16 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
 {
     using Z = PagedSizes<T, C>;
     using R = typename Z::R;
-    // fp16 has no range for a probability times a scale: its values are scaled before
-    // they are rounded (by a relative 2^-11 at most), others by way of the probabilities
-    constexpr bool kValues = kScaled<S> && std::is_same<T, f16>::value, kProbs = kScaled<S> && !kValues;
+    // Numbers of 8 bits are exact in fp16, whose 11 bits leave next to nothing of a probability
+    // beside a bf16 result.  It has no range for a probability times a scale, so that scales go
+    // in relative to a power of two above the largest so far, and the sums follow when it grows
+    // (what is below 2^-20 of the largest product loses precision, at most 2^-31 of it each).
+    // Otherwise probabilities enter their product as two operands, so that the result alone is
+    // rounded (with one, out is off by 1.3 to 1.6 times as much as by its own rounding; e4m3
+    // with bf16 as two operands instead: 114 us for 94, 16 x 16384).
+    constexpr bool kRelative = kScaled<S> && sizeof(T) == 2;
+    constexpr bool kTwo = sizeof(T) == 2 && !(kScaled<S> && std::is_same<T, bf16>::value);
+    typedef typename std::conditional<kRelative, f16, T>::type VT;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int l = lane_id(), w = wave_id();
     const float c = a.scale * kLog2e;
@@ -286,7 +279,8 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
             to = uniform(from + per + (run < more));
         }
 
-        Staged<T, S, C, PE> ks, vs;
+        Staged<T, S, C, PE> ks;
+        Staged<VT, S, C, PE> vs;
         int rid = -1, next = -1;          // rows of the tile under way, and of the one after
         float sk0 = 0.0f, sk1 = 0.0f, sv = 0.0f;
         auto find = [&](int t) {          // lane j: row of key j of tile t
@@ -332,9 +326,28 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
         }
         f32x16 o[Z::TV] = {};
         float top = -INFINITY, sum = 0.0f;
+        int unit_exp = -126;  // scales of values are in units of 2^unit_exp
         for (int t = from; t < to; ++t) {
             const uint32_t seen = (uint32_t)__ballot(rid >= 0);
-            ks.template put<false>(tile, 0.0f);
+            ks.put(tile);
+            if constexpr (kRelative) {
+                float most = sv;
+                most = __builtin_fmaxf(most, lane_move<0xb1>(most));
+                most = __builtin_fmaxf(most, lane_move<0x4e>(most));
+                most = __builtin_fmaxf(most, lane_move<0x141>(most));
+                most = __builtin_fmaxf(most, lane_move<0x140>(most));
+                const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+                most = __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+                const int e = min(max(uniform(__builtin_amdgcn_frexp_expf(most)), -126), 127);  // most < 2^e
+                if (e > unit_exp) {
+                    const float f = __builtin_ldexpf(1.0f, max(unit_exp - e, -200));
+#pragma unroll
+                    for (int v = 0; v < Z::TV; ++v)
+                        o[v] *= f;
+                    unit_exp = e;
+                }
+                sv = __builtin_ldexpf(sv, -unit_exp);
+            }
             if constexpr (kScaled<S>) {
                 if (l < 32) {
                     scales[l] = sk0;
@@ -342,7 +355,6 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
                     scales[64 + l] = sv;
                 }
             }
-            const float sv_here = sv;
             wave_fence();
             const int after = rid = next;
             if (t + 1 < to) {
@@ -382,7 +394,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
                 for (int v = 0; v < Z::TV; ++v)
                     o[v] *= f;
             }
-            const float base = top == -INFINITY ? 0.0f : top - kLift<T>;
+            const float base = top == -INFINITY ? 0.0f : top - kLift<VT>;
             float add = 0.0f;
 #pragma unroll
             for (int y = 0; y < 16; ++y) {
@@ -390,7 +402,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
                 add += s[y];
             }
             sum += add;
-            if constexpr (kProbs) {
+            if constexpr (kScaled<S>) {
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     const float4v f = *reinterpret_cast<const float4v *>(scales + 64 + 8 * y + 4 * (l >> 5));
@@ -399,23 +411,37 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
                         s[4 * y + z] *= f[z];
                 }
             }
-            uint4v p[Z::CP];
+            uint4v p[Z::CP], low[Z::CP];
 #pragma unroll
-            for (int k = 0; k < Z::CP; ++k)
-                p[k] = operand<T>(s, k);
+            for (int k = 0; k < Z::CP; ++k) {
+                if constexpr (kTwo)
+                    operands<VT>(s, k, p[k], low[k]);
+                else
+                    p[k] = operand<VT>(s, k);
+            }
             wave_fence();  // the keys are read
-            vs.template put<kValues>(tile, sv_here);
+            vs.put(tile);
             wave_fence();
             if (t + 1 < to)
                 vs.load((const S *)a.pool.v, after, a.pool.dim_v);
 #pragma unroll
             for (int k = 0; k < Z::CP; ++k)
 #pragma unroll
-                for (int v = 0; v < Z::TV; ++v)
-                    mma<T>(o[v], R::col_chunk(vc, 0, k, 32 * v), p[k]);
+                for (int v = 0; v < Z::TV; ++v) {
+                    const uint4v vf = R::col_chunk(vc, 0, k, 32 * v);
+                    mma<VT>(o[v], vf, p[k]);
+                    if constexpr (kTwo)
+                        mma<VT>(o[v], vf, low[k]);
+                }
             wave_fence();  // the values are read
         }
         sum = xor32_add(sum);
+        if constexpr (kRelative) {
+            const float f = __builtin_ldexpf(1.0f, unit_exp);
+#pragma unroll
+            for (int v = 0; v < Z::TV; ++v)
+                o[v] *= f;
+        }
         // [row][channel] of this wave where its tile was, tops and sums where its scales were
         float *mine = reinterpret_cast<float *>(tile);
         if ((l & 31) < a.live) {
