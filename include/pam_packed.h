@@ -239,7 +239,9 @@ pam_status_t pam_cache_read(const pam_cache_desc_t *desc, int32_t length, const 
  *         map); out: sequences x len_q x heads x dim_v, contiguous.
  *   key_bound : a length that most sequences reach at the most, 0 for that of
  *         the table.  It decides how finely the keys are split, for speed alone.
- * kv_heads divides heads; sequences heads len_q less than 2^31, len_q less than 2^20; scale
+ * With dtype of 16 bits and numbers of 8, a product of a probability and a value's
+ * scale is rounded to 11 bits or to 2^-31 of the largest scale seen, whichever is more.
+ * kv_heads divides heads; sequences heads len_q maps at most 2^30, len_q less than 2^20; scale
  * positive and finite.  The workspace is 16-byte aligned; by the descriptors.
  */
 typedef struct {

@@ -167,7 +167,8 @@ pam_status_t check_paged(const pam_cache_desc_t *c, const pam_paged_attn_desc_t 
     REQUIRE(d, "desc is NULL");
     REQUIRE(d->heads >= 1 && d->heads % c->kv_heads == 0, "kv_heads must divide heads");
     REQUIRE(d->len_q >= 0 && d->len_q < 1 << 20, "len_q must be in [0, 2^20)");
-    REQUIRE((__int128)c->sequences * d->heads * d->len_q <= kMost31, "sequences heads len_q must be less than 2^31");
+    REQUIRE((__int128)c->sequences * d->heads * d->len_q * c->maps <= 1 << 30,
+            "sequences heads len_q maps must be at most 2^30");  // rows and units are numbers of 32 bits
     REQUIRE(d->key_bound >= 0, "key_bound must not be negative");
     REQUIRE(d->scale > 0.0f && d->scale < INFINITY, "scale must be positive and finite");
     return PAM_OK;

@@ -129,6 +129,8 @@ struct Place {
             const int at = (int)(slot - before(hi)), mine = __builtin_amdgcn_mbcnt_hi(
                 (uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
             const uint64_t one = __ballot(t > lo && mine == at);
+            if (!one)  // starts that fall: the sums need not be exact
+                return;
             b = __builtin_ctzll(one);
             rank = lo;
             tiles = uniform(__shfl(t, b));
@@ -221,6 +223,12 @@ __device__ __forceinline__ void hide_rows(f32x16 &s, uint32_t bits)
 // forward
 // ---------------------------------------------------------------------------
 
+// One pass over the keys with the running maximum and sum of the softmax, 4 products of pairs and
+// channels: bound by the matrix cores and, side by side with them, by the exponentials.  Measured, bf16:
+// 16384 tokens, causal, 8 heads of 128 over 2 key heads 555 us (990 TFLOP/s; matrix cores busy
+// 46 % of the time); 2 x 4800, 8 heads of 64, 132 us (34 % busy: 64 channels per exponential
+// instead of 128).  64 keys per step halve what a step costs besides (three tiles ahead
+// instead of one changed nothing).
 // Maxima are followed only when they grow by more than 2^8 (then the sums are
 // scaled): the probabilities are at most 2^8 then, and nothing is lost, since both
 // sums carry the same factor.  Probabilities are rounded to the activations' type for
@@ -235,7 +243,9 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
     const int l = lane_id(), w = wave_id() % kAttnWaves, ks = wave_id() / kAttnWaves;
     const float c = a.scale * kLog2e;
     clear_outside<KS>((T *)a.out, a.q_start, a.sequences, a.tokens, (int64_t)a.heads * a.dim_v);
-    if (a.dim < C || a.dim_v < C) {  // the channels that no load writes
+    // the channels that no load writes (teams meet where they lie, and then take no further item:
+    // a plan has two teams only with fewer than 1024 units)
+    if (a.dim < C || a.dim_v < C) {
         for (int e = threadIdx.x; e < 2 * KS * S::kKeyTile / 16; e += KS * kAttnThreads)
             store16(lds + e * 16, uint4v{0, 0, 0, 0});
         __syncthreads();
@@ -416,7 +426,9 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
     }
 }
 
-// Joins the parts of every unit, a thread per four channels of a row.
+// Joins the parts of every unit, a thread per four channels of a row:
+//   o = sum_p 2^(top_p - top) o_p / sum_p 2^(top_p - top) sum_p.
+// Bound by memory: 2 x 4800 tokens, 8 heads of 64, three parts 8.6 us.
 template <class T, int C, bool WIDE>
 __global__ __launch_bounds__(kAttnThreads) void k_packed_join(PackedArgs a)
 {
@@ -466,7 +478,9 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_join(PackedArgs a)
 // backward: queries
 // ---------------------------------------------------------------------------
 
-// D and dq.  D is taken from out in 32 bits: it is the difference of dp and D that
+// D and dq: three products of pairs, bound by the matrix cores and the exponentials (bf16:
+// 16384 tokens, causal, 8 heads of 128, 768 us, 1075 TFLOP/s, matrix cores busy 54 %; 2 x 4800, 8 of
+// 64, 212 us).  D is taken from out in 32 bits: it is the difference of dp and D that
 // counts, which may be far smaller than either.  A row's score gradients add up to 0, so that
 // what their rounding leaves counts for more than in the other products, the more the fewer
 // channels there are: with one operand dq was off by 1.45 (heads of 128) to 1.56 times (of 16) as
@@ -644,7 +658,9 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
 // backward: keys and values
 // ---------------------------------------------------------------------------
 
-// dk and dv of 128 keys, over the queries of every head of the key head.  Scores
+// dk and dv of 128 keys, over the queries of every head of the key head: four products of pairs,
+// bound as dq's (bf16: 16384 tokens, causal, 8 heads of 128 over 2 key heads 1130 us, 975 TFLOP/s,
+// matrix cores busy 46 %; 2 x 4800, 8 of 64, 265 us; 64 queries at once there, with 32 it was 279).  Scores
 // are formed with queries as rows here: a lane holds one key.  A kernel of its own,
 // apart from dq's: one pass would save two of the seven products, but either dq or
 // dk and dv would have to be summed over blocks, by atomics in an order that changes
@@ -884,7 +900,8 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
     }
 }
 
-// Sums of the parts of both passes' units, in a fixed order: a thread per four channels.
+// Sums of the parts of both passes' units, in a fixed order: a thread per four channels.  Bound by
+// memory: 16384 tokens, 8 heads of 128 over 2 key heads, parts of both 24 us.
 template <class T, int C, bool WIDE>
 __global__ __launch_bounds__(kAttnThreads) void k_packed_finish(PackedArgs a)
 {

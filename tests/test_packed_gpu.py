@@ -952,6 +952,28 @@ def test_paged_attention_large_scores_and_scales(store):
     c.compare(c.run())
 
 
+@pytest.mark.parametrize("store", ["e4m3", "int8"])
+@pytest.mark.parametrize("order", ["rising", "falling", "mixed"])
+def test_paged_attention_value_scales(store, order):
+    """Values from 2^-30 to 2^30 over the keys of a sequence: scales go into the product relative to the largest so far."""
+    c = Paged(60, 2, 2, 400, 16, 4, 2, 64, 64, "bf16", store, k_len=[400, 333])
+    rng = np.random.default_rng(61)
+    size = np.ones((c.pages, 2, 16, 1))
+    for b in range(2):
+        for p in range(400):
+            e = {"rising": p / 400 * 60 - 30, "falling": 30 - p / 400 * 60, "mixed": rng.uniform(-30, 30)}[order]
+            size[c.table_h[b, p // 16], :, p % 16] = 2.0 ** e
+    c.fill(rng.standard_normal((c.pages, 2, 16, 64)), rng.standard_normal((c.pages, 2, 16, 64)) * size)
+    out = c.run()
+    k, v, live = c.gathered(400)
+    want, mag = O.paged(c.qh.reshape(2, 2, 4, 1, 64), k, v, live, c.k_len_h, None, None, 0.125)
+    S = 0.125 * np.linalg.norm(c.qh, axis=-1).max() * np.linalg.norm(k, axis=-1).max()
+    # a product of a probability and a scale: 11 bits, or 2^-31 of the largest scale, whose numbers reach
+    # the largest value; a sum of probabilities is at least 1
+    tol = U["bf16"] * np.abs(want) + (U["f16"] + E * (2 * 70 * S + 420)) * mag + 400 * 2.0 ** -31 * np.abs(v).max()
+    check("out", out, want, tol + TINY["bf16"])
+
+
 def test_paged_attention_strides_streams_graph():
     """Queries as a part of a projection; another stream; captured, the lengths growing between replays."""
     import torch

@@ -191,6 +191,12 @@ def test_paged_attention_refuses(L):
                  dict(scale=math.nan), dict(q_stride=(2 ** 62, 1, 1, 1))):
         assert call(**over) == BAD, over
     assert call(cache=dict(sequences=2 ** 15), heads=2 ** 10, len_q=2 ** 10) == BAD
+    # rows of both maps and units are numbers of 32 bits
+    for over, cache in ((dict(heads=2 ** 11, len_q=2 ** 19), dict(maps=2)), (dict(heads=2 ** 12, len_q=2 ** 19 - 1), dict(maps=1)),
+                        (dict(heads=2 ** 16, len_q=1), dict(sequences=2 ** 15 - 1))):
+        assert call(cache=cache, **over) == BAD and "2^30" in B.last_error()
+        assert L.pam_paged_attn_workspace(ctypes.byref(made(B.CacheDesc, CACHE, cache)),
+                                          ctypes.byref(made(B.PagedAttnDesc, PAGED, over))) == none
     for i in (0, 3, 4, 5, 6, 7, 8, 9):
         args = list(good)
         args[i] = None
