@@ -226,7 +226,7 @@ __device__ __forceinline__ void hide_rows(f32x16 &s, uint32_t bits)
 // One pass over the keys with the running maximum and sum of the softmax, 4 products of pairs and
 // channels: bound by the matrix cores and, side by side with them, by the exponentials.  Measured, bf16:
 // 16384 tokens, causal, 8 heads of 128 over 2 key heads 555 us (990 TFLOP/s; matrix cores busy
-// 46 % of the time); 2 x 4800, 8 heads of 64, 132 us (34 % busy: 64 channels per exponential
+// 50 % of the time); 2 x 4800, 8 heads of 64, 132 us (39 % busy: 64 channels per exponential
 // instead of 128).  64 keys per step halve what a step costs besides (three tiles ahead
 // instead of one changed nothing).
 // Maxima are followed only when they grow by more than 2^8 (then the sums are
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_join(PackedArgs a)
 // ---------------------------------------------------------------------------
 
 // D and dq: three products of pairs, bound by the matrix cores and the exponentials (bf16:
-// 16384 tokens, causal, 8 heads of 128, 768 us, 1075 TFLOP/s, matrix cores busy 54 %; 2 x 4800, 8 of
+// 16384 tokens, causal, 8 heads of 128, 768 us, 1075 TFLOP/s, matrix cores busy 58 %; 2 x 4800, 8 of
 // 64, 212 us).  D is taken from out in 32 bits: it is the difference of dp and D that
 // counts, which may be far smaller than either.  A row's score gradients add up to 0, so that
 // what their rounding leaves counts for more than in the other products, the more the fewer
@@ -660,7 +660,7 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
 
 // dk and dv of 128 keys, over the queries of every head of the key head: four products of pairs,
 // bound as dq's (bf16: 16384 tokens, causal, 8 heads of 128 over 2 key heads 1130 us, 975 TFLOP/s,
-// matrix cores busy 46 %; 2 x 4800, 8 of 64, 265 us; 64 queries at once there, with 32 it was 279).  Scores
+// matrix cores busy 47 %; 2 x 4800, 8 of 64, 265 us; 64 queries at once there, with 32 it was 279).  Scores
 // are formed with queries as rows here: a lane holds one key.  A kernel of its own,
 // apart from dq's: one pass would save two of the seven products, but either dq or
 // dk and dv would have to be summed over blocks, by atomics in an order that changes
