@@ -23,9 +23,10 @@ struct PagedPlan {
     int64_t units, floats;
 };
 
-// The keys are split so that the units fill the card once, unless a wave of a part had fewer
-// than two tiles of 32 keys then.  (16 sequences of up to 16384, 8 key heads: twice or four times
-// as many parts 103 and 116 us for 100, before shares went by lengths.)
+// The keys are split so that the units fill the card once with two blocks per CU, unless a wave
+// of a part had fewer than two tiles of 32 keys then.  One, two and three blocks per CU: 16 sequences of up
+// to 16384, 32 heads of 128 over 8, e4m3, 164, 94 and 112 us; 8 of up to 9000, 4 tokens, 8 heads over 4, 2 maps of
+// 64, int8, 34, 29 and 40; 32 of up to 2000 39, 35 and 42; one of 65536, bf16, 33, 35 and 40.
 PagedPlan plan_of(const pam_cache_desc_t &c, const pam_paged_attn_desc_t &d)
 {
     PagedPlan p;
