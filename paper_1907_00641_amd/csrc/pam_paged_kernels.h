@@ -341,7 +341,9 @@ __global__ __launch_bounds__(64 * kPagedWaves, (PagedSizes<T, C>::kWavesPerSimd)
                 most = __builtin_fmaxf(most, lane_move<0x140>(most));
                 const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(most), __float_as_uint(most), false, false);
                 most = __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-                const int e = min(max(uniform(__builtin_amdgcn_frexp_expf(most)), -126), 127);  // most < 2^e
+                // most < 2^e.  By the exponent's bits: a tile that has no scale, without a page or of zeros, is
+                // at the lowest and leaves the unit as it is.
+                const int e = min((int)((uint32_t)uniform(__float_as_int(most)) >> 23) - 126, 127);
                 if (e > unit_exp) {
                     const float f = __builtin_ldexpf(1.0f, max(unit_exp - e, -200));
 #pragma unroll
