@@ -176,7 +176,8 @@ typedef enum {
  * table_width int32 on the device.  A page number that is not in [0, pages)
  * names no page: its tokens are not written, read as 0 and seen by no query.
  *   k_len : sequences int32 on the device: tokens of each sequence, the new ones
- *           included; clamped to [0, table_width page_size].
+ *           included; clamped to [0, table_width page_size] by what reads the
+ *           cache.  Positions of tokens that are written count from it as it is.
  * Stored rows of 8 bits: scale = max(largest magnitude / top, 2^-126) with top
  * 448 or 127, number = x / scale, clamped to [-top, top], rounded to nearest,
  * ties to even; quotients in fp32.  A row of keys is its dim channels of one map.  The

@@ -222,9 +222,10 @@ __global__ __launch_bounds__(kThreads) void k_cache_write(CacheArgs a)
                 i = (int)(x.row - b * (uint32_t)a.length);
                 n = a.new_len ? min(max(a.new_len[b], 0), a.length) : a.length;
             }
-            const int p = cached(a.pool, b) - n + i;
-            const bool live = u < units && i >= 0 && i < n && p >= 0;
-            at[k] = live ? cache_row(a.pool, a.by_page, b, x.head, p) : -1;
+            // from the length as it is: of one past the table, only what the table reaches is written
+            const uint32_t p = (uint32_t)max(a.pool.k_len[b], 0) - (uint32_t)n + (uint32_t)i;
+            const bool live = u < units && i >= 0 && i < n && p < (uint32_t)a.pool.width * (uint32_t)a.pool.page;
+            at[k] = live ? cache_row(a.pool, a.by_page, b, x.head, (int)p) : -1;
             map[k] = x.map;
             m[k] = live ? max(min(dim - c, E), 0) : 0;
             // with starts, rows are the tokens of one sequence
