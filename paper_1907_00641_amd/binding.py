@@ -962,8 +962,16 @@ def pam_head_norm_rotary_bwd(q: torch.Tensor, k: torch.Tensor | None, table: tor
     return dict(zip(("q", "k", "w_q", "w_k"), grads))
 
 
+def _check_scales(k, k_scale, v_scale):
+    if k.dtype in _STORES and (k_scale is None or v_scale is None):
+        raise ValueError(f"a cache of {k.dtype} has k_scale and v_scale")
+    if k.dtype not in _STORES and (k_scale is not None or v_scale is not None):
+        raise ValueError(f"a cache of {k.dtype} has no scales")
+
+
 class PagedCache:
-    """The tensors of a paged cache, which the caller owns.
+    """The tensors of a paged cache, which the caller owns.  They may be replaced by others of the same shapes, of
+    types that go together: every call takes them as they are then.
 
     ``k`` is pages x Hk x page x d, or pages x Hk x page x 2 x d for differential attention, ``v`` pages x Hk x page
     x dv, contiguous, float32, float16 or bfloat16, or float8_e4m3fn or int8 with ``k_scale`` and ``v_scale``
@@ -975,18 +983,14 @@ class PagedCache:
             raise ValueError("k must be pages x Hk x page x d or pages x Hk x page x 2 x d, v pages x Hk x page x dv")
         if k.dtype not in _DTYPES and k.dtype not in _STORES:
             raise ValueError("a cache is float32, float16, bfloat16, float8_e4m3fn or int8")
-        dev, f32 = k.get_device(), torch.float32
+        dev = k.get_device()
         if dev < 0:
             raise ValueError("k must be a device tensor")
-        if k.dtype in _STORES and (k_scale is None or v_scale is None):
-            raise ValueError(f"a cache of {k.dtype} has k_scale and v_scale")
-        if k.dtype not in _STORES and (k_scale is not None or v_scale is not None):
-            raise ValueError(f"a cache of {k.dtype} has no scales")
+        _check_scales(k, k_scale, v_scale)
         _counts(*k.shape, *v.shape)
         self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, dev
-        self._pool = [_shaped_ptr(k, k.shape, k.dtype, dev, "k"), _shaped_ptr(v, v.shape, k.dtype, dev, "v"),
-                      _shaped_ptr(k_scale, k.shape[:-1], f32, dev, "k_scale"),
-                      _shaped_ptr(v_scale, v.shape[:-1], f32, dev, "v_scale")]
+        self._shapes, self._seen = (k.shape, v.shape, k.shape[:-1], v.shape[:-1]), None
+        self._pool()
         self.maps = 2 if k.dim() == 5 else 1
         self._sizes = (k.shape[0], k.shape[2], k.shape[1], k.shape[-1], v.shape[-1], self.maps)
 
@@ -1002,6 +1006,25 @@ class PagedCache:
             return cls(k, v)
         return cls(k.view(dtype), v.view(dtype), torch.zeros(k.shape[:-1], device=device),
                    torch.zeros(v.shape[:-1], device=device))
+
+    def _pool(self):
+        """Pointers of the tensors as they are now.  Their shapes and types are looked at again where a tensor is another
+        one than before, or its memory is (0.6 us of a call over 8 bits, with all of it each time 1.5)."""
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        if ks is None or vs is None:
+            ptrs = k.data_ptr(), v.data_ptr(), None, None
+            seen = id(k), id(v), id(ks), id(vs), k.nbytes, v.nbytes, ptrs
+        else:
+            ptrs = k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()
+            seen = id(k), id(v), id(ks), id(vs), k.nbytes, v.nbytes, ks.nbytes, vs.nbytes, ptrs
+        if seen == self._seen:
+            return ptrs
+        _check_scales(k, ks, vs)
+        dev, f32, shapes = self.device, torch.float32, self._shapes
+        ptrs = (_shaped_ptr(k, shapes[0], k.dtype, dev, "k"), _shaped_ptr(v, shapes[1], k.dtype, dev, "v"),
+                _shaped_ptr(ks, shapes[2], f32, dev, "k_scale"), _shaped_ptr(vs, shapes[3], f32, dev, "v_scale"))
+        self._seen = seen
+        return ptrs
 
     def _call(self, dtype, table, k_len):
         """Descriptor and the pointers of table, lengths and pool of a call with activations of ``dtype``."""
@@ -1052,7 +1075,7 @@ def pam_cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, table: 
     _check(lib().pam_cache_write(
         ctypes.byref(desc), ctypes.byref(rows), _rows_ptr(k, k.dtype, dev, "k"), _rows_ptr(v, k.dtype, dev, "v"),
         _shaped_ptr(starts, (B + 1,), torch.int32, dev, "starts"), _shaped_ptr(new_len, (B,), torch.int32, dev, "new_len"),
-        pt, pn, *cache._pool, _stream_ptr(stream)), "pam_cache_write")
+        pt, pn, *cache._pool(), _stream_ptr(stream)), "pam_cache_write")
 
 
 def pam_cache_read(cache: PagedCache, table: torch.Tensor, k_len: torch.Tensor, length: int, *, dtype=None,
@@ -1069,7 +1092,7 @@ def pam_cache_read(cache: PagedCache, table: torch.Tensor, k_len: torch.Tensor, 
     kshape, where = (*lead, 2, d) if maps == 2 else (*lead, d), cache.k.device
     k, v = _new(stream, lambda: (torch.empty(kshape, dtype=dtype, device=where),
                                  torch.empty((*lead, dv), dtype=dtype, device=where)))
-    _check(lib().pam_cache_read(ctypes.byref(desc), length, pt, pn, *cache._pool, k.data_ptr(), v.data_ptr(),
+    _check(lib().pam_cache_read(ctypes.byref(desc), length, pt, pn, *cache._pool(), k.data_ptr(), v.data_ptr(),
                                 _stream_ptr(stream)), "pam_cache_read")
     return k, v
 
@@ -1102,6 +1125,6 @@ def pam_paged_attn(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, k_le
     ws_bytes = _workspace_bytes(L.pam_paged_attn_workspace(c, a), "pam_paged_attn")
     out, ws = _new(stream, lambda: (q.new_empty((B, n, H, dv)),
                                     q.new_empty(ws_bytes, dtype=torch.uint8) if ws_bytes else None))
-    _check(L.pam_paged_attn(c, a, pq, pl, pql, pt, pn, *cache._pool, out.data_ptr(),
+    _check(L.pam_paged_attn(c, a, pq, pl, pql, pt, pn, *cache._pool(), out.data_ptr(),
                             ws.data_ptr() if ws_bytes else None, _stream_ptr(stream)), "pam_paged_attn")
     return out
