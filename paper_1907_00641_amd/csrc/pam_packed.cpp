@@ -34,6 +34,11 @@ int64_t at_once(const pam_attn_desc_t &d)
 // Parts: units beyond whole rounds of the blocks that the card holds are cut, to fill one more
 // round; of causal units, which are of unequal lengths, all or none, longest first, and
 // `rounds` rounds of them (keys, 16384 tokens, 2 key heads of 128: one round 1774 us, two 1132).
+// Each part has a place for its sums, also those of places that hold no tile, of which there are up to
+// one per sequence and head: with four times the parts of those rounds nothing is cut. Not causal, 16 heads,
+// cut and whole: 52 x 512 tokens, heads of 64, 2176 parts of 2048, 110 and 96 us, backward 385 and 372; 60 x 512, of
+// 128, 269 and 229, 860 and 831; below, 36 x 512, of 64, 1664 parts,
+// 91 and 275 cut. (4097 x 512 took 4.4 GB for 64 units.)
 PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_t walked, int64_t many,
                    const int64_t (&least)[3], int64_t rounds)
 {
@@ -53,7 +58,8 @@ PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_
     const int64_t room = at_once(d) / p.teams, full = causal ? 0 : units / room * room, rest = units - full;
     const int64_t fill = causal ? (units < room ? rounds * room / units : 1) : (rest ? room / rest : 1);
     const int64_t parts = std::min(walked / least[two ? (units <= kCUs / 4 ? 2 : 1) : 0], fill);
-    if (parts > 1) {
+    const int64_t most = 4 * (causal ? rounds : 1) * room;
+    if (parts > 1 && ((int64_t)p.units() - full) * parts <= most) {
         p.full = (uint32_t)full;
         p.parts = (uint32_t)parts;
     } else if (causal && room == 2 * kCUs && units >= 2 * kCUs) {

@@ -1,9 +1,14 @@
-"""Host-side checks that need no GPU and that test_packed_host.py leaves out: which memory a paged cache's calls take."""
+"""Host-side checks that need no GPU and that test_packed_host.py leaves out: which memory a paged cache's calls take,
+workspaces of many packed sequences."""
+import ctypes
+
 import pytest
 import torch
 
 import paper_1907_00641_amd as P
 from paper_1907_00641_amd import binding as B
+from test_attn_host import L  # noqa: F401
+from test_packed_host import ATTN, made
 
 
 class Recorder:
@@ -100,3 +105,27 @@ def refused(cache, new, table, n):
                  lambda: P.pam_cache_read(cache, table, n, 4, dtype=torch.bfloat16)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_workspaces_of_many_sequences(L, d, causal, dtype):  # noqa: F811
+    """Parts are for the few units beyond whole rounds of the card: at most four times as many as the 512 blocks of a
+    round (causal keys: of two rounds), each 128 rows of sums and, forward, two statistics, however many sequences
+    there are, whose spare places are no work.  A count of units just past a whole round, and just below, of lengths
+    that are whole tiles and others; the gradients' statistics, 2 numbers per row and head, come on top."""
+    channels = 64 if d == 64 else 128
+    most = 4 * 512 * 128 * 4
+    for sequences in (1, 2, 3, 7, 64, 127, 128, 129, 511, 513, 1021, 4096, 4097, 65537):
+        for length in (1, 127, 128, 129, 512, 4096):
+            for heads, kv_heads in ((1, 1), (5, 5), (16, 16), (16, 2)):
+                tokens = sequences * length
+                if tokens >= 2 ** 28:
+                    continue
+                desc = ctypes.byref(made(B.AttnDesc, ATTN, dict(dtype=dtype, sequences=sequences, heads=heads, kv_heads=kv_heads,
+                                                                dim=d, dim_v=d, tokens=tokens, keys=tokens, flags=causal)))
+                what = sequences, length, heads, kv_heads
+                assert L.pam_attn_fwd_workspace(desc) <= most * (channels + 2), what
+                parts = L.pam_attn_bwd_workspace(desc) - 8 * heads * tokens
+                assert parts <= most * channels + (2 if causal else 1) * most * 2 * channels, what
