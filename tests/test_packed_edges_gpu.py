@@ -1,14 +1,82 @@
-"""Edges of attention over packed sequences and of the paged cache that test_packed_gpu.py leaves out: lengths past
-the table, small values beside pages that are not there.  Bounds as there."""
+"""Edges of attention over packed sequences and of the paged cache that test_packed_gpu.py leaves out: starts that fall,
+lengths past the table, small values beside pages that are not there.  Bounds as there."""
 import numpy as np
 import pytest
 
 from helpers import log
 from oracle import packed as O
 from test_attn_gpu import TINY, U, _cuda, check, dev, host  # noqa: F401
-from test_packed_gpu import Cache, E, Paged, ints, numbers, stored_as
+from test_packed_gpu import Cache, E, Packed, Paged, ints, numbers, stored_as
 
 pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------
+# attention over packed sequences
+# ---------------------------------------------------------------------------
+
+class Guarded:
+    """Arrays with 4 KB before and behind each that nothing may change."""
+
+    def __init__(self):
+        self.all = []
+
+    def array(self, shape, dtype):
+        import torch
+
+        n = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+        raw = torch.full((n + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.all.append((raw, n))
+        return raw[4096:4096 + n].view(dtype).view(*shape)
+
+    def untouched(self):
+        return all((raw[:4096] == 0xA5).all() and (raw[4096 + n:] == 0xA5).all() for raw, n in self.all)
+
+
+def guarded_attention(c, q_start, k_start):
+    """Forward and backward through the C ABI on guarded arrays: (out, grads), and whether the guards are whole."""
+    import ctypes
+
+    import torch
+
+    from paper_1907_00641_amd import binding as B
+
+    desc, ptrs, _ = B._attn_desc(c.q, c.k, c.v, q_start, k_start, c.scale, c.causal)
+    L, d, g = B.lib(), ctypes.byref(desc), Guarded()
+    (T, H, _), f32 = c.q.shape, torch.float32
+    out, so, lse = g.array(c.g.shape, c.q.dtype), g.array(c.g.shape, f32), g.array((H, T), f32)
+    grads = [g.array(x.shape, x.dtype) for x in (c.q, c.k, c.v)]
+    ws = [g.array((max(f(d), 16),), torch.uint8) for f in (L.pam_attn_fwd_workspace, L.pam_attn_bwd_workspace)]
+    s = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert L.pam_attn_fwd(d, *ptrs, out.data_ptr(), so.data_ptr(), lse.data_ptr(), ws[0].data_ptr(), s) == B.PAM_OK
+    assert L.pam_attn_bwd(d, *ptrs, so.data_ptr(), lse.data_ptr(), c.g.data_ptr(), (ctypes.c_int64 * 2)(*c.g.stride()[:2]),
+                          *(x.data_ptr() for x in grads), ws[1].data_ptr(), s) == B.PAM_OK
+    torch.cuda.synchronize()
+    return (out, *grads), g.untouched()
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 72])
+def test_attention_starts_that_fall(d, causal, t):
+    """Sequences that would end before they start are empty, up to 64 of them and more: where no row is a sequence's, all
+    results are 0; where sequences lie over each other, nothing beside the arrays is written, forward or backward."""
+    rng = np.random.default_rng(66)
+    c = Packed(67, [300, 137], 0, 4, 2, d, d, t, causal)
+    for count in (2, 64, 65, 200):
+        falls = np.linspace(400, 0, count + 1).astype(int)
+        log(f"[falling starts] {count} sequences, all empty, {d} {t} causal={causal}")
+        res, whole = guarded_attention(c, ints(falls), ints(falls))
+        assert whole and not any(x.any() for x in res)
+        over = rng.integers(0, 438, count + 1)
+        over[::7] = rng.choice([-2 ** 31, 2 ** 31 - 1, 437, 0], len(over[::7]))
+        log(f"[falling starts] {count} sequences over each other")
+        assert guarded_attention(c, ints(over), ints(over[::-1].copy()))[1]
+        assert guarded_attention(c, ints(over), ints(np.linspace(0, 437, count + 1).astype(int)))[1]
+    ends = ints([0, 300, 437])
+    res, whole = guarded_attention(c, ends, ends)
+    assert whole
+    c.compare(res)
 
 
 # ---------------------------------------------------------------------------
