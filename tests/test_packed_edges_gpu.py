@@ -1,19 +1,69 @@
 """Edges of attention over packed sequences and of the paged cache that test_packed_gpu.py leaves out: starts that fall,
-lengths past the table, small values beside pages that are not there.  Bounds as there."""
+lengths past the table, small values beside pages that are not there, and results that are off by their own rounding
+alone.  Bounds as there."""
 import numpy as np
 import pytest
 
 from helpers import log
 from oracle import packed as O
-from test_attn_gpu import TINY, U, _cuda, check, dev, host  # noqa: F401
+from test_attn_gpu import TINY, U, _cuda, check, dev, dt, host  # noqa: F401
 from test_packed_gpu import Cache, E, Packed, Paged, ints, numbers, stored_as
 
 pytestmark = pytest.mark.gpu
 
 
+def own_rounding(name, got, want, t, rest):
+    """Whether ``got`` is off by no more than by being rounded to its type when it is stored, of the norm.
+
+    ``want`` rounded to the type is off by e, and the kernel's values, which differ from ``want`` by less than a step,
+    are when they are rounded, but for chance: 2 / sqrt(N) of it over N values.  ``rest`` is how far they are off before that,
+    which adds at random, in squares.  An operand that is rounded to the type alone would make it 1.41 e and more: its
+    terms are off by as much as the result's values are by their rounding, and their squares add up to more than its own."""
+    import torch
+
+    e = np.linalg.norm(torch.from_numpy(want).to(dt(t)).double().numpy() - want)
+    off, n = np.linalg.norm(host(got) - want), want.size
+    log(f"  {name}: off by {off / e:.3f} times its own rounding, {rest / e:.3f} before it")
+    assert n >= 3000 and rest < 0.6 * e and off <= (1 + 2 / np.sqrt(n)) * np.hypot(e, rest), (name, off / e)
+
+
 # ---------------------------------------------------------------------------
 # attention over packed sequences
 # ---------------------------------------------------------------------------
+
+def sequences(c):
+    """Queries, keys and who sees whom, of each sequence."""
+    for b in range(len(c.q_ends) - 1):
+        x, y = slice(c.q_ends[b], c.q_ends[b + 1]), slice(c.k_ends[b], c.k_ends[b + 1])
+        n, m = x.stop - x.start, y.stop - y.start
+        yield x, y, O.causal(n, m) if c.causal else np.ones((n, m), dtype=bool)
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lens,d", [([300, 137], 64), ([300, 137], 40), ([500], 16), ([140] * 40, 32)], ids=str)
+def test_attention_grad_q_is_rounded_once(lens, d, causal, t):
+    """Heads of up to 64: score gradients enter their product with what their rounding leaves, u^2 of them."""
+    log(f"[packed dq] {lens[:3]} {d} {t} causal={causal}")
+    c = Packed(68, lens, 20, 4, 2, d, d, t, causal)
+    (_, dq, _, _), _ = c.run()
+    r, _ = O.packed(c.qh, c.kh, c.vh, c.scale, c.q_ends, c.k_ends, causal, c.gh)
+    S = c.scale * np.linalg.norm(c.qh, axis=-1).max() * np.linalg.norm(c.kh, axis=-1).max()
+    # 32-bit sums at random: of a score of up to S and of dp over d products, of a row and a column over n keys, an
+    # exponential; the squares of a value's terms, of zero mean, add up to 1.0 to 1.3 times its own (as numpy has them)
+    n = max(lens) + 20
+    rest = 1.2 * (E * (np.sqrt(d + 6) * S + np.sqrt(d + 8) + np.sqrt(n) + 8) + U[t] ** 2) * np.linalg.norm(r["dq"])
+    # D is of out as the forward pass saves it, whose probabilities are rounded to the type: off by at most u each,
+    # u^2 / 3 in squares, D_i by the root of sum u^2 / 3 (p_ij dp_ij)^2, and dq_i by that times scale sum p_ij k_j
+    square = 0.0
+    for x, y, see in sequences(c):
+        for h in range(4):
+            p, _ = O._softmax(c.scale * c.qh[x, h] @ c.kh[y, h // 2].T, see)
+            dp = c.gh[x, h] @ c.vh[y, h // 2].T
+            square += (((p * dp) ** 2).sum(1) * ((p @ c.kh[y, h // 2]) ** 2).sum(1)).sum()
+    rest = np.hypot(rest, c.scale * U[t] * np.sqrt(square / 3))
+    own_rounding("dq", dq, r["dq"], t, rest)
+
 
 class Guarded:
     """Arrays with 4 KB before and behind each that nothing may change."""
@@ -160,3 +210,21 @@ def test_paged_attention_small_values_beside_a_hole(what, from_, to, store, t, s
     # reach the largest value; a sum of probabilities is at least 1
     tol = U[t] * np.abs(want) + (U["f16"] + E * (2 * 70 * S + 420)) * mag + 400 * 2.0 ** -31 * np.abs(v).max()
     check("out", out, want, tol + TINY[t])
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("store", ["same", "e4m3", "int8"])
+@pytest.mark.parametrize("maps,d,total", [(1, 64, 400), (2, 64, 400), (1, 128, 90), (1, 40, 3000)], ids=str)
+def test_paged_attention_is_rounded_once(maps, d, total, store, t):
+    """Pages of 16 bits, and of 8 with fp16: probabilities enter their product with what their rounding leaves; pages of
+    8 bits with bf16: in fp16, 2^-11 of each term."""
+    log(f"[paged] {maps} {d} {total} {store} {t}")
+    c = Paged(69, 3, 2, total, 16, 16, 2, d, d * maps, t, stored_as(t, store), maps, k_len=[total, total // 2, total - 1])
+    out = c.run()
+    k, v, live = c.gathered(total)
+    want, _ = O.paged(c.qh.reshape(3, 2, 16, maps, d), k, v, live, c.k_len_h, None, c.lamh, d ** -0.5)
+    S = d ** -0.5 * np.linalg.norm(c.qh, axis=-1).max() * np.linalg.norm(k, axis=-1).max()
+    rounded = U["f16"] if store != "same" and t == "bf16" else U[t] ** 2
+    # as above; values are of zero mean
+    rest = 1.2 * (E * (np.sqrt(maps * d + 6) * S + np.sqrt(total) + 8) + rounded) * np.linalg.norm(want)
+    own_rounding("out", out, want, t, rest)
