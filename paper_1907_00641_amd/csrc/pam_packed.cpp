@@ -70,12 +70,13 @@ PackedPlan plan_of(const pam_attn_desc_t &d, int64_t rows, int64_t heads, int64_
 
 struct Plans {
     PackedPlan rows, keys;
-    int64_t row_part, key_part, stats;  // floats
+    int64_t row_part, key_part, stats, places;  // numbers of 4 bytes; places: of an axis
 };
 
 Plans plans_of(const pam_attn_desc_t &d, bool backward)
 {
     Plans p{};
+    p.places = d.sequences > kScanned ? d.sequences + 1 : 0;
     const int64_t cls = packed_class(d.dim, d.dim_v);
     p.rows = plan_of(d, d.tokens, d.heads, ceil_div(d.keys / d.sequences, 64), 48, {4, 8, 8}, 1);
     p.row_part = (int64_t)p.rows.cut() * p.rows.parts * kPackedRows * (cls + (backward ? 0 : 2));
@@ -133,13 +134,14 @@ bool at16(const void *p) { return (uintptr_t)p % 16 == 0; }
 
 size_t packed_fwd_workspace(const pam_attn_desc_t &d)
 {
-    return d.tokens ? (size_t)plans_of(d, false).row_part * sizeof(float) : 0;
+    const Plans p = plans_of(d, false);
+    return d.tokens ? (size_t)(p.row_part + p.places) * sizeof(float) : 0;
 }
 
 size_t packed_bwd_workspace(const pam_attn_desc_t &d)
 {
     const Plans p = plans_of(d, true);
-    return (size_t)(p.row_part + p.key_part + p.stats) * sizeof(float);
+    return (size_t)(p.row_part + p.key_part + p.stats + 2 * p.places) * sizeof(float);
 }
 
 hipError_t launch_packed_fwd(const pam_attn_desc_t &d, const void *q, const void *k, const void *v,
@@ -147,8 +149,10 @@ hipError_t launch_packed_fwd(const pam_attn_desc_t &d, const void *q, const void
                              void *workspace, hipStream_t s)
 {
     PackedArgs a = args_of(d, q, k, v, q_start, k_start);
-    a.plan = plans_of(d, false).rows;
+    const Plans p = plans_of(d, false);
+    a.plan = p.rows;
     a.part = (float *)workspace;
+    a.q_places = p.places ? (uint32_t *)(a.part + p.row_part) : nullptr;
     a.out = out;
     a.so = so;
     a.lse = lse;
@@ -170,6 +174,8 @@ hipError_t launch_packed_bwd(const pam_attn_desc_t &d, const void *q, const void
     a.part = (float *)workspace;
     a.key_part = a.part + p.row_part;
     a.stats = a.key_part + p.key_part;
+    a.q_places = p.places ? (uint32_t *)(a.stats + p.stats) : nullptr;
+    a.k_places = p.places ? a.q_places + p.places : nullptr;
     a.so = const_cast<float *>(so);
     a.lse = const_cast<float *>(lse);
     a.dout = dout;

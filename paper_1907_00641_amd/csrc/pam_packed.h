@@ -6,6 +6,7 @@
 namespace pam {
 
 constexpr int kPackedRows = 128;  // rows (queries, or keys) of a block
+constexpr int kScanned = 256;     // sequences that a block looks through for its place
 
 // How a launch's work is dealt out.  A unit is a place for a tile of 128 rows, of one head:
 // there are as many places as the sequences' tiles at the most (which sequence's tile a place
@@ -28,6 +29,7 @@ struct PackedArgs {
     float scale;
     PackedPlan plan, key_plan;
     float *part, *key_part;
+    uint32_t *q_places, *k_places;  // more than kScanned sequences: tiles before each, and in all
     void *out;
     float *so, *lse;
     const void *dout;

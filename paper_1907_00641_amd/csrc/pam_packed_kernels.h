@@ -86,28 +86,82 @@ __device__ __forceinline__ void rows_of(const int32_t *start, int total, int b, 
     }
 }
 
+__device__ __forceinline__ int tiles_of(const int32_t *start, int total, int s)
+{
+    int from, n;
+    rows_of(start, total, s, from, n);
+    return (n + kPackedRows - 1) / kPackedRows;
+}
+
+// Tiles before every sequence and, behind the last one, in all, for places of more than kScanned
+// sequences; a block for the queries' and one for the keys'.  Sums stop at 2^30, past every place: only those of
+// starts that fall come there.
+constexpr int kPlacesThreads = 1024, kPlacesPer = 8;  // sequences of a thread and turn
+__global__ __launch_bounds__(kPlacesThreads) void k_packed_places(PackedArgs a)
+{
+    __shared__ uint32_t wave[kPlacesThreads / 64];
+    const bool key = blockIdx.x;
+    const int32_t *start = key ? a.k_start : a.q_start;
+    const int total = key ? a.keys : a.tokens, l = lane_id(), w = wave_id();
+    uint32_t *upto = key ? a.k_places : a.q_places;
+    auto add = [](uint32_t x, uint32_t y) { return min(x + y, 1u << 30); };
+    uint32_t past = 0;
+    for (int s0 = 0; s0 < a.sequences; s0 += kPlacesThreads * kPlacesPer) {
+        const int s = s0 + threadIdx.x * kPlacesPer;
+        uint32_t t[kPlacesPer], sum = 0;
+#pragma unroll
+        for (int j = 0; j < kPlacesPer; ++j) {
+            t[j] = s + j < a.sequences ? tiles_of(start, total, s + j) : 0;
+            sum = add(sum, t[j]);
+        }
+        uint32_t before = sum;
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) {
+            const uint32_t y = __shfl_up(before, x);
+            before = l >= x ? add(before, y) : before;
+        }
+        __syncthreads();  // the turn before is done with the waves' sums
+        if (l == 63)
+            wave[w] = before;
+        const uint32_t lane = __shfl_up(before, 1);
+        __syncthreads();
+        before = past;
+        for (int x = 0; x < kPlacesThreads / 64; ++x) {
+            before = x < w ? add(before, wave[x]) : before;
+            past = add(past, wave[x]);
+        }
+        before = l > 0 ? add(before, lane) : before;
+#pragma unroll
+        for (int j = 0; j < kPlacesPer; ++j) {
+            if (s + j < a.sequences)
+                upto[s + j] = before;
+            before = add(before, t[j]);
+        }
+    }
+    if (threadIdx.x == 0)
+        upto[a.sequences] = past;
+}
+
 // Which tile a place holds.  Up to 64 sequences: the longest first (tiles in the order
 // of how many their sequence has before them: a causal query tile walks over so many
 // keys), a sequence to a lane; the number of tiles with `t` or more before them
-// falls with t, which is found by halving.  More sequences: one after the other.
+// falls with t, which is found by halving.  More sequences: one after the other, up to
+// kScanned of them in runs of 64 from the first on, and still more among `upto` (k_packed_places), which 64 lanes cut in 64 at
+// a time.  Scanned, and with places (causal, 8 heads of 64, bf16, forward and backward): 128 sequences of 128 tokens 22 and 71 us
+// for 27 and 78, 300 49 and 170 for 49 and 162, 512 89 and 342 for 75 and 289, 4096 2219 and 6175 for 698 and 2235. The
+// search of all blocks grows with the square of the sequences where each starts at the first.
 // RANK: as many tiles before it in its sequence, of `tiles`.
 struct Place {
     int b = -1, rank = 0, tiles = 0;
-    __device__ __forceinline__ Place(const int32_t *start, int sequences, int total, uint32_t slot)
+    __device__ __forceinline__ Place(const int32_t *start, const uint32_t *upto, int sequences, int total, uint32_t slot)
     {
-        auto tiles_of = [&](int s) {
-            int from, n = 0;
-            if (s < sequences)
-                rows_of(start, total, s, from, n);
-            return (n + kPackedRows - 1) / kPackedRows;
-        };
         const int l = lane_id();
         if (sequences == 1) {
-            tiles = tiles_of(0);
+            tiles = tiles_of(start, total, 0);
             rank = tiles - 1 - (int)slot;
             b = rank >= 0 ? 0 : -1;
         } else if (sequences <= 64) {
-            const int t = tiles_of(l);
+            const int t = l < sequences ? tiles_of(start, total, l) : 0;
             // sums of at most 2^24 tiles are exact in 32 bits
             auto before = [&](int x) { return (uint32_t)uniform((int)lanes_sum<64>((float)max(t - x, 0))); };
             int most = t;
@@ -134,26 +188,39 @@ struct Place {
             b = __builtin_ctzll(one);
             rank = lo;
             tiles = uniform(__shfl(t, b));
-        } else {
+        } else if (!upto) {
             uint32_t past = 0;
             for (int s0 = 0; s0 < sequences; s0 += 64) {
-                const int t = tiles_of(s0 + l);
-                uint32_t upto = t;
+                const int t = s0 + l < sequences ? tiles_of(start, total, s0 + l) : 0;
+                uint32_t to = t;
 #pragma unroll
                 for (int s = 1; s < 64; s <<= 1) {
-                    const uint32_t x = __shfl_up(upto, s);
-                    upto += l >= s ? x : 0;
+                    const uint32_t x = __shfl_up(to, s);
+                    to += l >= s ? x : 0;
                 }
-                const uint64_t reach = __ballot(past + upto > slot);
+                const uint64_t reach = __ballot(past + to > slot);
                 if (reach) {
                     const int at = __builtin_ctzll(reach);
                     b = s0 + at;
                     tiles = uniform(__shfl(t, at));
-                    rank = uniform((int)(past + __shfl(upto, at) - 1 - slot));
+                    rank = uniform((int)(past + __shfl(to, at) - 1 - slot));
                     return;
                 }
-                past += uniform((int)__shfl(upto, 63));
+                past += uniform((int)__shfl(to, 63));
             }
+        } else {
+            if (slot >= (uint32_t)uniform((int)upto[sequences]))
+                return;
+            int lo = 0, n = sequences;  // upto[lo] <= slot < upto[lo + n]
+            while (n > 1) {
+                const int step = (n + 63) / 64, at = l * step;
+                const int last = __popcll(__ballot(at < n && upto[lo + min(at, n - 1)] <= slot)) - 1;
+                lo = uniform(lo + last * step);
+                n = uniform(min(step, n - last * step));
+            }
+            b = lo;
+            tiles = uniform(tiles_of(start, total, b));
+            rank = uniform((int)upto[b]) + tiles - 1 - (int)slot;
         }
     }
 };
@@ -171,14 +238,15 @@ struct PackedItem {
     {
         return n >= p.fold && n < 2 * p.fold ? 3 * p.fold - 1 - n : n;
     }
-    __device__ __forceinline__ PackedItem(const PackedPlan &p, const int32_t *start, int sequences, int total, uint32_t n)
-        : PackedItem(p, start, sequences, total, order(p, n), uniform((order(p, n) - p.full) / p.parts))
+    __device__ __forceinline__ PackedItem(const PackedPlan &p, const int32_t *start, const uint32_t *upto, int sequences,
+                                          int total, uint32_t n)
+        : PackedItem(p, start, upto, sequences, total, order(p, n), uniform((order(p, n) - p.full) / p.parts))
     {
     }
-    __device__ __forceinline__ PackedItem(const PackedPlan &p, const int32_t *start, int sequences, int total, uint32_t m,
-                                          uint32_t cut)
+    __device__ __forceinline__ PackedItem(const PackedPlan &p, const int32_t *start, const uint32_t *upto, int sequences,
+                                          int total, uint32_t m, uint32_t cut)
         : unit(m < p.full ? m : p.full + cut), slot(m - p.full), part(m < p.full ? 0 : m - p.full - cut * p.parts),
-          parts(m < p.full ? 1 : p.parts), h(0), place(start, sequences, total, uniform(unit / p.heads))
+          parts(m < p.full ? 1 : p.parts), h(0), place(start, upto, sequences, total, uniform(unit / p.heads))
     {
         h = uniform(unit - unit / p.heads * p.heads);
     }
@@ -252,7 +320,7 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
     }
     const uint32_t items = a.plan.items();
     for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
-        const PackedItem item(a.plan, a.q_start, a.sequences, a.tokens, n);
+        const PackedItem item(a.plan, a.q_start, a.q_places, a.sequences, a.tokens, n);
         if (item.place.b < 0)  // the same in the whole block
             continue;
         const int h = item.h, hk = uniform(h / a.group);
@@ -438,7 +506,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_join(PackedArgs a)
     for (uint32_t n = blockIdx.x; n < blocks; n += gridDim.x) {
         const uint32_t u = n / STEPS, unit = a.plan.full + u, slot = unit / a.plan.heads;
         const int h = unit - slot * a.plan.heads;
-        const Place place(a.q_start, a.sequences, a.tokens, uniform(slot));
+        const Place place(a.q_start, a.q_places, a.sequences, a.tokens, uniform(slot));
         if (place.b < 0)
             continue;
         int qb, nq;
@@ -503,7 +571,7 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
     }
     const uint32_t items = a.plan.items();
     for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
-        const PackedItem item(a.plan, a.q_start, a.sequences, a.tokens, n);
+        const PackedItem item(a.plan, a.q_start, a.q_places, a.sequences, a.tokens, n);
         if (item.place.b < 0)
             continue;
         const int h = item.h, hk = uniform(h / a.group);
@@ -683,7 +751,7 @@ __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd
     }
     const uint32_t items = a.key_plan.items();
     for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
-        const PackedItem item(a.key_plan, a.k_start, a.sequences, a.keys, n);
+        const PackedItem item(a.key_plan, a.k_start, a.k_places, a.sequences, a.keys, n);
         if (item.place.b < 0)
             continue;
         const int hk = item.h, h0 = hk * a.group, h1 = h0 + a.group;
@@ -916,7 +984,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_finish(PackedArgs a)
         const int h = unit - slot * p.heads;
         const int32_t *start = key ? a.k_start : a.q_start;
         const int total = key ? a.keys : a.tokens;
-        const Place place(start, a.sequences, total, uniform(slot));
+        const Place place(start, key ? a.k_places : a.q_places, a.sequences, total, uniform(slot));
         if (place.b < 0)
             continue;
         int base, len;
@@ -997,9 +1065,21 @@ hipError_t packed_bwd_launch(const PackedArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
+// more than kScanned sequences: the tiles before each, for the queries, and (both) for the keys
+inline hipError_t packed_places(const PackedArgs &a, bool both, hipStream_t s)
+{
+    if (!a.q_places)
+        return hipSuccess;
+    hipLaunchKernelGGL(k_packed_places, dim3(both ? 2 : 1), dim3(kPlacesThreads), 0, s, a);
+    return hipGetLastError();
+}
+
 template <class T>
 hipError_t packed_fwd(const PackedArgs &a, hipStream_t s)
 {
+    const hipError_t e = packed_places(a, false, s);
+    if (e != hipSuccess)
+        return e;
     if (packed_class(a.dim, a.dim_v) == 64)
         return a.wide ? packed_fwd_launch<T, 64, true>(a, s) : packed_fwd_launch<T, 64, false>(a, s);
     return a.wide ? packed_fwd_launch<T, 128, true>(a, s) : packed_fwd_launch<T, 128, false>(a, s);
@@ -1008,6 +1088,9 @@ hipError_t packed_fwd(const PackedArgs &a, hipStream_t s)
 template <class T>
 hipError_t packed_bwd(const PackedArgs &a, hipStream_t s)
 {
+    const hipError_t e = packed_places(a, true, s);
+    if (e != hipSuccess)
+        return e;
     if (packed_class(a.dim, a.dim_v) == 64)
         return a.wide ? packed_bwd_launch<T, 64, true>(a, s) : packed_bwd_launch<T, 64, false>(a, s);
     return a.wide ? packed_bwd_launch<T, 128, true>(a, s) : packed_bwd_launch<T, 128, false>(a, s);

@@ -7,7 +7,7 @@ import pytest
 from helpers import log
 from oracle import packed as O
 from test_attn_gpu import TINY, U, _cuda, check, dev, dt, host  # noqa: F401
-from test_packed_gpu import Cache, E, Packed, Paged, ints, numbers, stored_as
+from test_packed_gpu import Cache, E, Packed, Paged, ints, numbers, same, stored_as
 
 pytestmark = pytest.mark.gpu
 
@@ -65,6 +65,61 @@ def test_attention_grad_q_is_rounded_once(lens, d, causal, t):
     own_rounding("dq", dq, r["dq"], t, rest)
 
 
+def compare_short(c, results):
+    """As Packed.compare, and with a term that only counts where a sequence has few keys: D is of out as the forward pass
+    saves it, from probabilities that are rounded to the type, each by u: it is off by d_i = u sum_j p_ij |dp_ij| at the
+    most, dq_i by d_i scale |sum_j p_ij k_j|, and dk_j by scale sum_i d_i p_ij |q_i|."""
+    r, a = O.packed(c.qh, c.kh, c.vh, c.scale, c.q_ends, c.k_ends, c.causal, c.gh)
+    u, tiny, (_, H, d), hk = U[c.t], TINY[c.t], c.qh.shape, c.kh.shape[1]
+    by_d = {"dq": np.zeros_like(c.qh), "dk": np.zeros_like(c.kh)}
+    for x, y, see in sequences(c):
+        for h in range(H):
+            k = h // (H // hk)
+            p, _ = O._softmax(c.scale * c.qh[x, h] @ c.kh[y, k].T, see)
+            off = u * (p * np.abs(c.gh[x, h] @ c.vh[y, k].T)).sum(1, keepdims=True)
+            by_d["dq"][x, h] = off * c.scale * np.abs(p @ c.kh[y, k])
+            by_d["dk"][y, k] += c.scale * (p * off).T @ np.abs(c.qh[x, h])
+    lk, lq = int(np.diff(c.k_ends).max()), int(np.diff(c.q_ends).max()) * (H // hk)
+    S = c.scale * np.linalg.norm(c.qh, axis=-1).max() * np.linalg.norm(c.kh, axis=-1).max()
+    e, ep = E * (2 * (d + 6) * S + 16 + lk), E * (c.vh.shape[-1] + 8)
+    check("out", results[0], r["out"], u * np.abs(r["out"]) + (u + e) * a["out"] + tiny)
+    for name, got, n in (("dq", results[1], lk), ("dk", results[2], lq)):
+        A0, AD, AP = a[name]
+        check(name, got, r[name], u * np.abs(r[name]) + (u + e + n * E) * A0 + (2 * e + ep) * (AD + AP) + by_d[name] + tiny)
+    check("dv", results[3], r["dv"], u * np.abs(r["dv"]) + (u + e + lq * E) * a["dv"] + tiny)
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("count", [256, 257, 1000, 4097])
+def test_attention_very_many_sequences(count, causal, t):
+    """Places found by looking through the sequences, and among sums of their tiles; of no row, of one, of a tile and of
+    several; replayed from a graph with other lengths in the same starts."""
+    import torch
+
+    import paper_1907_00641_amd as P
+
+    log(f"[packed] {count} sequences {t} causal={causal}")
+    rng = np.random.default_rng(count)
+    lens = [int(x) for x in rng.choice([0, 1, 5, 17, 40], count)]
+    for i, n in ((0, 129), (3, 256), (count // 2, 300), (count - 1, 130)):
+        lens[i] = n
+    c = Packed(70, lens, 1, 2, 1, 24, 24, t, causal, before=3, behind=5)
+    res, _ = c.run()
+    compare_short(c, res)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, s = P.pam_attn_fwd(c.q, c.k, c.v, save=True, **c.how)
+        grads = P.pam_attn_bwd(c.q, c.k, c.v, s, c.g, **c.how)
+    for ends in (c.q_ends, [n // 2 for n in c.q_ends], c.q_ends):
+        c.how["q_start"].copy_(ints(ends))
+        c.how["k_start"].copy_(ints(ends))
+        for _ in range(2):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert same((out, *grads), c.run()[0])
+
+
 class Guarded:
     """Arrays with 4 KB before and behind each that nothing may change."""
 
@@ -113,7 +168,7 @@ def test_attention_starts_that_fall(d, causal, t):
     results are 0; where sequences lie over each other, nothing beside the arrays is written, forward or backward."""
     rng = np.random.default_rng(66)
     c = Packed(67, [300, 137], 0, 4, 2, d, d, t, causal)
-    for count in (2, 64, 65, 200):
+    for count in (2, 64, 65, 200, 300, 9000):
         falls = np.linspace(400, 0, count + 1).astype(int)
         log(f"[falling starts] {count} sequences, all empty, {d} {t} causal={causal}")
         res, whole = guarded_attention(c, ints(falls), ints(falls))

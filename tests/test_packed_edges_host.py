@@ -114,7 +114,8 @@ def test_attention_workspaces_of_many_sequences(L, d, causal, dtype):  # noqa: F
     """Parts are for the few units beyond whole rounds of the card: at most four times as many as the 512 blocks of a
     round (causal keys: of two rounds), each 128 rows of sums and, forward, two statistics, however many sequences
     there are, whose spare places are no work.  A count of units just past a whole round, and just below, of lengths
-    that are whole tiles and others; the gradients' statistics, 2 numbers per row and head, come on top."""
+    that are whole tiles and others; the gradients' statistics, 2 numbers per row and head, come on top, and of more
+    than 256 sequences a number for each (queries and keys) and one."""
     channels = 64 if d == 64 else 128
     most = 4 * 512 * 128 * 4
     for sequences in (1, 2, 3, 7, 64, 127, 128, 129, 511, 513, 1021, 4096, 4097, 65537):
@@ -125,7 +126,7 @@ def test_attention_workspaces_of_many_sequences(L, d, causal, dtype):  # noqa: F
                     continue
                 desc = ctypes.byref(made(B.AttnDesc, ATTN, dict(dtype=dtype, sequences=sequences, heads=heads, kv_heads=kv_heads,
                                                                 dim=d, dim_v=d, tokens=tokens, keys=tokens, flags=causal)))
-                what = sequences, length, heads, kv_heads
-                assert L.pam_attn_fwd_workspace(desc) <= most * (channels + 2), what
-                parts = L.pam_attn_bwd_workspace(desc) - 8 * heads * tokens
+                what, places = (sequences, length, heads, kv_heads), 4 * (sequences + 1) if sequences > 256 else 0
+                assert L.pam_attn_fwd_workspace(desc) - places <= most * (channels + 2), what
+                parts = L.pam_attn_bwd_workspace(desc) - 8 * heads * tokens - 2 * places
                 assert parts <= most * channels + (2 if causal else 1) * most * 2 * channels, what
