@@ -90,8 +90,10 @@ pam_status_t pam_attn_fwd(const pam_attn_desc_t *desc, const void *q, const void
  *   grad_out : tokens x heads x dim_v with strides do_stride (token, head);
  *         grad_q, grad_k, grad_v contiguous, of type dtype, written in full.
  * Other arguments as the forward call's, which saved_o and saved_lse are from.
- * Sums run in a fixed order (the results of two calls are equal).
- * Asynchronous.
+ * Sums run in a fixed order (the results of two calls are equal).  With 16 bits
+ * the matrix units take p and ds rounded to dtype, but for grad_q of dim and
+ * dim_v up to 64 ds with what its rounding left: that is off by little more than
+ * its own rounding, the others by about 1.4 times as much.  Asynchronous.
  */
 pam_status_t pam_attn_bwd(const pam_attn_desc_t *desc, const void *q, const void *k, const void *v,
                           const int32_t *q_start, const int32_t *k_start, const float *saved_o, const float *saved_lse,
@@ -241,7 +243,9 @@ pam_status_t pam_cache_read(const pam_cache_desc_t *desc, int32_t length, const 
  *   key_bound : a length that most sequences reach at the most, 0 for that of
  *         the table.  It decides how finely the keys are split, for speed alone.
  * With dtype of 16 bits and numbers of 8, a product of a probability and a value's
- * scale is rounded to 11 bits or to 2^-31 of the largest scale seen, whichever is more.
+ * scale is rounded to 11 bits or to 2^-31 of the largest scale that a new token of
+ * the sequence sees, whichever is more.  Every 32 rows of a key head (its heads,
+ * tokens and maps) read the sequence's keys again: for one token or a few.
  * kv_heads divides heads; sequences heads len_q maps at most 2^30, len_q less than 2^20; scale
  * positive and finite.  The workspace is 16-byte aligned; by the descriptors.
  */

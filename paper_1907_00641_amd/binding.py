@@ -1054,7 +1054,8 @@ def pam_cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, table: 
     ``table`` (B x pages of a sequence, int32) names them, ``k_len`` (B int32) counts each sequence's tokens, the new
     ones included.  ``k`` is B x L x Hk x d (or B x L x Hk x 2 x d) and ``v`` B x L x Hk x dv, of which sequence b's
     first new_len[b] rows are new (B int32; None: L); with ``starts`` (B + 1 int32) they are packed, without the
-    first axis: sequence b has rows starts[b] .. starts[b + 1] - 1.  Any strides with the last axis contiguous."""
+    first axis: sequence b has rows starts[b] .. starts[b + 1] - 1.  Tokens that the table does not reach
+    are not written.  Any strides with the last axis contiguous."""
     pages, page, hk, d, dv, maps = cache._sizes
     lead = 1 if starts is not None else 2
     tail = (hk, 2, d) if maps == 2 else (hk, d)

@@ -552,7 +552,7 @@ __global__ __launch_bounds__(kAttnThreads) void k_packed_join(PackedArgs a)
 // counts, which may be far smaller than either.  A row's score gradients add up to 0, so that
 // what their rounding leaves counts for more than in the other products, the more the fewer
 // channels there are: with one operand dq was off by 1.45 (heads of 128) to 1.56 times (of 16) as
-// much as by being rounded alone, with two by 1.0.  Heads of up to 64 take two (bf16, 8 of 64, 2 x
+// much as by being rounded alone, with two by 1.01 to 1.04.  Heads of up to 64 take two (bf16, 8 of 64, 2 x
 // 4800: 212 us for 165), larger ones one (16384 causal, of 128: 768 us; with two 988).
 template <class T, int C, bool WIDE, int KS>
 __global__ __launch_bounds__(KS *kAttnThreads, (PackedSizes<T, C>::kWavesPerSimd)) void k_packed_dq(PackedArgs a)
