@@ -86,10 +86,12 @@ __device__ __forceinline__ void rows_of(const int32_t *start, int total, int b, 
     }
 }
 
-__device__ __forceinline__ int tiles_of(const int32_t *start, int total, int s)
+// tiles of sequence s, 0 past the last
+__device__ __forceinline__ int tiles_of(const int32_t *start, int sequences, int total, int s)
 {
-    int from, n;
-    rows_of(start, total, s, from, n);
+    int from, n = 0;
+    if (s < sequences)
+        rows_of(start, total, s, from, n);
     return (n + kPackedRows - 1) / kPackedRows;
 }
 
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(kPlacesThreads) void k_packed_places(PackedArgs a)
         uint32_t t[kPlacesPer], sum = 0;
 #pragma unroll
         for (int j = 0; j < kPlacesPer; ++j) {
-            t[j] = s + j < a.sequences ? tiles_of(start, total, s + j) : 0;
+            t[j] = tiles_of(start, a.sequences, total, s + j);
             sum = add(sum, t[j]);
         }
         uint32_t before = sum;
@@ -157,11 +159,11 @@ struct Place {
     {
         const int l = lane_id();
         if (sequences == 1) {
-            tiles = tiles_of(start, total, 0);
+            tiles = tiles_of(start, sequences, total, 0);
             rank = tiles - 1 - (int)slot;
             b = rank >= 0 ? 0 : -1;
         } else if (sequences <= 64) {
-            const int t = l < sequences ? tiles_of(start, total, l) : 0;
+            const int t = tiles_of(start, sequences, total, l);
             // sums of at most 2^24 tiles are exact in 32 bits
             auto before = [&](int x) { return (uint32_t)uniform((int)lanes_sum<64>((float)max(t - x, 0))); };
             int most = t;
@@ -191,7 +193,7 @@ struct Place {
         } else if (!upto) {
             uint32_t past = 0;
             for (int s0 = 0; s0 < sequences; s0 += 64) {
-                const int t = s0 + l < sequences ? tiles_of(start, total, s0 + l) : 0;
+                const int t = tiles_of(start, sequences, total, s0 + l);
                 uint32_t to = t;
 #pragma unroll
                 for (int s = 1; s < 64; s <<= 1) {
@@ -219,7 +221,7 @@ struct Place {
                 n = uniform(min(step, n - last * step));
             }
             b = lo;
-            tiles = uniform(tiles_of(start, total, b));
+            tiles = uniform(tiles_of(start, sequences, total, b));
             rank = uniform((int)upto[b]) + tiles - 1 - (int)slot;
         }
     }
